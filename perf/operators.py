@@ -1,0 +1,462 @@
+"""Timed cases of the operators around the routed experts of one MoE block.
+
+A block's rows are normed (residual added, an 8-bit copy beside the bf16 one),
+the gate picks each token's experts, the rows are packed per expert-parallel
+rank, and a dense gated feed-forward, the shared expert, runs beside the routed
+ones.  Each case is one call of one of these operators, or for ``ffn_step`` the
+forward and backward pass of a training step.
+
+Keys of a case: op, rows (tokens), and
+  norm, norm_grad  d, x / res / y formats ("none": absent), q (MXFP8 rows too)
+  gate             E experts, k slots, score, groups of which topg are kept
+  dispatch         E experts on R ranks, k slots, d, q (MXFP8 rows, else bf16)
+  ffn, ffn_step    d, I
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+DTYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "bf16": 2, "none": 0}
+
+
+def listed():
+    return [
+        # one decoded token: residual and norm, rows for the shared expert in
+        # bf16 and for the routed ones in MXFP8; launch latency is all of it
+        dict(name="norm_token", op="norm", rows=1, d=7168, x="bf16", res="bf16", y="bf16", q=True),
+        # a prefill's rows as the layer before leaves them: the combine's
+        # float32 sums onto a bf16 residual stream
+        dict(name="norm_prefill", op="norm", rows=8191, d=6144, x="f32", res="bf16", y="bf16",
+             q=True),
+        # the gradients of that norm in a training step
+        dict(name="norm_grad", op="norm_grad", rows=4096, d=7168, x="bf16", res="bf16", y="bf16",
+             q=False),
+        # a few decoded tokens choose among 256 experts in groups, with the
+        # balancing bias
+        dict(name="gate_tokens", op="gate", rows=9, E=256, k=8, score="sigmoid", groups=8, topg=4),
+        # eight replicas' prefill tokens of the 160-expert layer
+        dict(name="gate_prefill", op="gate", rows=65536, E=160, k=8, score="softmax", groups=1,
+             topg=1),
+        # a few decoded tokens packed for eight ranks of 32 experts
+        dict(name="dispatch_tokens", op="dispatch", rows=13, E=256, R=8, k=8, d=7168, q=False),
+        # one replica's prefill packed for ten ranks of 16 experts, 8-bit rows
+        dict(name="dispatch_prefill", op="dispatch", rows=8192, E=160, R=10, k=8, d=6144, q=True),
+        # the shared expert of one token: its weights are streamed once
+        dict(name="ffn_token", op="ffn", rows=1, d=4096, I=2048),
+        # a decode batch
+        dict(name="ffn_batch", op="ffn", rows=61, d=7168, I=2048),
+        # a short prompt
+        dict(name="ffn_ragged", op="ffn", rows=777, d=6144, I=2560),
+        # one replica's prefill of the widest layer
+        dict(name="ffn_prefill", op="ffn", rows=8192, d=7168, I=2048),
+        # a training step's forward and backward pass
+        dict(name="ffn_step", op="ffn_step", rows=4095, d=4096, I=2048),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(lo * (hi / lo) ** rng.random()))
+
+
+def draw(rng):
+    op = rng.choice(["norm", "norm", "norm_grad", "gate", "gate", "dispatch", "dispatch", "ffn",
+                     "ffn", "ffn", "ffn_step"])
+    # widths: the layers' own, and ones that are multiples of the 32-channel
+    # block only
+    d = rng.choice([256, 1024, 2048, 2304, 4096, 6144, 7168, 32 * rng.randint(9, 95)])
+    rows = _log_int(rng, 1, 8192)
+    if op == "norm":
+        # an 8-bit output, a wide one, or both
+        y, q = rng.choice([("bf16", True), ("bf16", False), ("none", True), ("f32", False)])
+        if not q:  # any width at all without the 32-channel blocks
+            d = rng.choice([d, _log_int(rng, 65, 7168)])
+        return dict(op=op, rows=rows, d=d, x=rng.choice(["f32", "bf16"]),
+                    res=rng.choice(["f32", "bf16", "none"]), y=y, q=q)
+    if op == "norm_grad":
+        return dict(op=op, rows=rows, d=rng.choice([d, _log_int(rng, 65, 7168)]),
+                    x=rng.choice(["f32", "bf16"]), res=rng.choice(["bf16", "none"]),
+                    y=rng.choice(["f32", "bf16"]), q=False)
+    if op == "gate":
+        score, E, g = rng.choice([("softmax", rng.randint(8, 300), 1), ("softmax", 64, 1),
+                                  ("sigmoid", 256, 8), ("sigmoid", 160, 1), ("sigmoid", 96, 4)])
+        return dict(op=op, rows=_log_int(rng, 1, 65536), E=E, k=rng.randint(1, 8), score=score,
+                    groups=g, topg=(g + 1) // 2)
+    if op == "dispatch":
+        R, per = rng.choice([(8, 8), (8, 32), (10, 16), (1, 64), (5, 12)])
+        return dict(op=op, rows=rows, E=R * per, R=R, k=rng.randint(1, 8), d=min(d, 6144),
+                    q=rng.random() < 0.5)
+    d = rng.choice([256, 1024, 2304, 4096, 6144, 8 * rng.randint(40, 380)])
+    I = rng.choice([128, 1024, 1408, 2048, 8 * rng.randint(20, 250)])
+    return dict(op=op, rows=min(rows, 4095) if op == "ffn_step" else rows, d=d, I=I)
+
+
+def row_bytes(d):
+    """An MXFP8 row: d codes, d / 32 scales, padded to 16 bytes."""
+    return (d + d // 32 + 15) // 16 * 16
+
+
+def work(c):
+    T, op = c["rows"], c["op"]
+    if op == "norm":
+        el = SIZE[c["x"]] + 2 * SIZE[c["res"]] + SIZE[c["y"]] + (1 + 1 / 32 if c["q"] else 0)
+        return {"bytes": T * c["d"] * el + 4 * c["d"], "flops": 6 * T * c["d"]}
+    if op == "norm_grad":
+        # s, dy and the residual stream's gradient in, dx out
+        el = SIZE[c["x"]] + SIZE[c["y"]] + (2 if c["res"] != "none" else 1) * SIZE[c["x"]]
+        return {"bytes": T * c["d"] * el + 8 * c["d"], "flops": 10 * T * c["d"]}
+    if op == "gate":
+        return {"bytes": T * (4 * c["E"] + 8 * c["k"]), "flops": T * c["E"] * c["k"]}
+    if op == "dispatch":
+        # rows and metadata in; expected copies out for experts drawn evenly
+        n = T * c["R"] * (1 - math.prod((c["E"] - c["E"] // c["R"] - j) / (c["E"] - j)
+                                        for j in range(c["k"])))
+        row = row_bytes(c["d"]) if c["q"] else 2 * c["d"]
+        return {"bytes": (T + n) * (row + 8 * c["k"]), "flops": T * c["k"]}
+    d, I = c["d"], c["I"]
+    if op == "ffn":
+        return {"bytes": 2 * (2 * T * d + 3 * d * I), "flops": 6 * T * d * I}
+    return {"bytes": 2 * (4 * T * d + 6 * d * I), "flops": 18 * T * d * I}
+
+
+# ------------------------------------------------------------------ inputs
+
+def _gate_inputs(c, g):
+    """Logits N(0, 1), as a gate's projection leaves them, with some rows that
+    have all but a few experts masked.  A row in which a choice between two
+    experts (or groups) hangs on the last bits of the score is replaced."""
+    T, E, k = c["rows"], c["E"], min(c["k"], c["E"])
+    logits = torch.randn(T, E, device="cuda", generator=g)
+    open_ = torch.rand(T, E, device="cuda", generator=g) < 0.02
+    some = torch.arange(T, device="cuda") % 17 == 3
+    logits.masked_fill_(some[:, None] & ~open_, -math.inf)
+    bias = None
+    if c["score"] == "sigmoid":
+        bias = torch.randn(E, device="cuda", generator=g).mul_(0.05)
+        key = torch.sigmoid(logits.double()) + bias.double()
+        key.masked_fill_(logits == -math.inf, -math.inf)
+        near = torch.zeros(T, dtype=torch.bool, device="cuda")
+        if c["groups"] > 1:
+            top = key.view(T, c["groups"], -1).topk(2, -1)[0].clamp_min(-9.0).sum(-1)
+            top = top.sort(-1)[0].diff(dim=-1)
+            near |= ((top < 1e-5) & (top > 0)).any(-1)
+        gap = -key.topk(min(c["groups"] * k + 1, E), -1)[0].diff(dim=-1)
+        near |= (gap < 1e-6).any(-1)  # false between two masked experts (NaN)
+        good = torch.argmin((near | some).int())
+        logits = torch.where(near[:, None], logits[good], logits)
+    return logits, bias
+
+
+def prepare(c, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    T, op = c["rows"], c["op"]
+
+    def normal(*shape, std=1.0, dtype="bf16"):
+        return torch.randn(*shape, device="cuda", generator=g).mul_(std).to(DTYPE[dtype])
+
+    s = dict(case=c)
+    if op in ("norm", "norm_grad"):
+        d = c["d"]
+        s["x"] = normal(T, d, dtype=c["x"])
+        s["w"] = 1.0 + normal(d, std=0.1, dtype="f32")
+        if op == "norm":
+            s["res"] = None if c["res"] == "none" else normal(T, d, std=3.0, dtype=c["res"])
+        else:  # the gradients of the norm's output and of the residual stream
+            s["dy"] = normal(T, d, std=0.1, dtype=c["y"])
+            s["res"] = None if c["res"] == "none" else normal(T, d, std=0.1, dtype=c["x"])
+    elif op == "gate":
+        s["logits"], s["bias"] = _gate_inputs(c, g)
+    elif op == "dispatch":
+        E, k = c["E"], c["k"]
+        s["ids"] = torch.rand(T, E, device="cuda", generator=g).topk(k, -1)[1].to(torch.int32)
+        s["w"] = torch.rand(T, k, device="cuda", generator=g)
+        if c["q"]:  # MXFP8 rows, as bytes
+            s["x"] = torch.randint(0, 256, (T, row_bytes(c["d"])), dtype=torch.uint8,
+                                   device="cuda", generator=g)
+        else:
+            s["x"] = normal(T, c["d"])
+    else:
+        d, I = c["d"], c["I"]
+        s["x"] = normal(T, d)
+        s["wg"], s["wu"] = normal(d, I, std=0.02), normal(d, I, std=0.02)
+        s["wd"] = normal(I, d, std=0.02)
+        if op == "ffn_step":
+            s["dy"] = normal(T, d, std=0.01)
+    return s
+
+
+# ---------------------------------------------------- the framework's calls
+
+def _plan(s):
+    """Descriptors, output buffers and workspace, as a program keeps them."""
+    from paper_2609_33252_amd import cep
+    c = s["case"]
+    T, op = c["rows"], c["op"]
+    code = {"f32": cep.CEP_F32, "bf16": cep.CEP_BF16, "none": cep.CEP_BF16}
+    p = dict(cep=cep)
+
+    def empty(*shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device="cuda")
+
+    def space(n):
+        return empty(max(int(n), 16), dtype=torch.uint8)
+
+    if op == "norm":
+        d = c["d"]
+        p["desc"] = cep.make_norm(rows=T, d=d, x_dtype=code[c["x"]], res_dtype=code[c["res"]],
+                                  w_dtype=cep.CEP_F32, y_dtype=code[c["y"]], eps=EPS)
+        p["res"] = None if s["res"] is None else torch.empty_like(s["res"])
+        p["y"] = None if c["y"] == "none" else empty(T, d, dtype=DTYPE[c["y"]])
+        p["codes"] = empty(T, d, dtype=torch.float8_e4m3fn) if c["q"] else None
+        p["scales"] = empty(T, d // 32, dtype=torch.float8_e8m0fnu) if c["q"] else None
+    elif op == "norm_grad":
+        d = c["d"]
+        p["desc"] = cep.make_norm(rows=T, d=d, x_dtype=code[c["x"]], res_dtype=code[c["x"]],
+                                  w_dtype=cep.CEP_F32, y_dtype=code[c["y"]], eps=EPS)
+        p["dx"], p["dw"] = torch.empty_like(s["x"]), empty(d, dtype=torch.float32)
+        p["ws"] = space(cep.cep_rms_norm_workspace(p["desc"]))
+    elif op == "gate":
+        p["desc"] = cep.make_gate(rows=T, n_experts=c["E"], top_k=c["k"],
+                                  score=cep.CEP_SOFTMAX if c["score"] == "softmax"
+                                  else cep.CEP_SIGMOID, n_groups=c["groups"],
+                                  topk_groups=c["topg"], normalize=1, scale=1.0)
+        p["ids"] = empty(T, c["k"], dtype=torch.int32)
+        p["w"] = empty(T, c["k"], dtype=torch.float32)
+    elif op == "dispatch":
+        R, k = c["R"], c["k"]
+        cap = T * min(k, R)
+        row = s["x"][0].numel() * s["x"].element_size()
+        p["desc"] = cep.make_dispatch(rows=T, top_k=k, n_ranks=R, experts_per_rank=c["E"] // R,
+                                      row_bytes=row, capacity=cap)
+        zeros = dict(device="cuda", dtype=torch.int32)
+        p["plan"] = torch.zeros(2 * R + 2, **zeros)
+        p["token"], p["id"] = torch.zeros(cap, **zeros), torch.zeros(cap, k, **zeros)
+        p["w"] = torch.zeros(cap, k, device="cuda")
+        p["x"] = torch.zeros(cap, s["x"].shape[1], dtype=s["x"].dtype, device="cuda")
+        p["ws"] = space(cep.cep_dispatch_workspace(p["desc"]))
+    else:
+        d, I = c["d"], c["I"]
+        p["desc"] = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I)
+        p["y"] = empty(T, d)
+        back = op == "ffn_step"
+        if back:
+            p["pre"] = empty(T, 2, I, dtype=torch.float32)
+            p["dx"], p["dwd"] = empty(T, d), empty(I, d)
+            p["dwg"], p["dwu"] = empty(d, I), empty(d, I)
+        p["ws"] = space(cep.cep_gated_ffn_workspace(p["desc"], back))
+    return p
+
+
+def _run_own(s):
+    if "plan" not in s:
+        s["plan"] = _plan(s)
+    p, op = s["plan"], s["case"]["op"]
+    cep, desc = p["cep"], p["desc"]
+    if op == "norm":
+        cep.cep_rms_norm(desc, s["x"], s["w"], residual=s["res"], res_out=p["res"], y=p["y"],
+                         codes=p["codes"], scales=p["scales"])
+        return dict(res=p["res"], y=p["y"], codes=p["codes"], scales=p["scales"])
+    if op == "norm_grad":
+        cep.cep_rms_norm_backward(desc, s["x"], s["w"], s["dy"], s["res"], p["dx"], p["dw"],
+                                  p["ws"])
+        return dict(dx=p["dx"], dw=p["dw"])
+    if op == "gate":
+        cep.cep_gate_topk(desc, s["logits"], s["bias"], p["ids"], p["w"])
+        return dict(ids=p["ids"], w=p["w"])
+    if op == "dispatch":
+        cep.cep_dispatch(desc, s["ids"], s["w"], s["x"], p["plan"], p["token"], p["id"], p["w"],
+                         p["x"], p["ws"])
+        return dict(plan=p["plan"], token=p["token"], id=p["id"], w=p["w"], x=p["x"])
+    w = (s["wg"], s["wu"], s["wd"])
+    if op == "ffn":
+        cep.cep_gated_ffn(desc, s["x"], *w, p["y"], p["ws"])
+        return dict(y=p["y"])
+    cep.cep_gated_ffn(desc, s["x"], *w, p["y"], p["ws"], preact=p["pre"])
+    cep.cep_gated_ffn_backward(desc, s["dy"], s["x"], *w, p["pre"], p["dx"], p["dwg"], p["dwu"],
+                               p["dwd"], p["ws"])
+    return dict(y=p["y"], dx=p["dx"], dwg=p["dwg"], dwu=p["dwu"], dwd=p["dwd"])
+
+
+# ---------------------------------------------------------- the plain forms
+
+def _norm(c, x, w, res):
+    s = x.float() if res is None else x.float() + res.float()
+    y = s * torch.rsqrt((s * s).mean(-1, keepdim=True) + EPS) * w
+    out = dict(res=None if res is None else s.to(res.dtype),
+               y=None if c["y"] == "none" else y.to(DTYPE[c["y"]]), codes=None, scales=None)
+    if c["q"]:
+        b = y.view(*y.shape[:-1], -1, 32)
+        # a block's exponent: that of its largest magnitude, less e4m3's own 8
+        e = torch.frexp(b.abs().amax(-1)).exponent.sub(1 + 8).clamp_min(-127)
+        q = torch.ldexp(b, -e[..., None]).clamp(-448.0, 448.0)
+        out["codes"] = q.view_as(y).to(torch.float8_e4m3fn)
+        out["scales"] = (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
+    return out
+
+
+def _norm_grad(x, w, dy, res):
+    s, dy = x.float(), dy.float()
+    inv = torch.rsqrt((s * s).mean(-1, keepdim=True) + EPS)
+    n, dn = s * inv, dy * w
+    dx = inv * (dn - n * (dn * n).mean(-1, keepdim=True))
+    if res is not None:
+        dx = dx + res.float()
+    return dict(dx=dx.to(x.dtype), dw=(dy * n).sum(0))
+
+
+def _gate(c, logits, bias):
+    T, E, k = c["rows"], c["E"], c["k"]
+    soft = c["score"] == "softmax"
+    shut = logits == -math.inf
+    score = torch.softmax(logits, -1) if soft else torch.sigmoid(logits)
+    key = logits if soft else (score + bias).masked_fill(shut, -math.inf)
+    if c["groups"] > 1:
+        two = key.view(T, c["groups"], -1).sort(dim=-1, descending=True)[0][..., :2]
+        total = two.masked_fill(two == -math.inf, 0.0).sum(-1)
+        total = total.masked_fill(two[..., 0] == -math.inf, -math.inf)
+        rank = total.sort(dim=-1, descending=True, stable=True)[1].argsort(-1)
+        keep = (rank < c["topg"]).repeat_interleave(E // c["groups"], -1)
+        key = key.masked_fill(~keep, -math.inf)
+    key, ids = key.sort(dim=-1, descending=True, stable=True)
+    key, ids = key[:, :k], ids[:, :k]
+    none = key == -math.inf
+    w = score.gather(-1, ids).masked_fill(none, 0.0)
+    total = w.sum(-1, keepdim=True)
+    w = torch.where(total > 0, w / total, 0.0)
+    return dict(ids=ids.masked_fill(none, -1).to(torch.int32), w=w)
+
+
+def _dispatch(c, ids, w, x):
+    T, R, k, per = c["rows"], c["R"], c["k"], c["E"] // c["R"]
+    cap, dev = T * min(k, R), x.device
+    ranks = torch.arange(R, device=dev)
+    there = (ids // per)[None] == ranks[:, None, None]
+    sent = there.any(-1)
+    at = (sent.flatten().cumsum(0) - 1).view(R, T)
+    at = torch.where(sent, at, cap).flatten()
+    total = sent.sum()
+
+    def place(v):  # the values of every (rank, token) at their place
+        out = torch.zeros(cap + 1, *v.shape[2:], dtype=v.dtype, device=dev)
+        out[at] = v.flatten(0, 1)
+        return out[:cap]
+
+    token = place(torch.arange(T, device=dev).expand(R, T))
+    live = torch.arange(cap, device=dev) < total
+    token = torch.where(live, token, 0)
+    here = torch.where(there, ids[None] - ranks[:, None, None] * per, -1)
+    counts = sent.sum(-1)
+    plan = torch.cat([counts.new_zeros(1), counts.cumsum(0), there.sum((1, 2)),
+                      counts.new_zeros(1)])
+    zero = torch.zeros((), dtype=x.dtype, device=dev)
+    return dict(plan=plan.to(torch.int32), token=token.to(torch.int32),
+                id=torch.where(live[:, None], place(here), 0).to(torch.int32),
+                w=torch.where(live[:, None], place(torch.where(there, w[None], 0.0)), 0.0),
+                x=torch.where(live[:, None], x[token], zero))
+
+
+def _ffn(x, wg, wu, wd, dy=None):
+    x, wg, wu, wd = x.float(), wg.float(), wu.float(), wd.float()
+    g, u = x @ wg, x @ wu
+    sig = 1.0 / (1.0 + torch.exp(-g))
+    h = g * sig * u
+    bf = torch.bfloat16
+    out = dict(y=(h @ wd).to(bf))
+    if dy is not None:
+        dy = dy.float()
+        dh = dy @ wd.T
+        dg = dh * u * sig * (1.0 + g * (1.0 - sig))
+        du = dh * g * sig
+        out |= dict(dx=(dg @ wg.T + du @ wu.T).to(bf), dwg=(x.T @ dg).to(bf),
+                    dwu=(x.T @ du).to(bf), dwd=(h.T @ dy).to(bf))
+    return out
+
+
+def run(s):
+    if own:
+        return _run_own(s)
+    c = s["case"]
+    if c["op"] == "norm":
+        return _norm(c, s["x"], s["w"], s["res"])
+    if c["op"] == "norm_grad":
+        return _norm_grad(s["x"], s["w"], s["dy"], s["res"])
+    if c["op"] == "gate":
+        return _gate(c, s["logits"], s["bias"])
+    if c["op"] == "dispatch":
+        return _dispatch(c, s["ids"], s["w"], s["x"])
+    return _ffn(s["x"], s["wg"], s["wu"], s["wd"], s.get("dy"))
+
+
+# --------------------------------------------------- definitions in 64 bits
+
+def exact(c, seed):
+    s = prepare(c, seed)
+    op, T = c["op"], c["rows"]
+    v = {k: t.double() for k, t in s.items()
+         if isinstance(t, torch.Tensor) and t.is_floating_point()}
+    if op == "norm":
+        z = v["x"] + v["res"] if s["res"] is not None else v["x"]
+        y = z / z.pow(2).mean(1, keepdim=True).add(EPS).sqrt() * v["w"]
+        out = dict(res=z if s["res"] is not None else None, y=y if c["y"] != "none" else None,
+                   codes=None, scales=None)
+        if c["q"]:  # the values that the codes round
+            scale = torch.exp2(torch.floor(torch.log2(
+                y.reshape(T, -1, 32).abs().max(2)[0].clamp_min(2.0 ** -119))) - 8)
+            out |= dict(codes=y / scale.repeat_interleave(32, 1), scales=scale)
+        return out
+    if op == "norm_grad":
+        z, d = v["x"], c["d"]
+        r = z.pow(2).mean(1, keepdim=True).add(EPS).sqrt()
+        a = v["dy"] * v["w"]
+        dx = a / r - z * (a * z).sum(1, keepdim=True) / (d * r ** 3)
+        return dict(dx=dx + v["res"] if s["res"] is not None else dx, dw=(v["dy"] * z / r).sum(0))
+    if op == "gate":
+        key = v["logits"]
+        if c["score"] == "sigmoid":
+            key = 1 / (1 + torch.exp(-key)) + v["bias"]
+            key = torch.where(v["logits"].isinf(), -math.inf, key)
+        if c["groups"] > 1:  # only experts of the kept groups
+            groups = key.reshape(T, c["groups"], -1)
+            best, second = groups.topk(2, 2)[0].unbind(2)
+            best = best + torch.where(second.isinf(), 0.0, second)
+            kept = torch.zeros_like(best).scatter(1, best.topk(c["topg"], 1)[1], 1.0)
+            key = torch.where(kept[..., None] > 0, groups, -math.inf).reshape(T, -1)
+        key, ids = key.topk(c["k"], 1)
+        picked = v["logits"].gather(1, ids).masked_fill(key.isinf(), -math.inf)
+        if c["score"] == "softmax":
+            w = torch.exp(picked - picked.max(1, keepdim=True)[0])
+        else:
+            w = 1 / (1 + torch.exp(-picked))
+        return dict(ids=None, w=(w / w.sum(1, keepdim=True)).nan_to_num(0.0))
+    if op == "dispatch":
+        out = {k: None for k in ("plan", "token", "id", "w", "x")}
+        ids, per = s["ids"].cpu(), c["E"] // c["R"]
+        cap, at = T * min(c["k"], c["R"]), 0
+        w = torch.zeros(cap, c["k"], dtype=torch.float64, device="cuda")
+        x = None if c["q"] else torch.zeros(cap, c["d"], dtype=torch.float64, device="cuda")
+        for r in range(c["R"]):  # one rank's tokens, in order
+            here = (ids >= r * per) & (ids < (r + 1) * per)
+            tok = here.any(1).nonzero()[:, 0].cuda()
+            w[at:at + len(tok)] = (v["w"] * here.cuda())[tok]
+            if x is not None:
+                x[at:at + len(tok)] = v["x"][tok]
+            at += len(tok)
+        return out | dict(w=w, x=x)
+    g, u = v["x"].matmul(v["wg"]), v["x"].matmul(v["wu"])
+    silu = g / (1 + torch.exp(-g))
+    out = dict(y=torch.matmul(silu * u, v["wd"]))
+    if op == "ffn_step":
+        dh = v["dy"].matmul(v["wd"].t().contiguous())
+        slope = silu / g + silu - silu * silu / g
+        slope = torch.where(g == 0, 0.5, slope)
+        dg, du = dh * u * slope, dh * silu
+        out["dx"] = dg.matmul(v["wg"].t().contiguous()) + du.matmul(v["wu"].t().contiguous())
+        xt = v["x"].t().contiguous()
+        out |= dict(dwg=xt.matmul(dg), dwu=xt.matmul(du),
+                    dwd=(silu * u).t().contiguous().matmul(v["dy"]))
+    return out

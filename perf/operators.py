@@ -292,7 +292,7 @@ def _norm(c, x, w, res):
     if c["q"]:
         b = y.view(*y.shape[:-1], -1, 32)
         # a block's exponent: that of its largest magnitude, less e4m3's own 8
-        e = torch.frexp(b.abs().amax(-1)).exponent.sub(1 + 8).clamp_min(-127)
+        e = torch.frexp(b.abs().amax(-1).clamp_min(2.0 ** -120)).exponent.sub(1 + 8).clamp_min(-127)
         q = torch.ldexp(b, -e[..., None]).clamp(-448.0, 448.0)
         out["codes"] = q.view_as(y).to(torch.float8_e4m3fn)
         out["scales"] = (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)

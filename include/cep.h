@@ -69,9 +69,14 @@ enum cep_dtype {
   CEP_FP8_E4M3_B128 = 2, /* weights only: OCP e4m3fn codes, one float32 scale
                            per 128x128 block; activations and h run as MXFP8
                            (e4m3, one E8M0 scale per 32) inside the library */
-  CEP_MXFP4 = 3          /* weights only: OCP MXFP4 (e2m1 codes, one E8M0 scale
+  CEP_MXFP4 = 3,         /* weights only: OCP MXFP4 (e2m1 codes, one E8M0 scale
                            per 32 along K; Section 4.1's DeepSeek-V4 experts);
                            activations and h run as MXFP8 inside the library */
+  CEP_MXFP8 = 4         /* token rows only: e4m3 codes with one E8M0 scale per
+                           32 channels (a row: d code bytes, d/32 scale bytes,
+                           padded to 16), as cep_rms_norm writes them; taken
+                           by contexts with e4m3 or MXFP4 weights, which use
+                           them as they are */
 };
 
 /* How cep_weight_fetch brings a fetched expert's weights (Appendix C,
@@ -100,7 +105,8 @@ typedef struct {
   int max_replicas;           /* R_max                                        */
   int max_tokens_per_replica; /* T_max; also the row stride of `out` per replica */
   int w_dtype;                /* cep_dtype of the expert weights              */
-  int x_dtype;                /* cep_dtype of the token rows (F32 or BF16)    */
+  int x_dtype;                /* cep_dtype of the token rows (F32, BF16, or
+                                 MXFP8 with e4m3 / MXFP4 weights)             */
   int n_streams;              /* stream slots for batches, 1..8               */
   int max_pairs_per_batch;    /* capacity of one batch in valid pairs; 0 means
                                  max_replicas * max_tokens_per_replica * top_k */
@@ -334,6 +340,149 @@ int cep_destroy(cep_ctx *ctx);
 int cep_ffn_noalloc(cep_ctx *ctx, int replica, int n_rows, int n_pairs, const int32_t *token_idx,
                     const void *x, const int32_t *topk_id, const float *topk_w, float *out,
                     hipStream_t s);
+
+/* ------------------------------------------------------------------------
+ * Operators around the routed experts of one MoE block: the norm before the
+ * gate, the gate's choice, the packing of tokens per expert-parallel rank, and
+ * a dense gated feed-forward (a shared expert), with gradients where the
+ * operator's own inputs are trained.
+ *
+ * They need no context.  Work is enqueued on stream s of the current device
+ * and nothing is allocated: an operator that needs scratch takes it from the
+ * caller (cep_*_workspace gives the bytes; contents need not be kept between
+ * calls, and calls that overlap in time need one each), so every call can be
+ * captured in a graph.  Arguments are checked on the host before any work:
+ * CEP_EINVAL for a bad descriptor, NULL or misaligned pointer, CEP_ENOMEM for
+ * a workspace or output capacity that is too small, CEP_EHIP when a launch
+ * fails, with a message in cep_last_error(NULL).  rows = 0 is valid.  Row
+ * strides of 0 mean dense rows.  Results do not depend on timing: two calls
+ * on the same inputs give the same bits.
+ */
+
+/* Bytes of one token row of width d as cep_submit_chunk takes it: 4d for
+ * CEP_F32, 2d for CEP_BF16, d + d/32 rounded up to 16 for CEP_MXFP8 (d a
+ * multiple of 32).  0 for anything else. */
+size_t cep_row_bytes(int d, int x_dtype);
+
+typedef struct {
+  int rows;               /* 0..2^24                                          */
+  int d;                  /* 1..32768; a multiple of 32 for MXFP8 output      */
+  int x_dtype, res_dtype, w_dtype, y_dtype; /* CEP_F32 or CEP_BF16            */
+  float eps;
+  int64_t ld_x, ld_res, ld_y;       /* row strides in elements                */
+  int64_t ld_codes, ld_scales;      /* row strides in bytes                   */
+} cep_norm_desc;
+
+/* Root-mean-square norm of each row, with the residual's addition:
+ *   s = x + residual;  y = s * w / sqrt(mean(s^2) + eps)     (in float32)
+ * x [rows][d] (x_dtype); residual (res_dtype, NULL: none); w [d] (w_dtype).
+ * Outputs, at least one of y and codes: res_out (res_dtype, may be NULL and
+ * may be `residual` itself) gets s; y (y_dtype, may be x itself if the types
+ * and strides agree) gets the norm, which is taken of s before s is rounded to
+ * res_dtype; codes and scales get y as MXFP8, quantised from float32: e4m3
+ * codes [rows][d], E8M0 scales [rows][d/32].  A block of 32 that holds an
+ * infinity or NaN gets scale code 255 (NaN).  Rows for cep_submit_chunk
+ * (CEP_MXFP8): scales = codes + d, both strides cep_row_bytes(d, CEP_MXFP8). */
+int cep_rms_norm(const cep_norm_desc *desc, const void *x, const void *residual, const void *w,
+                 void *res_out, void *y, uint8_t *codes, uint8_t *scales, hipStream_t s);
+
+/* Gradient of cep_rms_norm.  x (x_dtype): the rows that were normed (x, or
+ * res_out where there was a residual); dy (y_dtype, stride ld_y): the gradient
+ * of y; dres (res_dtype, stride ld_res, NULL: none): the gradient of res_out,
+ * which joins dx.  dx (res_dtype, stride ld_res, may be dres itself): the
+ * gradient of s, hence of x and of the residual; dw [d] (w_dtype, written, not
+ * added to), summed in float32 over the rows in a fixed order. */
+size_t cep_rms_norm_workspace(const cep_norm_desc *desc);
+int cep_rms_norm_backward(const cep_norm_desc *desc, const void *x, const void *w, const void *dy,
+                          const void *dres, void *dx, void *dw, void *workspace,
+                          size_t workspace_bytes, hipStream_t s);
+
+enum cep_score {
+  CEP_SOFTMAX = 0, /* chosen by logit; coefficients from the softmax          */
+  CEP_SIGMOID = 1  /* chosen by sigmoid(logit) + bias; coefficients from the
+                      sigmoid, without the bias                               */
+};
+
+typedef struct {
+  int rows;            /* 0..2^24                                             */
+  int n_experts;       /* 1..1024                                             */
+  int top_k;           /* 1..16, at most n_experts                            */
+  int logit_dtype;     /* CEP_F32 or CEP_BF16                                 */
+  int score;           /* cep_score                                           */
+  int n_groups;        /* 0 or 1: none; up to 64, divides n_experts           */
+  int topk_groups;     /* groups kept, 1..n_groups (CEP_SIGMOID only)         */
+  int normalize;       /* nonzero: coefficients over the sum of the chosen's  */
+  float scale;         /* factor on every coefficient                         */
+  int64_t ld;          /* row stride of the logits in elements                */
+} cep_gate_desc;
+
+/* The gate's choice: for each row of logits [rows][n_experts] the top_k
+ * experts by descending key into topk_id [rows][top_k] and their coefficients
+ * into topk_w [rows][top_k] (float32).  Equal keys: the lower expert first.
+ * bias: float32 [n_experts], CEP_SIGMOID only, may be NULL.  With groups
+ * (consecutive experts), only experts of the topk_groups groups with the
+ * largest sum of their two best keys are chosen.  A logit of -inf or NaN masks
+ * its expert; a slot that no expert fills gets id -1 and coefficient 0.
+ * Coefficients: CEP_SOFTMAX the softmax over all experts, CEP_SIGMOID the
+ * sigmoid; with normalize over the chosen's sum (0 where that is 0). */
+int cep_gate_topk(const cep_gate_desc *desc, const void *logits, const float *bias,
+                  int32_t *topk_id, float *topk_w, hipStream_t s);
+
+typedef struct {
+  int rows;              /* 0..2^24                                           */
+  int top_k;             /* 1..16                                             */
+  int n_ranks;           /* 1..64; rank r holds experts                       */
+  int experts_per_rank;  /*   [r, r + 1) * experts_per_rank                   */
+  int capacity;          /* output rows, >= rows * min(top_k, n_ranks)        */
+  int64_t row_bytes;     /* 1..131072                                         */
+  int64_t ld_x;          /* row stride of x in bytes                          */
+} cep_dispatch_desc;
+
+/* Packs routed tokens rank by rank (Appendix C, "Asynchronous dispatch"):
+ * rank r's segment holds, in order, every token with an expert there, and is a
+ * chunk for that rank's cep_submit_chunk.  topk_id [rows][top_k] global ids
+ * (-1: empty slot), topk_w [rows][top_k], x [rows] rows of row_bytes bytes.
+ * Outputs: plan [2 n_ranks + 2] = segment offsets [n_ranks + 1] in rows, valid
+ * (token, slot) pairs per rank [n_ranks], number of ids that no rank holds
+ * (apart from -1; such slots are dropped); then for each sent row token_idx,
+ * out_id [.][top_k] (ids local to the rank, -1 for the other ranks' slots),
+ * out_w [.][top_k] (0 there) and out_x [.][row_bytes].  Rows past the last
+ * segment are left as they are. */
+size_t cep_dispatch_workspace(const cep_dispatch_desc *desc);
+int cep_dispatch(const cep_dispatch_desc *desc, const int32_t *topk_id, const float *topk_w,
+                 const void *x, int32_t *plan, int32_t *token_idx, int32_t *out_id, float *out_w,
+                 void *out_x, void *workspace, size_t workspace_bytes, hipStream_t s);
+
+typedef struct {
+  int rows;              /* 0..2^24                                           */
+  int d_model, d_ff;     /* multiples of 8, 8..32768                          */
+  int64_t ld_x;          /* row strides in elements, multiples of 8: x,       */
+  int64_t ld_y;          /*   y and dy,                                       */
+  int64_t ld_dx;         /*   dx                                              */
+} cep_gated_ffn_desc;
+
+/* Dense gated feed-forward, y = (silu(x Wg) * (x Wu)) Wd, in bf16 with float32
+ * accumulation.  x [rows][d_model]; w_gate, w_up [d_model][d_ff]; w_down
+ * [d_ff][d_model] (the math orientation of cep_weights, read as they are);
+ * y [rows][d_model].  The hidden row is rounded to bf16 once, for the second
+ * product.  preact (NULL: not kept) gets x Wg and x Wu, float32
+ * [rows][2][d_ff], for cep_gated_ffn_backward.  All pointers 16-byte aligned;
+ * y may not overlap x.  workspace: cep_gated_ffn_workspace(desc, 0) bytes. */
+size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *desc, int backward);
+int cep_gated_ffn(const cep_gated_ffn_desc *desc, const void *x, const void *w_gate,
+                  const void *w_up, const void *w_down, void *y, float *preact, void *workspace,
+                  size_t workspace_bytes, hipStream_t s);
+
+/* Its gradient: from dy [rows][d_model] (stride ld_y), the forward call's x,
+ * weights and preact, the gradients dx [rows][d_model], dw_gate, dw_up
+ * [d_model][d_ff] and dw_down [d_ff][d_model], bf16, written, not added to.
+ * The gradients of the two projections and the hidden row are rounded to bf16
+ * once, for the products that follow.  workspace:
+ * cep_gated_ffn_workspace(desc, 1) bytes. */
+int cep_gated_ffn_backward(const cep_gated_ffn_desc *desc, const void *dy, const void *x,
+                           const void *w_gate, const void *w_up, const void *w_down,
+                           const float *preact, void *dx, void *dw_gate, void *dw_up,
+                           void *dw_down, void *workspace, size_t workspace_bytes, hipStream_t s);
 
 /* ------------------------------------------------------------------------
  * FFN throughput profile (host only; no GPU work).

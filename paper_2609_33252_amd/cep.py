@@ -14,7 +14,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcep.so")
 
 CEP_OK, CEP_EINVAL, CEP_ENOMEM, CEP_EHIP, CEP_ESTATE, CEP_EBUSY = 0, -1, -2, -3, -4, -5
-CEP_F32, CEP_BF16, CEP_FP8_E4M3_B128, CEP_MXFP4 = 0, 1, 2, 3
+CEP_F32, CEP_BF16, CEP_FP8_E4M3_B128, CEP_MXFP4, CEP_MXFP8 = 0, 1, 2, 3, 4
+CEP_SOFTMAX, CEP_SIGMOID = 0, 1
 CEP_WAIT_ALL, CEP_PER_CHUNK, CEP_THRESHOLD = 0, 1, 2
 CEP_FETCH_COPY, CEP_FETCH_IN_PLACE, CEP_FETCH_FAIL_COPY = 0, 1, 2
 STATUS_NAMES = {0: "CEP_OK", -1: "CEP_EINVAL", -2: "CEP_ENOMEM", -3: "CEP_EHIP",
@@ -24,7 +25,10 @@ EXPORTED = ["cep_packed_expert_bytes", "cep_pack_experts", "cep_init_experts", "
             "cep_begin_layer", "cep_submit_chunk", "cep_flush", "cep_weight_fetch",
             "cep_combine", "cep_get_batch_routing", "cep_get_batch_count", "cep_get_stats",
             "cep_get_status", "cep_last_error", "cep_destroy", "cep_set_phase_timing",
-            "cep_set_fetch_mode", "cep_ffn_noalloc",
+            "cep_set_fetch_mode", "cep_ffn_noalloc", "cep_row_bytes",
+            "cep_rms_norm", "cep_rms_norm_workspace", "cep_rms_norm_backward", "cep_gate_topk",
+            "cep_dispatch_workspace", "cep_dispatch", "cep_gated_ffn_workspace", "cep_gated_ffn",
+            "cep_gated_ffn_backward",
             "cep_profile_create",
             "cep_profile_peak", "cep_profile_theta", "cep_profile_eta", "cep_profile_latency",
             "cep_profile_destroy", "cep_oewf_create", "cep_oewf_begin_layer", "cep_oewf_set_rank",
@@ -47,6 +51,32 @@ class cep_weights(ctypes.Structure):
     _fields_ = [("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p),
                 ("w_down", ctypes.c_void_p), ("s_gate", ctypes.c_void_p),
                 ("s_up", ctypes.c_void_p), ("s_down", ctypes.c_void_p)]
+
+
+class cep_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("d", ctypes.c_int), ("x_dtype", ctypes.c_int),
+                ("res_dtype", ctypes.c_int), ("w_dtype", ctypes.c_int),
+                ("y_dtype", ctypes.c_int), ("eps", ctypes.c_float), ("ld_x", ctypes.c_int64),
+                ("ld_res", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+                ("ld_codes", ctypes.c_int64), ("ld_scales", ctypes.c_int64)]
+
+
+class cep_gate_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("n_experts", ctypes.c_int), ("top_k", ctypes.c_int),
+                ("logit_dtype", ctypes.c_int), ("score", ctypes.c_int),
+                ("n_groups", ctypes.c_int), ("topk_groups", ctypes.c_int),
+                ("normalize", ctypes.c_int), ("scale", ctypes.c_float), ("ld", ctypes.c_int64)]
+
+
+class cep_dispatch_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("top_k", ctypes.c_int), ("n_ranks", ctypes.c_int),
+                ("experts_per_rank", ctypes.c_int), ("capacity", ctypes.c_int),
+                ("row_bytes", ctypes.c_int64), ("ld_x", ctypes.c_int64)]
+
+
+class cep_gated_ffn_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("d_model", ctypes.c_int), ("d_ff", ctypes.c_int),
+                ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_dx", ctypes.c_int64)]
 
 
 class cep_oewf_fetch(ctypes.Structure):
@@ -83,7 +113,6 @@ def lib():
         vp, i32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
         P = ctypes.POINTER
         L.cep_packed_expert_bytes.argtypes = [P(cep_config)]
-        L.cep_packed_expert_bytes.restype = sz
         L.cep_pack_experts.argtypes = [P(cep_config), P(cep_weights), i32, i32, vp, vp]
         L.cep_init_experts.argtypes = [P(vp), P(cep_config), P(cep_weights), vp, vp]
         L.cep_set_policy.argtypes = [vp, i32, i32, i32]
@@ -104,6 +133,16 @@ def lib():
         L.cep_set_phase_timing.argtypes = [vp, i32]
         L.cep_set_fetch_mode.argtypes = [vp, i32]
         L.cep_ffn_noalloc.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.cep_row_bytes.argtypes = [i32, i32]
+        L.cep_rms_norm.argtypes = [P(cep_norm_desc)] + [vp] * 8
+        L.cep_rms_norm_workspace.argtypes = [P(cep_norm_desc)]
+        L.cep_rms_norm_backward.argtypes = [P(cep_norm_desc)] + [vp] * 7 + [sz, vp]
+        L.cep_gate_topk.argtypes = [P(cep_gate_desc)] + [vp] * 5
+        L.cep_dispatch_workspace.argtypes = [P(cep_dispatch_desc)]
+        L.cep_dispatch.argtypes = [P(cep_dispatch_desc)] + [vp] * 9 + [sz, vp]
+        L.cep_gated_ffn_workspace.argtypes = [P(cep_gated_ffn_desc), i32]
+        L.cep_gated_ffn.argtypes = [P(cep_gated_ffn_desc)] + [vp] * 7 + [sz, vp]
+        L.cep_gated_ffn_backward.argtypes = [P(cep_gated_ffn_desc)] + [vp] * 11 + [sz, vp]
         i64, f64 = ctypes.c_int64, ctypes.c_double
         L.cep_profile_create.argtypes = [P(i64), P(f64), i32, P(vp)]
         L.cep_profile_peak.argtypes = [vp]
@@ -124,7 +163,9 @@ def lib():
         L.cep_oewf_destroy.argtypes = [vp]
         L.cep_oewf_destroy.restype = None
         for name in EXPORTED:
-            if name not in ("cep_packed_expert_bytes", "cep_last_error", "cep_profile_peak",
+            if name.endswith("_bytes") or name.endswith("_workspace"):
+                getattr(L, name).restype = sz
+            elif name not in ("cep_last_error", "cep_profile_peak",
                             "cep_profile_destroy", "cep_oewf_destroy"):
                 getattr(L, name).restype = i32
         _lib = L
@@ -299,6 +340,84 @@ def cep_last_error(ctx) -> str:
 
 def cep_destroy(ctx):
     _check(None, lib().cep_destroy(ctx))
+
+
+# ------------------------------------- operators around the routed experts
+# Descriptors: fields by name, the others 0 (dense rows, float32).
+
+def make_norm(**kw) -> cep_norm_desc:
+    return cep_norm_desc(**kw)
+
+
+def make_gate(**kw) -> cep_gate_desc:
+    return cep_gate_desc(**kw)
+
+
+def make_dispatch(**kw) -> cep_dispatch_desc:
+    return cep_dispatch_desc(**kw)
+
+
+def make_gated_ffn(**kw) -> cep_gated_ffn_desc:
+    return cep_gated_ffn_desc(**kw)
+
+
+def _room(t):
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def cep_row_bytes(d, x_dtype) -> int:
+    return int(lib().cep_row_bytes(d, x_dtype))
+
+
+def cep_rms_norm(desc, x, w, residual=None, res_out=None, y=None, codes=None, scales=None,
+                 stream=None):
+    _check(None, lib().cep_rms_norm(desc, _ptr(x), _ptr(residual), _ptr(w), _ptr(res_out),
+                                    _ptr(y), _ptr(codes), _ptr(scales), _stream(stream)))
+
+
+def cep_rms_norm_workspace(desc) -> int:
+    return int(lib().cep_rms_norm_workspace(desc))
+
+
+def cep_rms_norm_backward(desc, x, w, dy, dres, dx, dw, workspace, stream=None):
+    _check(None, lib().cep_rms_norm_backward(desc, _ptr(x), _ptr(w), _ptr(dy), _ptr(dres),
+                                             _ptr(dx), _ptr(dw), _ptr(workspace),
+                                             _room(workspace), _stream(stream)))
+
+
+def cep_gate_topk(desc, logits, bias, topk_id, topk_w, stream=None):
+    _check(None, lib().cep_gate_topk(desc, _ptr(logits), _ptr(bias), _ptr(topk_id), _ptr(topk_w),
+                                     _stream(stream)))
+
+
+def cep_dispatch_workspace(desc) -> int:
+    return int(lib().cep_dispatch_workspace(desc))
+
+
+def cep_dispatch(desc, topk_id, topk_w, x, plan, token_idx, out_id, out_w, out_x, workspace,
+                 stream=None):
+    _check(None, lib().cep_dispatch(desc, _ptr(topk_id), _ptr(topk_w), _ptr(x), _ptr(plan),
+                                    _ptr(token_idx), _ptr(out_id), _ptr(out_w), _ptr(out_x),
+                                    _ptr(workspace), _room(workspace), _stream(stream)))
+
+
+def cep_gated_ffn_workspace(desc, backward=False) -> int:
+    return int(lib().cep_gated_ffn_workspace(desc, 1 if backward else 0))
+
+
+def cep_gated_ffn(desc, x, w_gate, w_up, w_down, y, workspace, preact=None, stream=None):
+    _check(None, lib().cep_gated_ffn(desc, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                                     _ptr(y), _ptr(preact), _ptr(workspace), _room(workspace),
+                                     _stream(stream)))
+
+
+def cep_gated_ffn_backward(desc, dy, x, w_gate, w_up, w_down, preact, dx, dw_gate, dw_up,
+                           dw_down, workspace, stream=None):
+    _check(None, lib().cep_gated_ffn_backward(desc, _ptr(dy), _ptr(x), _ptr(w_gate), _ptr(w_up),
+                                              _ptr(w_down), _ptr(preact), _ptr(dx),
+                                              _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down),
+                                              _ptr(workspace), _room(workspace),
+                                              _stream(stream)))
 
 
 # ------------------------------------------------------------ FFN profile

@@ -1,0 +1,309 @@
+// Root-mean-square norm of token rows with the residual's addition and an
+// MXFP8 copy of the result, and its gradient, for gfx950.
+//
+//   s = x + r                         (float32; stored as the new residual)
+//   y = s * w / sqrt(mean(s^2) + eps)
+//   MXFP8(y): e4m3 codes, one E8M0 scale per 32 channels
+// and with n = s / sqrt(mean(s^2) + eps), a = dy * w:
+//   dx = (a - n * mean(a * n)) / sqrt(mean(s^2) + eps) + dres
+//   dw = sum over rows of dy * n
+//
+// Both read every input once and write every output once: bound by HBM.
+// A row stays in registers between the sum of its squares and its scaling.
+#include "block_ops.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace cep {
+namespace {
+
+struct NormArgs {
+  const void *x, *res, *w;
+  void *res_out, *y;
+  uint8_t *codes, *scales;
+  int64_t ld_x, ld_res, ld_y, ld_codes, ld_scales;
+  int rows, d, x_dtype, res_dtype, w_dtype, y_dtype;
+  float eps;
+};
+
+// Sum over the LANES threads of a row (a wave, or the whole block).
+template <int LANES>
+__device__ inline float row_sum(float v, float *lds) {
+  v = wave_sum(v);
+  if (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANES / 64; ++i) v += lds[i];
+  }
+  return v;
+}
+
+// Eight channels of a 32-channel block in each of four neighbouring lanes:
+// E8M0 scale 2^(floor(log2 amax) - 8), codes e4m3(v / scale) saturated at 448.
+// A block with an infinity or NaN gets the scale code 255 (NaN).  Returns the
+// lane's codes; *code gets the scale's code.
+__device__ inline uint2 mxfp8_block(const float v[8], int *code) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
+  m = max(m, (uint32_t)__shfl_xor((int)m, 1, 4));
+  m = max(m, (uint32_t)__shfl_xor((int)m, 2, 4));
+  const int ex = (int)(m >> 23);
+  *code = ex == 255 ? 255 : max(ex - 8, 0);
+  const int e = 127 - max(ex - 8, 0);
+  int w[2] = {0, 0};
+  float q[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) q[j] = fminf(fmaxf(ldexpf(v[j], e), -448.0f), 448.0f);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], w[h], false);
+    w[h] = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], w[h], true);
+  }
+  return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+}
+
+// LANES threads a row, NV groups of eight channels each.
+template <int LANES, int NV>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs a) {
+  __shared__ float lds[LANES > 64 ? LANES / 64 : 1];
+  const int lane = threadIdx.x % LANES;
+  const int row = LANES < 256 ? blockIdx.x * (256 / LANES) + threadIdx.x / LANES : blockIdx.x;
+  if (row >= a.rows) return;  // uniform over the row's threads
+  float s[NV][8];
+  float sq = 0.f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int c = (u * LANES + lane) * 8;
+    load8(a.x, a.x_dtype, row * a.ld_x + c, a.d - c, s[u]);
+  }
+  if (a.res) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (u * LANES + lane) * 8;
+      float r[8];
+      load8(a.res, a.res_dtype, row * a.ld_res + c, a.d - c, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[u][j] += r[j];
+      if (a.res_out) store8(a.res_out, a.res_dtype, row * a.ld_res + c, a.d - c, s[u]);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sq = fmaf(s[u][j], s[u][j], sq);
+  const float inv = 1.0f / sqrtf(row_sum<LANES>(sq, lds) / (float)a.d + a.eps);
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int c = (u * LANES + lane) * 8;
+    if (c >= a.d) continue;
+    float w[8], y[8];
+    load8(a.w, a.w_dtype, c, a.d - c, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = s[u][j] * inv * w[j];
+    if (a.y) store8(a.y, a.y_dtype, row * a.ld_y + c, a.d - c, y);
+    if (a.codes) {  // d is a multiple of 32: whole blocks
+      int code;
+      const uint2 q = mxfp8_block(y, &code);
+      *(uint2 *)(a.codes + row * a.ld_codes + c) = q;
+      if ((lane & 3) == 0) a.scales[row * a.ld_scales + c / kMxBlock] = (uint8_t)code;
+    }
+  }
+}
+
+struct NormGradArgs {
+  const void *s, *w, *dy, *dres;
+  void *dx;
+  float *part;  // [blocks][d] partial sums of dw
+  int64_t ld_s, ld_dy, ld_dx;
+  int rows, d, s_dtype, dx_dtype, w_dtype, dy_dtype;
+  float eps;
+};
+
+// Block b takes rows b, b + gridDim.x, ... and keeps its part of dw in
+// registers; the parts are summed in block order by k_rms_norm_dw, so dw does
+// not depend on which block ran first.
+template <int LANES, int NV>
+__global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
+  __shared__ float lds[2][LANES / 64];
+  const int lane = threadIdx.x;
+  float dw[NV][8] = {};
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    float s[NV][8], dy[NV][8];
+    float sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (u * LANES + lane) * 8;
+      float w[8];
+      load8(a.s, a.s_dtype, row * a.ld_s + c, a.d - c, s[u]);
+      load8(a.dy, a.dy_dtype, row * a.ld_dy + c, a.d - c, dy[u]);
+      load8(a.w, a.w_dtype, c, a.d - c, w);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sq = fmaf(s[u][j], s[u][j], sq);
+        dot = fmaf(dy[u][j] * w[j], s[u][j], dot);
+      }
+    }
+    sq = wave_sum(sq);
+    dot = wave_sum(dot);
+    __syncthreads();  // the row before has read its sums
+    if ((lane & 63) == 0) {
+      lds[0][lane >> 6] = sq;
+      lds[1][lane >> 6] = dot;
+    }
+    __syncthreads();
+    sq = dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < LANES / 64; ++i) {
+      sq += lds[0][i];
+      dot += lds[1][i];
+    }
+    const float inv = 1.0f / sqrtf(sq / (float)a.d + a.eps);
+    const float mean = dot * inv / (float)a.d;  // of a * n
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (u * LANES + lane) * 8;
+      if (c >= a.d) continue;
+      float w[8], dx[8], dres[8] = {};
+      load8(a.w, a.w_dtype, c, a.d - c, w);
+      if (a.dres) load8(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c, dres);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float n = s[u][j] * inv;
+        dx[j] = inv * (dy[u][j] * w[j] - n * mean) + dres[j];
+        dw[u][j] = fmaf(dy[u][j], n, dw[u][j]);
+      }
+      store8(a.dx, a.dx_dtype, row * a.ld_dx + c, a.d - c, dx);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int c = (u * LANES + lane) * 8;
+    store8(a.part, CEP_F32, (int64_t)blockIdx.x * a.d + c, a.d - c, dw[u]);
+  }
+}
+
+// dw: 32 columns a block, eight strands of the parts each, summed in a fixed
+// order.
+__global__ __launch_bounds__(256) void k_rms_norm_dw(const float *part, int n, int d, int w_dtype,
+                                                     void *dw) {
+  __shared__ float lds[8][32];
+  const int col = blockIdx.x * 32 + (threadIdx.x & 31), strand = threadIdx.x >> 5;
+  float v = 0.f;
+  if (col < d)
+    for (int i = strand; i < n; i += 8) v += part[(size_t)i * d + col];
+  lds[strand][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (strand == 0 && col < d) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += lds[i][threadIdx.x];
+    if (w_dtype == CEP_BF16) ((__bf16 *)dw)[col] = (__bf16)v;
+    else ((float *)dw)[col] = v;
+  }
+}
+
+// Calls f with the threads a row takes and the groups of eight channels each
+// of them holds: a wave up to 1024 channels (no barrier), else 256 threads, or
+// 1024 for the widest rows.
+template <class F>
+void by_width(int d, F f) {
+  using std::integral_constant;
+  if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  else if (d <= 16384) f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+  else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+
+int grad_blocks(int rows) { return std::min(rows, 1024); }
+
+// nullptr, or what is wrong with a descriptor
+const char *bad_desc(const cep_norm_desc *n) {
+  if (!n) return "desc is NULL";
+  if (n->rows < 0 || n->rows > kMaxOpRows) return "rows must be in 0..2^24";
+  if (n->d < 1 || n->d > kMaxDim) return "d must be in 1..32768";
+  if (!is_float_dtype(n->x_dtype) || !is_float_dtype(n->res_dtype) ||
+      !is_float_dtype(n->w_dtype) || !is_float_dtype(n->y_dtype))
+    return "dtypes must be CEP_F32 or CEP_BF16";
+  if (!(n->eps >= 0.f)) return "eps must be >= 0";
+  for (int64_t ld : {n->ld_x, n->ld_res, n->ld_y})
+    if (ld != 0 && ld < n->d) return "a row stride is shorter than a row";
+  return nullptr;
+}
+
+int64_t stride_of(int64_t ld, int64_t dense) { return ld ? ld : dense; }
+
+}  // namespace
+}  // namespace cep
+
+using namespace cep;
+
+CEP_API int cep_rms_norm(const cep_norm_desc *n, const void *x, const void *residual,
+                         const void *w, void *res_out, void *y, uint8_t *codes, uint8_t *scales,
+                         hipStream_t s) {
+  if (const char *why = bad_desc(n)) return refuse(CEP_EINVAL, "cep_rms_norm: %s", why);
+  if (!w || (!x && n->rows)) return refuse(CEP_EINVAL, "cep_rms_norm: NULL x or w");
+  if (!y && !codes) return refuse(CEP_EINVAL, "cep_rms_norm: neither y nor codes is asked for");
+  if ((codes != nullptr) != (scales != nullptr))
+    return refuse(CEP_EINVAL, "cep_rms_norm: codes and scales come together");
+  if (res_out && !residual) return refuse(CEP_EINVAL, "cep_rms_norm: res_out without residual");
+  const int64_t ld_codes = stride_of(n->ld_codes, n->d);
+  if (codes && (n->d % kMxBlock || ld_codes < n->d || ld_codes % 8 || !aligned(codes, 8) ||
+                (n->ld_scales && n->ld_scales < n->d / kMxBlock)))
+    return refuse(CEP_EINVAL, "cep_rms_norm: MXFP8 rows need d a multiple of 32, 8-byte aligned "
+                              "codes and row strides of at least a row");
+  if (!aligned(x, dtype_bytes(n->x_dtype)) || !aligned(residual, dtype_bytes(n->res_dtype)) ||
+      !aligned(res_out, dtype_bytes(n->res_dtype)) || !aligned(w, dtype_bytes(n->w_dtype)) ||
+      !aligned(y, dtype_bytes(n->y_dtype)))
+    return refuse(CEP_EINVAL, "cep_rms_norm: a pointer is not aligned to its type");
+  if (n->rows == 0) return CEP_OK;
+  const NormArgs a{x, residual, w, res_out, y, codes, scales, stride_of(n->ld_x, n->d),
+                   stride_of(n->ld_res, n->d), stride_of(n->ld_y, n->d), ld_codes,
+                   stride_of(n->ld_scales, n->d / kMxBlock), n->rows, n->d, n->x_dtype,
+                   n->res_dtype, n->w_dtype, n->y_dtype, n->eps};
+  by_width(n->d, [&](auto lanes, auto nv) {
+    constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
+    const int per = L < 256 ? 256 / L : 1;
+    hipLaunchKernelGGL((k_rms_norm<L, NV>), dim3((n->rows + per - 1) / per),
+                       dim3(L < 256 ? 256 : L), 0, s, a);
+  });
+  return launched("cep_rms_norm");
+}
+
+CEP_API size_t cep_rms_norm_workspace(const cep_norm_desc *n) {
+  if (bad_desc(n)) return 0;
+  return std::max<size_t>((size_t)grad_blocks(n->rows) * n->d * 4, 256);
+}
+
+CEP_API int cep_rms_norm_backward(const cep_norm_desc *n, const void *x, const void *w,
+                                  const void *dy, const void *dres, void *dx, void *dw,
+                                  void *workspace, size_t workspace_bytes, hipStream_t s) {
+  const char *fn = "cep_rms_norm_backward";
+  if (const char *why = bad_desc(n)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
+  if (!w || !dw || (n->rows && (!x || !dy || !dx)))
+    return refuse(CEP_EINVAL, "%s: NULL x, w, dy, dx or dw", fn);
+  if (!workspace || !aligned(workspace, 4) || workspace_bytes < cep_rms_norm_workspace(n))
+    return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
+                  cep_rms_norm_workspace(n));
+  if (!aligned(x, dtype_bytes(n->x_dtype)) || !aligned(dres, dtype_bytes(n->res_dtype)) ||
+      !aligned(dx, dtype_bytes(n->res_dtype)) || !aligned(w, dtype_bytes(n->w_dtype)) ||
+      !aligned(dw, dtype_bytes(n->w_dtype)) || !aligned(dy, dtype_bytes(n->y_dtype)))
+    return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  const int blocks = grad_blocks(n->rows);
+  const NormGradArgs a{x, w, dy, dres, dx, (float *)workspace, stride_of(n->ld_x, n->d),
+                       stride_of(n->ld_y, n->d), stride_of(n->ld_res, n->d), n->rows, n->d,
+                       n->x_dtype, n->res_dtype, n->w_dtype, n->y_dtype, n->eps};
+  if (blocks)
+    by_width(n->d, [&](auto lanes, auto nv) {
+      constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
+      hipLaunchKernelGGL((k_rms_norm_grad<L, NV>), dim3(blocks), dim3(L), 0, s, a);
+    });
+  hipLaunchKernelGGL(k_rms_norm_dw, dim3((n->d + 31) / 32), dim3(256), 0, s, a.part, blocks, n->d,
+                     n->w_dtype, dw);
+  return launched(fn);
+}

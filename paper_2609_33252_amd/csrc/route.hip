@@ -8,6 +8,7 @@
 // token.
 //
 // All of these are HBM-bound scans; none of them is a contraction.
+#include "cep.h"
 #include "common.h"
 
 #include <type_traits>
@@ -618,8 +619,9 @@ __global__ __launch_bounds__(256) void k_pack_rows(Arena a, Scratch sc, int row0
 // blockIdx.y naming the part of the row, and first loads all of them.  Bound
 // by HBM with many rows (NG 8), by latency with few (DIRECT, NG 2: more waves
 // a row, and the scale bytes go straight to the GEMM's layout, which saves
-// k_scale_layout).
-template <int NG, bool DIRECT>
+// k_scale_layout).  MX8: the rows are MXFP8 already (d codes, then d / 32
+// scales) and are copied.
+template <int NG, bool DIRECT, bool MX8>
 __global__ __launch_bounds__(256) void k_pack_tokens(Arena a, Scratch sc, int row0, int n_rows,
                                                      int k, int d) {
   const int lane = threadIdx.x & 63;
@@ -627,7 +629,7 @@ __global__ __launch_bounds__(256) void k_pack_tokens(Arena a, Scratch sc, int ro
   if (i >= n_rows) return;  // uniform over the wave
   static_assert(kMaxTopK <= 64, "a row's slots fit one wave");
   const int ps = lane < k ? sc.pos_of[(size_t)i * k + lane] : -1;
-  const uint4 *s4 = (const uint4 *)a.xrow[row0 + i];
+  const uint8_t *src = (const uint8_t *)a.xrow[row0 + i];
   const uint64_t valid = __ballot(ps >= 0);
   if (valid == 0) return;
   const int p0 = blockIdx.y * 512 * NG;
@@ -635,14 +637,21 @@ __global__ __launch_bounds__(256) void k_pack_tokens(Arena a, Scratch sc, int ro
 #pragma unroll
   for (int u = 0; u < NG; ++u) {
     const int c = p0 + u * 512 + lane * 8;
-    in[u] = c < d ? s4[c / 8] : make_uint4(0u, 0u, 0u, 0u);
+    in[u] = make_uint4(0u, 0u, 0u, 0u);
+    if (c >= d) continue;
+    if (MX8) {
+      const uint2 q = *(const uint2 *)(src + c);
+      in[u] = make_uint4(q.x, q.y, src[d + c / kMxBlock], 0u);
+    } else {
+      in[u] = *(const uint4 *)(src + 2 * c);
+    }
   }
 #pragma unroll
   for (int u = 0; u < NG; ++u) {
     if (p0 + u * 512 >= d) break;  // uniform over the wave
     const int c = p0 + u * 512 + lane * 8;
-    int code;
-    const uint2 q = quant_mx8(in[u], &code);
+    int code = (int)in[u].z;
+    const uint2 q = MX8 ? make_uint2(in[u].x, in[u].y) : quant_mx8(in[u], &code);
     if (c >= d) continue;
     for (uint64_t m = valid; m; m &= m - 1) {
       const int pos = __shfl(ps, __builtin_ctzll(m));
@@ -981,13 +990,16 @@ hipError_t launch_route(const Arena &a, const Scratch &sc, const IngestGroup *st
   const int n_pad = (int)std::min<long long>(bound, max_mpad);
   if (wk == kWMx || wk == kWFp8) {
     const dim3 rows((n_rows + 3) / 4);
+    const bool mx8 = x_dtype == CEP_MXFP8;
     if (expected_pairs <= kPackDirectPairs) {
-      hipLaunchKernelGGL((k_pack_tokens<2, true>), dim3(rows.x, (d + 1023) / 1024), dim3(256), 0,
-                         s, a, sc, row0, n_rows, k, d);
+      auto *pack = mx8 ? k_pack_tokens<2, true, true> : k_pack_tokens<2, true, false>;
+      hipLaunchKernelGGL(pack, dim3(rows.x, (d + 1023) / 1024), dim3(256), 0, s, a, sc, row0,
+                         n_rows, k, d);
       return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_pack_tokens<8, false>), dim3(rows.x, (d + 4095) / 4096), dim3(256), 0, s,
-                       a, sc, row0, n_rows, k, d);
+    auto *pack = mx8 ? k_pack_tokens<8, false, true> : k_pack_tokens<8, false, false>;
+    hipLaunchKernelGGL(pack, dim3(rows.x, (d + 4095) / 4096), dim3(256), 0, s, a, sc, row0, n_rows,
+                       k, d);
     const int nb = d / kMxBlock;
     hipLaunchKernelGGL(k_scale_layout, dim3((n_pad + 127) / 128, (nb + kScaleCols - 1) / kScaleCols),
                        dim3(256), 0, s, sc, nb);

@@ -169,9 +169,10 @@ bool valid_config(const cep_config *c, std::string *why) {
   if (c->max_replicas < 1 || c->max_tokens_per_replica < 1) return bad("max_replicas and max_tokens_per_replica must be >= 1");
   if ((long long)c->max_replicas * c->max_tokens_per_replica > (1LL << 24)) return bad("max_replicas * max_tokens_per_replica too large");
   if (c->w_dtype < CEP_F32 || c->w_dtype > CEP_MXFP4) return bad("bad w_dtype");
-  if (c->x_dtype != CEP_F32 && c->x_dtype != CEP_BF16) return bad("x_dtype must be CEP_F32 or CEP_BF16");
-  if (c->w_dtype == CEP_FP8_E4M3_B128 && c->x_dtype != CEP_BF16) return bad("fp8 weights need bf16 token rows");
-  if (c->w_dtype == CEP_MXFP4 && c->x_dtype != CEP_BF16) return bad("MXFP4 weights need bf16 token rows");
+  const bool quantised = c->w_dtype == CEP_FP8_E4M3_B128 || c->w_dtype == CEP_MXFP4;
+  if (c->x_dtype != CEP_F32 && c->x_dtype != CEP_BF16 && !(quantised && c->x_dtype == CEP_MXFP8))
+    return bad("x_dtype must be CEP_F32 or CEP_BF16, or CEP_MXFP8 with fp8 or MXFP4 weights");
+  if (quantised && c->x_dtype == CEP_F32) return bad("fp8 and MXFP4 weights need bf16 or MXFP8 token rows");
   if (c->n_streams < 1 || c->n_streams > 8) return bad("n_streams must be in 1..8");
   if (c->max_pairs_per_batch < 0) return bad("max_pairs_per_batch must be >= 0");
   return true;
@@ -233,7 +234,7 @@ int64_t stage_group(const cep_ctx *c, int64_t from, int64_t upto, IngestGroup *g
 }
 
 size_t x_row_bytes(const cep_config &cfg) {
-  return (size_t)cfg.d_model * (cfg.x_dtype == CEP_F32 ? 4 : 2);
+  return cep_row_bytes(cfg.d_model, cfg.x_dtype);
 }
 
 // Stages the metadata of chunks [c->staged, upto) into the arena on stream s
@@ -423,6 +424,14 @@ int launch_pending(cep_ctx *c) {
 }  // namespace
 
 // ================================================================== ABI
+
+CEP_API size_t cep_row_bytes(int d, int x_dtype) {
+  if (d < 1 || d > kMaxDim) return 0;
+  if (x_dtype == CEP_F32) return (size_t)d * 4;
+  if (x_dtype == CEP_BF16) return (size_t)d * 2;
+  if (x_dtype == CEP_MXFP8 && d % kMxBlock == 0) return align_up((size_t)d + d / kMxBlock, 16);
+  return 0;
+}
 
 CEP_API size_t cep_packed_expert_bytes(const cep_config *cfg) {
   std::string why;

@@ -1,0 +1,178 @@
+"""Operators around the routed experts without a GPU: refusals come before any
+HIP call, and the formulas the GPU tests compare with agree with differences."""
+import ctypes
+import os
+
+import pytest
+import torch
+
+from paper_2609_33252_amd import cep
+
+from . import _block_ref as R
+
+PTR = 1 << 20  # an aligned address that no refused call reads
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(cep.LIB_PATH):
+        from paper_2609_33252_amd import build
+        build.build()
+
+
+def _refused(status, fn, *a, **kw):
+    with pytest.raises(cep.CepError) as e:
+        fn(*a, **kw)
+    assert e.value.status == status
+    assert fn.__name__ in str(e.value)
+
+
+def test_row_bytes():
+    assert cep.cep_row_bytes(256, cep.CEP_F32) == 1024
+    assert cep.cep_row_bytes(256, cep.CEP_BF16) == 512
+    assert cep.cep_row_bytes(256, cep.CEP_MXFP8) == 272  # 256 + 8, padded to 16
+    assert cep.cep_row_bytes(4096, cep.CEP_MXFP8) == 4096 + 128
+    for d, t in ((0, cep.CEP_F32), (40, cep.CEP_MXFP8), (1 << 16, cep.CEP_F32), (256, cep.CEP_MXFP4)):
+        assert cep.cep_row_bytes(d, t) == 0
+
+
+def _norm(**kw):
+    return cep.make_norm(**{**dict(rows=4, d=64, x_dtype=cep.CEP_BF16, res_dtype=cep.CEP_BF16,
+                                   w_dtype=cep.CEP_F32, y_dtype=cep.CEP_BF16, eps=1e-6), **kw})
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(rows=(1 << 24) + 1), dict(d=0), dict(d=32769),
+                                 dict(x_dtype=cep.CEP_MXFP4), dict(y_dtype=7), dict(eps=-1.0),
+                                 dict(eps=float("nan")), dict(ld_x=63), dict(ld_y=-64)])
+def test_norm_refuses_descriptors(bad):
+    _refused(cep.CEP_EINVAL, cep.cep_rms_norm, _norm(**bad), PTR, PTR, y=PTR)
+    _refused(cep.CEP_EINVAL, cep.cep_rms_norm_backward, _norm(**bad), PTR, PTR, PTR, None, PTR,
+             PTR, None)
+    assert cep.cep_rms_norm_workspace(_norm(**bad)) == 0
+
+
+def test_norm_refuses_arguments():
+    f = cep.cep_rms_norm
+    for a, kw in (((None, PTR), dict(y=PTR)), ((PTR, None), dict(y=PTR)), ((PTR, PTR), {}),
+                  ((PTR, PTR), dict(codes=PTR)), ((PTR, PTR), dict(y=PTR, res_out=PTR)),
+                  ((PTR, PTR), dict(codes=PTR + 4, scales=PTR)), ((PTR + 1, PTR), dict(y=PTR)),
+                  ((PTR, PTR + 2), dict(y=PTR))):
+        _refused(cep.CEP_EINVAL, f, _norm(), *a, **kw)
+    for bad in (dict(d=40), dict(ld_codes=60), dict(ld_scales=1)):
+        _refused(cep.CEP_EINVAL, f, _norm(**bad), PTR, PTR, codes=PTR, scales=PTR)
+    _refused(cep.CEP_EINVAL, f, None, PTR, PTR, y=PTR)
+    f(_norm(rows=0), None, PTR, y=PTR)  # nothing to do, nothing launched
+    small = torch.empty(16, dtype=torch.uint8)
+    _refused(cep.CEP_ENOMEM, cep.cep_rms_norm_backward, _norm(), PTR, PTR, PTR, None, PTR, PTR,
+             small)
+    _refused(cep.CEP_EINVAL, cep.cep_rms_norm_backward, _norm(), PTR, PTR, PTR, None, PTR, PTR,
+             None)
+
+
+def _gate(**kw):
+    return cep.make_gate(**{**dict(rows=4, n_experts=64, top_k=8, normalize=1, scale=1.0), **kw})
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(n_experts=0), dict(n_experts=1025),
+                                 dict(top_k=0), dict(top_k=17), dict(top_k=5, n_experts=4),
+                                 dict(logit_dtype=2), dict(score=2), dict(ld=63),
+                                 dict(scale=float("nan")), dict(score=1, n_groups=3, topk_groups=1),
+                                 dict(score=1, n_groups=8, topk_groups=9),
+                                 dict(score=1, n_groups=8), dict(n_groups=8, topk_groups=4),
+                                 dict(score=1, n_groups=128, n_experts=128, topk_groups=1)])
+def test_gate_refuses_descriptors(bad):
+    _refused(cep.CEP_EINVAL, cep.cep_gate_topk, _gate(**bad), PTR, None, PTR, PTR)
+
+
+def test_gate_refuses_arguments():
+    for a in ((None, None, PTR, PTR), (PTR, None, None, PTR), (PTR, None, PTR, None),
+              (PTR, PTR, PTR, PTR), (PTR + 2, None, PTR, PTR), (PTR, None, PTR + 2, PTR)):
+        _refused(cep.CEP_EINVAL, cep.cep_gate_topk, _gate(), *a)
+    cep.cep_gate_topk(_gate(rows=0), None, None, None, None)
+
+
+def _send(**kw):
+    return cep.make_dispatch(**{**dict(rows=4, top_k=2, n_ranks=8, experts_per_rank=4, capacity=8,
+                                       row_bytes=64), **kw})
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(top_k=0), dict(top_k=17), dict(n_ranks=0),
+                                 dict(n_ranks=65), dict(experts_per_rank=0), dict(row_bytes=0),
+                                 dict(row_bytes=131073), dict(ld_x=63), dict(capacity=-1),
+                                 dict(rows=1 << 24, top_k=16, n_ranks=64 * 3)])
+def test_dispatch_refuses_descriptors(bad):
+    _refused(cep.CEP_EINVAL, cep.cep_dispatch, _send(**bad), *[PTR] * 8, None)
+    assert cep.cep_dispatch_workspace(_send(**bad)) == 0
+
+
+def test_dispatch_refuses_arguments():
+    big = torch.empty(1 << 16, dtype=torch.uint8)
+    _refused(cep.CEP_ENOMEM, cep.cep_dispatch, _send(capacity=7), *[PTR] * 8, big)
+    for i in range(8):
+        _refused(cep.CEP_EINVAL, cep.cep_dispatch, _send(), *[None if j == i else PTR
+                                                              for j in range(8)], big)
+    _refused(cep.CEP_ENOMEM, cep.cep_dispatch, _send(), *[PTR] * 8, big[:16])
+    _refused(cep.CEP_EINVAL, cep.cep_dispatch, _send(), *[PTR] * 8, None)
+
+
+def _ffn(**kw):
+    return cep.make_gated_ffn(**{**dict(rows=4, d_model=64, d_ff=32), **kw})
+
+
+@pytest.mark.parametrize("bad", [dict(rows=-1), dict(d_model=0), dict(d_model=12),
+                                 dict(d_model=32776), dict(d_ff=4), dict(d_ff=-8), dict(ld_x=56),
+                                 dict(ld_y=68), dict(ld_dx=8)])
+def test_ffn_refuses_descriptors(bad):
+    _refused(cep.CEP_EINVAL, cep.cep_gated_ffn, _ffn(**bad), *[PTR] * 5, None)
+    _refused(cep.CEP_EINVAL, cep.cep_gated_ffn_backward, _ffn(**bad), *[PTR] * 10, None)
+    assert cep.cep_gated_ffn_workspace(_ffn(**bad)) == 0
+
+
+def test_ffn_refuses_arguments():
+    big = torch.empty(1 << 22, dtype=torch.uint8)
+    assert big.data_ptr() % 16 == 0
+    for i in range(5):
+        for wrong in (None, PTR + 8):
+            a = [wrong if j == i else PTR for j in range(5)]
+            _refused(cep.CEP_EINVAL, cep.cep_gated_ffn, _ffn(), *a, big)
+    for i in range(10):
+        a = [None if j == i else PTR for j in range(10)]
+        _refused(cep.CEP_EINVAL, cep.cep_gated_ffn_backward, _ffn(), *a, big)
+    _refused(cep.CEP_ENOMEM, cep.cep_gated_ffn, _ffn(), *[PTR] * 5, big[:64])
+    _refused(cep.CEP_ENOMEM, cep.cep_gated_ffn_backward, _ffn(), *[PTR] * 10, big[:64])
+    cep.cep_gated_ffn(_ffn(rows=0), *[None] * 5, None)
+
+
+def test_descriptors_match_the_header():
+    # the sizes a C compiler gives the header's structs
+    assert ctypes.sizeof(cep.cep_norm_desc) == 72
+    assert ctypes.sizeof(cep.cep_gate_desc) == 48
+    assert ctypes.sizeof(cep.cep_dispatch_desc) == 40
+    assert ctypes.sizeof(cep.cep_gated_ffn_desc) == 40
+
+
+def _slope(f, x, v, h=1e-5):
+    return float((f(x + h * v) - f(x - h * v)) / (2 * h))
+
+
+def test_norm_gradient_formula_agrees_with_differences():
+    g = torch.Generator().manual_seed(0)
+    s, w, dy, v = (torch.randn(3, 17, generator=g, dtype=torch.float64) for _ in range(4))
+    w = w[0]
+    dx, dw = R.rms_norm_grad(s, w, dy, None, 1e-3)
+    f = lambda s_, w_: (R.rms_norm(s_, None, w_, 1e-3)[1] * dy).sum()
+    # central differences: O(h^2) = 1e-10 of third derivatives of order 1
+    assert abs(_slope(lambda z: f(z, w), s, v) - float((dx * v).sum())) < 1e-7
+    assert abs(_slope(lambda z: f(s, z), w, v[0]) - float((dw * v[0]).sum())) < 1e-7
+
+
+def test_ffn_gradient_formula_agrees_with_differences():
+    g = torch.Generator().manual_seed(1)
+    r = lambda *n: torch.randn(*n, generator=g, dtype=torch.float64)
+    a = dict(x=r(5, 8), wg=r(8, 16) * 0.3, wu=r(8, 16) * 0.3, wd=r(16, 8) * 0.3)
+    dy = r(5, 8)
+    grads = R.gated_ffn_grad(dy, **a)
+    for name, key in (("x", "dx"), ("wg", "dwg"), ("wu", "dwu"), ("wd", "dwd")):
+        v = r(*a[name].shape)
+        f = lambda z: (R.gated_ffn(**{**a, name: z})[3] * dy).sum()
+        assert abs(_slope(f, a[name], v) - float((grads[key] * v).sum())) < 1e-6, name

@@ -1,0 +1,544 @@
+"""Operators around the routed experts on the GPU against float64 forms.
+
+Tolerances, from the formats: u16 = 2^-8 is half a unit in the last place of
+bf16, u32 = 2^-24 of float32.  A float32 sum of n terms in any order is within
+n u32 of the sum of the magnitudes; the ones here run over at most a few
+hundred sequential terms a lane, so 2^-15 of the magnitudes is ample.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx
+from paper_2609_33252_amd import cep
+
+from . import _block_ref as R
+
+pytestmark = pytest.mark.gpu
+
+U16, SUM32 = 2.0 ** -8, 2.0 ** -15
+F32, BF16 = cep.CEP_F32, cep.CEP_BF16
+DT = {F32: torch.float32, BF16: torch.bfloat16}
+EPS = 1e-6
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    cep.lib()
+    torch.cuda.set_device(0)
+
+
+def _randn(g, *shape, dtype=torch.bfloat16, std=1.0):
+    return torch.randn(*shape, device="cuda", generator=g).mul_(std).to(dtype)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _close(got, ref, tol, what):
+    err = (got.double() - ref).abs()
+    bad = ~(err <= tol)
+    assert not bad.any(), (what, float(err.max()), int(bad.sum()), bad.nonzero()[:4].tolist())
+
+
+def _padded(t, ld, fill=float("nan")):
+    """t's rows in a buffer of row stride ld; the padding is NaN."""
+    buf = torch.full((t.shape[0], ld), fill, dtype=t.dtype, device=t.device)
+    buf[:, :t.shape[1]] = t
+    return buf
+
+
+def _float_tol(ref, mag, dtype):
+    return (U16 * 1.01 * ref.abs() if dtype == BF16 else 0) + SUM32 * mag + 1e-37
+
+
+# -------------------------------------------------------------------- norm
+
+@pytest.mark.parametrize("rows,d,x,res,y,q,pad", [
+    (1, 7168, BF16, BF16, BF16, True, 0),
+    (5, 32, F32, None, F32, True, 0),
+    (3, 1, F32, F32, F32, False, 0),
+    (7, 77, BF16, BF16, BF16, False, 0),       # odd width: rows at any alignment
+    (9, 513, BF16, F32, F32, False, 3),
+    (4, 1000, F32, BF16, BF16, False, 8),
+    (6, 1056, BF16, None, None, True, 16),
+    (33, 2304, F32, BF16, BF16, True, 0),
+    (2, 4096, BF16, BF16, F32, True, 1),
+    (3, 8191, BF16, BF16, BF16, False, 1),
+    (2, 16384, F32, F32, None, True, 0),
+    (2, 32768, BF16, BF16, BF16, True, 0),
+    (301, 256, BF16, BF16, BF16, True, 0),
+])
+def test_norm(rows, d, x, res, y, q, pad):
+    g = _gen(rows * 31 + d)
+    xt, wt = _randn(g, rows, d, dtype=DT[x]), 1 + 0.1 * _randn(g, d, dtype=torch.float32)
+    rt = None if res is None else _randn(g, rows, d, dtype=DT[res], std=3)
+    ld = d + pad
+    desc = cep.make_norm(rows=rows, d=d, x_dtype=x, res_dtype=BF16 if res is None else res,
+                         w_dtype=F32, y_dtype=BF16 if y is None else y, eps=EPS,
+                         ld_x=ld if pad else 0, ld_res=ld if pad else 0, ld_y=ld if pad else 0)
+    xb, rb = _padded(xt, ld), None if rt is None else _padded(rt, ld)
+    rob = None if rt is None else torch.full_like(rb, 7.0)
+    yb = None if y is None else torch.full((rows, ld), 7.0, dtype=DT[y], device="cuda")
+    codes = torch.full((rows, d), 7, dtype=torch.uint8, device="cuda") if q else None
+    scales = torch.full((rows, d // 32), 7, dtype=torch.uint8, device="cuda") if q else None
+    cep.cep_rms_norm(desc, xb, wt, residual=rb, res_out=rob, y=yb, codes=codes, scales=scales)
+    s, ref = R.rms_norm(xt, rt, wt, EPS)
+    if rt is not None:
+        _close(rob[:, :d], s, _float_tol(s, s.abs(), res), "residual")
+        assert (rob[:, d:] == 7.0).all()
+    if y is not None:
+        _close(yb[:, :d], ref, _float_tol(ref, ref.abs(), y), "y")
+        assert (yb[:, d:] == 7.0).all()
+    if q:
+        amax = ref.view(rows, -1, 32).abs().amax(-1)
+        e = torch.floor(torch.log2(amax)) - 8 + 127
+        near = (torch.floor(torch.log2(amax * (1 + SUM32))) !=
+                torch.floor(torch.log2(amax * (1 - SUM32))))  # either scale is right
+        assert (near | (scales.double() == e)).all()
+        assert ((scales.double() - e).abs() <= 1).all()
+        scale = torch.exp2(scales.double() - 127).repeat_interleave(32, 1)
+        val = codes.view(torch.float8_e4m3fn).double() * scale
+        # half a step: 2^-4 of a normal value, 2^-10 scales of a small one; past
+        # 448 scales (of up to 512) the code saturates
+        tol = torch.maximum(2.0 ** -4 * ref.abs(), 2.0 ** -10 * scale) + SUM32 * ref.abs()
+        tol = torch.maximum(tol, ref.abs() - 448 * scale * (1 - SUM32))
+        _close(val, ref, tol, "MXFP8")
+
+
+def test_norm_matches_the_mxfp8_oracle_and_makes_chunk_rows():
+    # bf16 rows of unit weight and unit mean square times a power of two: y is
+    # a bf16 row again only up to rounding, so the oracle gets y in float32
+    g = _gen(5)
+    rows, d = 37, 512
+    x, w = _randn(g, rows, d), torch.ones(d, device="cuda")
+    stride = cep.cep_row_bytes(d, cep.CEP_MXFP8)
+    buf = torch.zeros(rows, stride, dtype=torch.uint8, device="cuda")
+    y = torch.empty(rows, d, dtype=torch.float32, device="cuda")
+    desc = cep.make_norm(rows=rows, d=d, x_dtype=BF16, res_dtype=BF16, w_dtype=F32, y_dtype=F32,
+                         eps=EPS, ld_codes=stride, ld_scales=stride)
+    cep.cep_rms_norm(desc, x, w, y=y, codes=buf, scales=buf.data_ptr() + d)
+    codes, scode = mx.quantize_mxfp8(y.cpu().numpy())
+    got = buf.cpu().numpy()
+    assert np.array_equal(got[:, d:d + d // 32], scode.reshape(rows, -1))
+    assert np.array_equal(got[:, :d], codes.reshape(rows, d))
+    assert not got[:, d + d // 32:].any()
+
+
+def test_norm_of_unusual_rows():
+    d = 96
+    x = torch.zeros(6, d, device="cuda")
+    x[1] = 1e30                  # the squares overflow: y = 0
+    x[2, 5] = float("inf")
+    x[3, 40] = float("nan")
+    x[4] = 1e-30                 # below eps: y ~ x / sqrt(eps)
+    x[5] = -2.0
+    w = torch.ones(d, device="cuda")
+    y = torch.empty_like(x)
+    codes = torch.empty(6, d, dtype=torch.uint8, device="cuda")
+    scales = torch.empty(6, 3, dtype=torch.uint8, device="cuda")
+    desc = cep.make_norm(rows=6, d=d, eps=EPS)
+    cep.cep_rms_norm(desc, x, w, y=y, codes=codes, scales=scales)
+    assert (y[0] == 0).all() and (codes[0] == 0).all() and (scales[0] == 0).all()
+    assert (y[1] == 0).all() and (scales[1] == 0).all()
+    assert torch.isnan(y[2, 5]) and (y[2, 6:] == 0).all() and scales[2].tolist() == [255, 0, 0]
+    assert torch.isnan(y[3]).all() and (scales[3] == 255).all()
+    _close(y[4], torch.full((d,), 1e-30 / EPS ** 0.5, dtype=torch.float64, device="cuda"),
+           1e-27 * SUM32, "tiny")
+    _close(y[5], torch.full((d,), -1.0, dtype=torch.float64, device="cuda"), 1e-5, "constant")
+
+
+def test_norm_in_place_and_on_another_stream():
+    g = _gen(9)
+    rows, d = 65, 1024
+    x, r, w = _randn(g, rows, d), _randn(g, rows, d), torch.ones(d, device="cuda")
+    desc = cep.make_norm(rows=rows, d=d, x_dtype=BF16, res_dtype=BF16, w_dtype=F32, y_dtype=BF16,
+                         eps=EPS)
+    ro, y = torch.empty_like(r), torch.empty_like(x)
+    cep.cep_rms_norm(desc, x, w, residual=r, res_out=ro, y=y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    cep.cep_rms_norm(desc, x, w, residual=r, res_out=r, y=x, stream=side)
+    side.synchronize()
+    assert torch.equal(r, ro) and torch.equal(x, y)
+
+
+@pytest.mark.parametrize("rows,d,s,dres,dy,wdt,pad", [
+    (1, 64, F32, True, F32, F32, 0), (0, 64, F32, False, F32, F32, 0),
+    (3, 1, F32, False, F32, F32, 0), (17, 77, BF16, True, BF16, BF16, 0),
+    (5, 1000, F32, False, BF16, F32, 5), (1300, 513, BF16, True, F32, F32, 0),
+    (2, 4096, BF16, False, BF16, F32, 0), (1025, 7168, BF16, True, BF16, F32, 8),
+    (3, 32768, F32, True, F32, F32, 0), (9, 16384, BF16, False, BF16, F32, 0),
+])
+def test_norm_backward(rows, d, s, dres, dy, wdt, pad):
+    g = _gen(rows + d)
+    ld = d + pad
+    st, dyt = _randn(g, rows, d, dtype=DT[s]), _randn(g, rows, d, dtype=DT[dy])
+    dr = _randn(g, rows, d, dtype=DT[s]) if dres else None
+    w = (1 + 0.1 * _randn(g, d, dtype=torch.float32)).to(DT[wdt])
+    desc = cep.make_norm(rows=rows, d=d, x_dtype=s, res_dtype=s, w_dtype=wdt, y_dtype=dy, eps=EPS,
+                         ld_x=ld, ld_res=ld, ld_y=ld)
+    ws = torch.empty(cep.cep_rms_norm_workspace(desc), dtype=torch.uint8, device="cuda")
+    dx = torch.full((rows, ld), 7.0, dtype=DT[s], device="cuda")
+    dw = torch.full((d,), 7.0, dtype=DT[wdt], device="cuda")
+    cep.cep_rms_norm_backward(desc, _padded(st, ld), w, _padded(dyt, ld),
+                              None if dr is None else _padded(dr, ld), dx, dw, ws)
+    rx, rw = R.rms_norm_grad(st, w, dyt, dr, EPS)
+    inv = 1 / torch.sqrt((st.double() ** 2).mean(-1, keepdim=True) + EPS)
+    a = (dyt.double() * w.double()).abs()
+    n = (st.double() * inv).abs()
+    mag = inv * (a + n * (a * n).mean(-1, keepdim=True)) + (0 if dr is None else dr.double().abs())
+    _close(dx[:, :d], rx, _float_tol(rx, mag, s), "dx")
+    assert (dx[:, d:] == 7.0).all()
+    _close(dw, rw, _float_tol(rw, (dyt.double().abs() * n).sum(0), wdt), "dw")
+    first = dw.clone()
+    cep.cep_rms_norm_backward(desc, _padded(st, ld), w, _padded(dyt, ld),
+                              None if dr is None else _padded(dr, ld), dx, dw, ws)
+    assert torch.equal(first, dw)
+
+
+def test_norm_backward_agrees_with_differences_of_the_forward_pass():
+    g = _gen(77)
+    rows, d, h = 6, 320, 2.0 ** -7
+    x, c, v = (_randn(g, rows, d, dtype=torch.float32) for _ in range(3))
+    w = 1 + 0.1 * _randn(g, d, dtype=torch.float32)
+    desc = cep.make_norm(rows=rows, d=d, eps=EPS)
+    y, out = torch.empty_like(x), []
+    for z in (x + h * v, x - h * v):
+        cep.cep_rms_norm(desc, z, w, y=y)
+        out.append(float((y.double() * c.double()).sum()))
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws = torch.empty(cep.cep_rms_norm_workspace(desc), dtype=torch.uint8, device="cuda")
+    cep.cep_rms_norm_backward(desc, x, w, c, None, dx, dw, ws)
+    slope = (out[0] - out[1]) / (2 * h)
+    # h^2 times third derivatives of order |c| |v|, and y's float32 rounding
+    # over 2 h: both far below 1e-2 of sqrt(rows d)
+    assert abs(slope - float((dx.double() * v.double()).sum())) < 1e-2 * (rows * d) ** 0.5
+
+
+# -------------------------------------------------------------------- gate
+
+def _run_gate(logits, k, bias=None, ld=0, **kw):
+    T = logits.shape[0]
+    ids = torch.full((T, k), 77, dtype=torch.int32, device="cuda")
+    w = torch.full((T, k), 77.0, device="cuda")
+    desc = cep.make_gate(rows=T, top_k=k, ld=ld, **kw)
+    cep.cep_gate_topk(desc, logits, bias, ids, w)
+    return ids.cpu().numpy(), w.cpu().numpy()
+
+
+def _gate_check(logits, k, score="softmax", bias=None, groups=1, topg=1, normalize=True, scale=1.0):
+    ids, w = _run_gate(logits, k, bias, n_experts=logits.shape[1],
+                       logit_dtype=BF16 if logits.dtype == torch.bfloat16 else F32,
+                       score=cep.CEP_SOFTMAX if score == "softmax" else cep.CEP_SIGMOID,
+                       n_groups=groups, topk_groups=topg, normalize=int(normalize), scale=scale)
+    rid, rw = R.gate(logits.float().cpu().numpy(), k, score,
+                     None if bias is None else bias.cpu().numpy(), groups, topg, normalize, scale)
+    assert np.array_equal(ids, rid)
+    # exp of a float32 difference of up to 100: 100 u32 of the value
+    assert np.all(np.abs(w - rw) <= 2.0 ** -16 * np.abs(rw) + 1e-30)
+
+
+@pytest.mark.parametrize("E", [1, 3, 8, 63, 64, 65, 128, 160, 161, 256, 257, 512, 1000, 1024])
+@pytest.mark.parametrize("k", [1, 2, 8, 16])
+def test_gate_softmax(E, k):
+    if k > E:
+        return
+    g = _gen(E * 100 + k)
+    for T in (1, 33):
+        _gate_check(_randn(g, T, E, dtype=torch.float32), k)
+    _gate_check(_randn(g, 5, E, dtype=torch.float32, std=20), k, normalize=False, scale=2.5)
+
+
+def _spaced(g, T, E, groups=1):
+    """Logits whose sigmoids differ by 0.5 / E at least, and the sums of a
+    group's two best by 1e-5 from the next group's."""
+    p = torch.rand(8 * T, E, device="cuda", generator=g).argsort(-1).double()
+    p = p + 0.4 * torch.rand(8 * T, E, device="cuda", generator=g).double()
+    p = 0.05 + 0.9 * p / E
+    if groups > 1:
+        total = p.view(8 * T, groups, -1).topk(min(2, E // groups), -1)[0].sum(-1)
+        p = p[total.sort(-1)[0].diff(dim=-1).amin(-1) > 1e-5]
+    assert len(p) >= T
+    return torch.log(p[:T] / (1 - p[:T])).float()
+
+
+@pytest.mark.parametrize("E,groups,topg,k", [(64, 1, 1, 6), (160, 8, 3, 6), (256, 8, 4, 8),
+                                             (256, 1, 1, 16), (512, 64, 7, 8), (96, 3, 3, 4),
+                                             (12, 12, 5, 5), (1024, 4, 1, 8)])
+def test_gate_sigmoid_groups(E, groups, topg, k):
+    g = _gen(E + groups)
+    logits = _spaced(g, 19, E, groups)
+    _gate_check(logits, k, "sigmoid", None, groups, topg)
+    bias = (0.9 / E) * 0.05 * torch.randint(-3, 4, (E,), device="cuda", generator=g).float()
+    ids = R.gate(logits.cpu().numpy(), k, "sigmoid", bias.cpu().numpy(), groups, topg)[0]
+    ids32, _ = _run_gate(logits, k, bias, n_experts=E, score=cep.CEP_SIGMOID, n_groups=groups,
+                         topk_groups=topg, normalize=1, scale=1.0)
+    if groups == 1:  # sums of two keys may tie to the last bit
+        assert np.array_equal(ids, ids32)
+    _gate_check(logits, k, "sigmoid", None, groups, topg, normalize=False, scale=0.5)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gate_ties_and_masks(dtype):
+    g = _gen(3)
+    E = 100
+    l = torch.randint(0, 3, (40, E), device="cuda", generator=g).to(dtype)
+    l[1] = 0.0
+    l[2] = -float("inf")                    # nothing is left
+    l[3, 5:] = -float("inf")                # fewer than k are left
+    l[4, ::2] = float("nan")
+    l[5, 7] = float("inf")
+    l[6] = torch.finfo(dtype).min           # the lowest number is no mask
+    l[7, :50] = -0.0
+    l[7, 50:] = 0.0                          # equal to -0: the lower expert
+    l[8] = float("nan")
+    _gate_check(l, 8)
+    _gate_check(l, 8, "sigmoid")
+    _gate_check(l, 16, normalize=False)
+    _gate_check(l[:9], 4, "sigmoid", None, 10, 2)
+
+
+def test_gate_strided_rows_and_unaligned_start():
+    g = _gen(4)
+    buf = torch.full((9, 300), 100.0, device="cuda")
+    buf[:, 3:3 + 129] = _randn(g, 9, 129, dtype=torch.float32)
+    desc_kw = dict(n_experts=129, normalize=1, scale=1.0)
+    ids, w = _run_gate(buf[:, 3:], 8, ld=300, **desc_kw)
+    rid, rw = R.gate(buf[:, 3:132].cpu().numpy(), 8)
+    assert np.array_equal(ids, rid) and np.allclose(w, rw, rtol=2.0 ** -16, atol=0)
+
+
+# ---------------------------------------------------------------- dispatch
+
+@pytest.mark.parametrize("T,k,ranks,per,row,pad", [
+    (0, 2, 4, 4, 64, 0), (1, 1, 1, 1, 1, 0), (1, 8, 8, 32, 14336, 0), (13, 8, 8, 32, 4224, 16),
+    (16, 16, 64, 3, 17, 1), (255, 4, 5, 12, 33, 0), (256, 6, 10, 16, 272, 0),
+    (257, 8, 10, 16, 1000, 24), (1000, 2, 64, 1, 16, 0), (3001, 8, 8, 8, 48, 0),
+    (5000, 1, 3, 7, 2, 3), (300, 8, 2, 20, 131072, 0),
+])
+def test_dispatch(T, k, ranks, per, row, pad):
+    g = np.random.default_rng(T * 7 + row)
+    ids = g.integers(0, ranks * per, (T, k)).astype(np.int32)  # repeats among them
+    ids[g.random((T, k)) < 0.2] = -1
+    if T > 8:
+        ids[4] = -1                       # a token that goes nowhere
+        ids[5, 0], ids[6, 0], ids[7, 0] = ranks * per, -2, 2 ** 31 - 1
+    w = g.random((T, k), np.float32)
+    x = g.integers(0, 256, (T, row + pad)).astype(np.uint8)
+    cap = T * min(k, ranks) + 3
+    desc = cep.make_dispatch(rows=T, top_k=k, n_ranks=ranks, experts_per_rank=per, capacity=cap,
+                             row_bytes=row, ld_x=row + pad)
+    dev = lambda a: torch.from_numpy(a).cuda()
+    plan = torch.full((2 * ranks + 2,), 9, dtype=torch.int32, device="cuda")
+    token = torch.full((cap,), -5, dtype=torch.int32, device="cuda")
+    oid = torch.full((cap, k), -5, dtype=torch.int32, device="cuda")
+    ow = torch.full((cap, k), -5.0, device="cuda")
+    ox = torch.full((cap, row), 5, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(cep.cep_dispatch_workspace(desc), dtype=torch.uint8, device="cuda")
+    cep.cep_dispatch(desc, dev(ids), dev(w), dev(x), plan, token, oid, ow, ox, ws)
+    rows, ref = R.dispatch(ids, w, ranks, per)
+    assert np.array_equal(plan.cpu().numpy(), ref)
+    n = len(rows)
+    token, oid, ow, ox = (t.cpu().numpy() for t in (token, oid, ow, ox))
+    if n:
+        t = np.array([r[0] for r in rows])
+        assert np.array_equal(token[:n], t)
+        assert np.array_equal(oid[:n], np.stack([r[1] for r in rows]))
+        assert np.array_equal(ow[:n], np.stack([r[2] for r in rows]).astype(np.float32))
+        assert np.array_equal(ox[:n], x[t, :row])
+    assert (token[n:] == -5).all() and (oid[n:] == -5).all() and (ow[n:] == -5).all()
+    assert (ox[n:] == 5).all()
+
+
+# --------------------------------------------------------------- gated FFN
+
+def _ffn_inputs(T, d, I, seed):
+    g = _gen(seed)
+    return (_randn(g, T, d), _randn(g, d, I, std=d ** -0.5), _randn(g, d, I, std=d ** -0.5),
+            _randn(g, I, d, std=I ** -0.5), _randn(g, T, d))
+
+
+SHAPES = [(1, 8, 8), (1, 256, 128), (2, 264, 136), (16, 512, 2048), (17, 1000, 504),
+          (64, 2304, 1408), (65, 256, 128), (129, 520, 72), (256, 1024, 256), (300, 264, 1032),
+          (513, 512, 384), (1500, 776, 520), (5, 4096, 16), (33, 16, 4096), (700, 2048, 1024)]
+
+
+def _ffn_tols(x, wg, wu, wd):
+    """Bounds of the error of h and y: the float32 sums of g and u carried
+    through h, h rounded to bf16, the sum over h, y rounded to bf16."""
+    g, u, h, y = R.gated_ffn(x, wg, wu, wd)
+    ax = x.double().abs()
+    eg, eu = SUM32 * (ax @ wg.double().abs()), SUM32 * (ax @ wu.double().abs())
+    s = torch.sigmoid(g)
+    eh = eg * 1.1 * u.abs() + eu * (g * s).abs() + 1.01 * U16 * h.abs()
+    ey = (eh + SUM32 * h.abs()) @ wd.double().abs() + 1.01 * U16 * y.abs()
+    return g, u, h, y, eg, eu, eh, ey + 1e-30
+
+
+@pytest.mark.parametrize("T,d,I", SHAPES)
+@pytest.mark.parametrize("pad", [0, 8])
+def test_ffn_forward(T, d, I, pad):
+    x, wg, wu, wd, _ = _ffn_inputs(T, d, I, T + d + I)
+    desc = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I, ld_x=d + pad, ld_y=d + 2 * pad)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc), dtype=torch.uint8, device="cuda")
+    ws.fill_(255)  # NaN, were any of it read before it is written
+    g, u, _, ref, eg, eu, _, ey = _ffn_tols(x, wg, wu, wd)
+    out = []
+    for keep in (False, True):
+        pre = torch.full((T, 2, I), float("nan"), device="cuda") if keep else None
+        y = torch.full((T, d + 2 * pad), 7.0, dtype=torch.bfloat16, device="cuda")
+        cep.cep_gated_ffn(desc, _padded(x, d + pad), wg, wu, wd, y, ws, preact=pre)
+        _close(y[:, :d], ref, ey, "y")
+        assert (y[:, d:] == 7.0).all()
+        out.append(y)
+    assert torch.equal(out[0], out[1])
+    _close(pre[:, 0], g, eg + 1e-30, "g")
+    _close(pre[:, 1], u, eu + 1e-30, "u")
+
+
+@pytest.mark.parametrize("T,d,I", SHAPES)
+@pytest.mark.parametrize("pad", [0, 8])
+def test_ffn_backward(T, d, I, pad):
+    x, wg, wu, wd, dy = _ffn_inputs(T, d, I, T + d + I + 1)
+    desc = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I, ld_x=d + pad, ld_y=d + pad,
+                              ld_dx=d + 2 * pad)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc, True), dtype=torch.uint8, device="cuda")
+    ws.fill_(255)
+    ref = R.gated_ffn_grad(dy, x, wg, wu, wd)
+    g, u, h, _, _, _, _, _ = _ffn_tols(x, wg, wu, wd)
+    pre = torch.stack([g, u], 1).float().contiguous()  # the forward pass's, rounded once
+    dx = torch.full((T, d + 2 * pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    dwg, dwu, dwd = (torch.full_like(t, 7.0) for t in (wg, wu, wd))
+    xb, dyb = _padded(x, d + pad), _padded(dy, d + pad)
+    cep.cep_gated_ffn_backward(desc, dyb, xb, wg, wu, wd, pre, dx, dwg, dwu, dwd, ws)
+    # errors of dh, then of dg, du and h rounded to bf16 (1.1 bounds silu')
+    ax, ady = x.double().abs(), dy.double().abs()
+    s = torch.sigmoid(g)
+    edh = SUM32 * (ady @ wd.double().abs().T.contiguous())
+    edg = 1.1 * (edh * u.abs()) + 1.02 * U16 * ref["dg"].abs() + SUM32 * (ref["dh"] * u).abs()
+    edu = edh * (g * s).abs() + 1.02 * U16 * ref["du"].abs()
+    eh = 1.02 * U16 * h.abs()
+    T_ = lambda t: t.T.contiguous()
+    for got, name, e in (
+            (dx[:, :d], "dx", (edg + SUM32 * ref["dg"].abs()) @ T_(wg.double().abs())
+             + (edu + SUM32 * ref["du"].abs()) @ T_(wu.double().abs())),
+            (dwg, "dwg", T_(ax) @ (edg + SUM32 * ref["dg"].abs())),
+            (dwu, "dwu", T_(ax) @ (edu + SUM32 * ref["du"].abs())),
+            (dwd, "dwd", T_(eh + SUM32 * h.abs()) @ ady)):
+        _close(got, ref[name], e + 1.01 * U16 * ref[name].abs() + 1e-30, name)
+    assert (dx[:, d:] == 7.0).all()
+    again = [torch.full_like(t, 3.0) for t in (dx, dwg, dwu, dwd)]
+    cep.cep_gated_ffn_backward(desc, dyb, xb, wg, wu, wd, pre, *again, ws)
+    for a, b in zip((dx[:, :d], dwg, dwu, dwd), (again[0][:, :d], *again[1:])):
+        assert torch.equal(a, b)
+
+
+def test_ffn_of_no_rows_has_zero_weight_gradients():
+    _, wg, wu, wd, _ = _ffn_inputs(1, 64, 32, 0)
+    desc = cep.make_gated_ffn(rows=0, d_model=64, d_ff=32)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc, True), dtype=torch.uint8, device="cuda")
+    out = [torch.full_like(t, 7.0) for t in (wg, wu, wd)]
+    cep.cep_gated_ffn_backward(desc, None, None, wg, wu, wd, None, None, *out, ws)
+    assert all((t == 0).all() for t in out)
+
+
+def test_ffn_rows_do_not_affect_each_other():
+    # a NaN row, an infinite row and a zero row among ordinary ones
+    T, d, I = 70, 256, 128
+    x, wg, wu, wd, _ = _ffn_inputs(T, d, I, 12)
+    desc = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc), dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(x)
+    cep.cep_gated_ffn(desc, x, wg, wu, wd, y, ws)
+    x2, y2 = x.clone(), torch.empty_like(x)
+    x2[3], x2[40, 7], x2[69] = float("nan"), float("inf"), 0.0
+    cep.cep_gated_ffn(desc, x2, wg, wu, wd, y2, ws)
+    same = torch.ones(T, dtype=torch.bool, device="cuda")
+    same[[3, 40, 69]] = False
+    assert torch.equal(y[same], y2[same])
+    assert torch.isnan(y2[3]).all() and (y2[69] == 0).all()
+    assert not torch.isfinite(y2[40]).all()
+
+
+def test_ffn_extreme_gates():
+    # silu of large negative and positive gates: 0 and the gate itself
+    d = I = 64
+    x = torch.zeros(3, d, device="cuda", dtype=torch.bfloat16)
+    x[0, 0], x[1, 0], x[2, 0] = 200.0, -200.0, 100.0
+    wg, wu = torch.zeros(d, I, device="cuda", dtype=torch.bfloat16), torch.zeros(
+        d, I, device="cuda", dtype=torch.bfloat16)
+    wg[0], wu[0] = 1.0, 1.0
+    wd = torch.eye(d, device="cuda", dtype=torch.bfloat16)
+    desc = cep.make_gated_ffn(rows=3, d_model=d, d_ff=I)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc, True), dtype=torch.uint8, device="cuda")
+    pre, y = torch.empty(3, 2, I, device="cuda"), torch.empty_like(x)
+    cep.cep_gated_ffn(desc, x, wg, wu, wd, y, ws, preact=pre)
+    assert (y[0] == 40000.0).all() == (torch.tensor(40000.0).bfloat16() == 40000.0)
+    assert (y[0].float() == torch.tensor(40000.0).bfloat16().float()).all()
+    assert (y[1] == 0).all() and (y[2].float() == torch.tensor(1e4).bfloat16().float()).all()
+    dx, dw = torch.empty_like(x), [torch.empty_like(t) for t in (wg, wu, wd)]
+    cep.cep_gated_ffn_backward(desc, torch.ones_like(x), x, wg, wu, wd, pre, dx, *dw, ws)
+    assert all(torch.isfinite(t).all() for t in (dx, *dw))
+
+
+# ------------------------------------------------------------------ graphs
+
+def test_operators_replay_in_a_graph():
+    g = _gen(21)
+    T, d, I, E, k, ranks = 300, 256, 128, 64, 4, 4
+    x, r = _randn(g, T, d), _randn(g, T, d)
+    w = torch.ones(d, device="cuda")
+    _, wg, wu, wd, dy = _ffn_inputs(T, d, I, 3)
+    logits = _randn(g, T, E, dtype=torch.float32)
+    stride = cep.cep_row_bytes(d, cep.CEP_MXFP8)
+    nd = cep.make_norm(rows=T, d=d, x_dtype=BF16, res_dtype=BF16, w_dtype=F32, y_dtype=BF16,
+                       eps=EPS, ld_codes=stride, ld_scales=stride)
+    gd = cep.make_gate(rows=T, n_experts=E, top_k=k, normalize=1, scale=1.0)
+    sd = cep.make_dispatch(rows=T, top_k=k, n_ranks=ranks, experts_per_rank=E // ranks,
+                           capacity=T * k, row_bytes=stride)
+    fd = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I)
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt, device="cuda")
+    o = dict(res=z(T, d), y=z(T, d), rows=z(T, stride, dt=torch.uint8),
+             ids=z(T, k, dt=torch.int32), tw=z(T, k, dt=torch.float32),
+             plan=z(2 * ranks + 2, dt=torch.int32), token=z(T * k, dt=torch.int32),
+             oid=z(T * k, k, dt=torch.int32), ow=z(T * k, k, dt=torch.float32),
+             ox=z(T * k, stride, dt=torch.uint8), out=z(T, d), pre=z(T, 2, I, dt=torch.float32),
+             dx=z(T, d), dwg=z(d, I), dwu=z(d, I), dwd=z(I, d), dn=z(T, d),
+             dw=z(d, dt=torch.float32))
+    space = lambda n: z(n, dt=torch.uint8)
+    w1, w2, w3 = (space(cep.cep_dispatch_workspace(sd)), space(cep.cep_gated_ffn_workspace(fd, 1)),
+                  space(cep.cep_rms_norm_workspace(nd)))
+
+    def step(s):
+        cep.cep_rms_norm(nd, x, w, residual=r, res_out=o["res"], y=o["y"], codes=o["rows"],
+                         scales=o["rows"].data_ptr() + d, stream=s)
+        cep.cep_gate_topk(gd, logits, None, o["ids"], o["tw"], stream=s)
+        cep.cep_dispatch(sd, o["ids"], o["tw"], o["rows"], o["plan"], o["token"], o["oid"],
+                         o["ow"], o["ox"], w1, stream=s)
+        cep.cep_gated_ffn(fd, o["y"], wg, wu, wd, o["out"], w2, preact=o["pre"], stream=s)
+        cep.cep_gated_ffn_backward(fd, dy, o["y"], wg, wu, wd, o["pre"], o["dx"], o["dwg"],
+                                   o["dwu"], o["dwd"], w2, stream=s)
+        cep.cep_rms_norm_backward(nd, o["res"], w, o["dx"], None, o["dn"], o["dw"], w3, stream=s)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(torch.cuda.current_stream())
+    for i in range(3):
+        # other inputs in the same places, and eager work between the replays
+        x.copy_(_randn(g, T, d))
+        logits.copy_(_randn(g, T, E, dtype=torch.float32))
+        for t in o.values():
+            t.zero_()
+        step(None)
+        torch.cuda.synchronize()
+        eager = {n: t.clone() for n, t in o.items()}
+        for t in o.values():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in o.items():
+            assert torch.equal(t, eager[n]), (i, n)

@@ -456,8 +456,8 @@ int cep_dispatch(const cep_dispatch_desc *desc, const int32_t *topk_id, const fl
 typedef struct {
   int rows;              /* 0..2^24                                           */
   int d_model, d_ff;     /* multiples of 8, 8..32768                          */
-  int64_t ld_x;          /* row strides in elements, multiples of 8: x,       */
-  int64_t ld_y;          /*   y and dy,                                       */
+  int64_t ld_x;          /* row strides in elements, multiples of 8, up to    */
+  int64_t ld_y;          /*   2^21: x; y and dy;                              */
   int64_t ld_dx;         /*   dx                                              */
 } cep_gated_ffn_desc;
 

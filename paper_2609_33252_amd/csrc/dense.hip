@@ -8,6 +8,7 @@
 // Six products of three layouts, C[m][n] = sum over k of A(m, k) B(k, n): A
 // has k or m contiguous, B k or n.
 #include "block_ops.h"
+#include "dense.h"
 #include "gemm_common.h"
 
 #include <algorithm>
@@ -369,8 +370,10 @@ using namespace cep;
 
 CEP_API size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *d, int backward) {
   if (bad_desc(d)) return 0;
-  // forward: h; backward: [dg | du] and h
-  return std::max<size_t>((size_t)d->rows * d->d_ff * (backward ? 6 : 2), 256);
+  // forward: h, or the row blocks' scratch; backward: [dg | du] and h
+  const RowsPlan p = rows_plan(d->rows, d->d_model, d->d_ff);
+  const size_t rows = p.use ? rows_workspace(p, d->rows, d->d_model, d->d_ff) : 0;
+  return std::max<size_t>({(size_t)d->rows * d->d_ff * (backward ? 6 : 2), rows, 256});
 }
 
 CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void *w_gate,
@@ -387,6 +390,12 @@ CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_gated_ffn_workspace(d, 0));
   const int T = d->rows, D = d->d_model, I = d->d_ff;
+  if (const RowsPlan p = rows_plan(T, D, I); p.use) {
+    launch_rows_ffn(p, T, D, I, (const __bf16 *)x, d->ld_x ? d->ld_x : D, (const __bf16 *)w_gate,
+                    (const __bf16 *)w_up, (const __bf16 *)w_down, (__bf16 *)y,
+                    d->ld_y ? d->ld_y : D, preact, (uint8_t *)workspace, s);
+    return launched(fn);
+  }
   DenseArgs a{};
   a.A = (const __bf16 *)x;
   a.B0 = (const __bf16 *)w_gate;

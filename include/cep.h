@@ -467,7 +467,9 @@ typedef struct {
  * y [rows][d_model].  The hidden row is rounded to bf16 once, for the second
  * product.  preact (NULL: not kept) gets x Wg and x Wu, float32
  * [rows][2][d_ff], for cep_gated_ffn_backward.  All pointers 16-byte aligned;
- * y may not overlap x.  workspace: cep_gated_ffn_workspace(desc, 0) bytes. */
+ * y may not overlap x.  workspace: cep_gated_ffn_workspace(desc, 0) bytes for
+ * this call alone, (desc, 1) bytes for this call and the backward one (one after
+ * the other; nothing in it is kept between them). */
 size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *desc, int backward);
 int cep_gated_ffn(const cep_gated_ffn_desc *desc, const void *x, const void *w_gate,
                   const void *w_up, const void *w_down, void *y, float *preact, void *workspace,
@@ -477,8 +479,7 @@ int cep_gated_ffn(const cep_gated_ffn_desc *desc, const void *x, const void *w_g
  * weights and preact, the gradients dx [rows][d_model], dw_gate, dw_up
  * [d_model][d_ff] and dw_down [d_ff][d_model], bf16, written, not added to.
  * The gradients of the two projections and the hidden row are rounded to bf16
- * once, for the products that follow.  workspace:
- * cep_gated_ffn_workspace(desc, 1) bytes. */
+ * once, for the products that follow. */
 int cep_gated_ffn_backward(const cep_gated_ffn_desc *desc, const void *dy, const void *x,
                            const void *w_gate, const void *w_up, const void *w_down,
                            const float *preact, void *dx, void *dw_gate, void *dw_up,

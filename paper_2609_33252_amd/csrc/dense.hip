@@ -25,6 +25,7 @@ enum Epilogue {
   kSwiGlu,  // two products g, u: h = silu(g) u to out0, g and u to pre
   kGrad     // dh: with g, u from pre, [dg | du] to out0 and h to out1
 };
+constexpr bool is_dual(int epi) { return epi == kStore2 || epi == kSwiGlu; }
 
 struct DenseArgs {
   const __bf16 *A, *B0, *B1;
@@ -34,9 +35,65 @@ struct DenseArgs {
   __bf16 *out0, *out1;
   int64_t ldo;
   float *pre;     // [M][2][N]
+  int splits;     // K shares; above one, their sums go to part
+  float *part;    // [splits][M][N, or 2 N of two products]
 };
 
 __device__ inline float sigma(float g) { return 1.0f / (1.0f + __expf(-g)); }
+
+__device__ inline void store_bf16(__bf16 *p, const f32x4 &v) {
+  *(uint2 *)p = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+}
+
+// Four consecutive outputs of row m from their sums v (and w, of the second
+// product).
+template <int EPI>
+__device__ inline void finish(const DenseArgs &a, int64_t m, int n, const f32x4 &v, const f32x4 &w) {
+  if (EPI == kStore || EPI == kStore2) store_bf16(a.out0 + m * a.ldo + n, v);
+  if (EPI == kStore2) store_bf16(a.out1 + m * a.ldo + n, w);
+  if (EPI == kSwiGlu) {
+    f32x4 h;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) h[r] = v[r] * sigma(v[r]) * w[r];
+    store_bf16(a.out0 + m * a.ldo + n, h);
+    if (a.pre) {
+      *(f32x4 *)(a.pre + m * 2 * a.N + n) = v;
+      *(f32x4 *)(a.pre + m * 2 * a.N + a.N + n) = w;
+    }
+  }
+  if (EPI == kGrad) {
+    const f32x4 g = *(const f32x4 *)(a.pre + m * 2 * a.N + n);
+    const f32x4 u = *(const f32x4 *)(a.pre + m * 2 * a.N + a.N + n);
+    f32x4 dg, du, h;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float s = sigma(g[r]);
+      dg[r] = v[r] * u[r] * s * (1.0f + g[r] * (1.0f - s));
+      du[r] = v[r] * g[r] * s;
+      h[r] = g[r] * s * u[r];
+    }
+    store_bf16(a.out0 + m * 2 * a.N + n, dg);
+    store_bf16(a.out0 + m * 2 * a.N + a.N + n, du);
+    store_bf16(a.out1 + m * a.N + n, h);
+  }
+}
+
+// The shares' sums, added in order, and what becomes of them.
+template <int EPI>
+__global__ __launch_bounds__(256) void k_dense_finish(DenseArgs a) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = q / (a.N / 4);
+  const int n = (int)(q % (a.N / 4)) * 4;
+  if (m >= a.M) return;
+  const int64_t width = is_dual(EPI) ? 2 * a.N : a.N;
+  f32x4 v = {}, w = {};
+  for (int i = 0; i < a.splits; ++i) {
+    const float *p = a.part + ((int64_t)i * a.M + m) * width + n;
+    v += *(const f32x4 *)p;
+    if (is_dual(EPI)) w += *(const f32x4 *)(p + a.N);
+  }
+  finish<EPI>(a, m, n, v, w);
+}
 
 // p, the same in every lane, in scalar registers
 __device__ inline const char *uniform(const char *p) {
@@ -46,12 +103,13 @@ __device__ inline const char *uniform(const char *p) {
   return (const char *)((uint64_t)hi << 32 | lo);
 }
 
-// The product in tiles of 2 HALF x 2 HALF, K in steps of 64, HALF / 16 waves.
+// The product in tiles of 2 HALF x 2 HALF outputs, K in steps of 64, by WM x WN
+// waves.
 //
 // Each operand's 64-wide step is two halves of HALF rows (columns), loaded
-// straight to LDS; the two operand halves meet in four quadrants, one phase
-// each, in which a wave multiplies HALF/2 x 32 outputs (16 matrix
-// instructions at HALF 128).  Quadrants follow a snake (A0 B0, A0 B1, A1 B1,
+// straight to LDS; the operands' halves meet in four quadrants, one phase
+// each, in which a wave multiplies HALF/WM x HALF/WN outputs (16 matrix
+// instructions in the larger tiles).  Quadrants follow a snake (A0 B0, A0 B1, A1 B1,
 // A1 B0, then B swapped in the next step), so that only one operand half
 // changes from phase to phase.  A half of A is read into the registers of the
 // one before as soon as their last matrix instruction has issued, a half of B
@@ -68,49 +126,54 @@ __device__ inline const char *uniform(const char *p) {
 //     a fragment is two transposing 8-byte reads of four lines of k
 // Measured (kernel alone): 8192 x 7168 x 2 x 2048 with SwiGLU 337 us, 1.43
 // PFLOP/s; bound by the matrix cores' issue and the loads that miss L2.
-template <int HALF, bool A_K, bool B_K, int EPI>
-__global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
-  constexpr bool DUAL = EPI == kStore2 || EPI == kSwiGlu;
-  constexpr int MF = HALF / 32, NF = 2;   // fragments of a wave in a half
-  constexpr int HB = HALF * 128;          // bytes of a half
-  constexpr int STAGE = 4 * HB;           // A0, A1, B0, B1
+template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
+  constexpr bool DUAL = is_dual(EPI);
+  constexpr int MF = HALF / 16 / WM, NF = HALF / 16 / WN;  // fragments of a wave in a half
+  constexpr int HB = HALF * 128;                           // bytes of a half
+  constexpr int STAGE = 4 * HB;                            // A0, A1, B0, B1
+  constexpr int LOADS = HB / 1024 / (WM * WN);             // 1 KB loads of a wave of a half
   constexpr int TN = DUAL ? HALF : 2 * HALF;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l15 = lane & 15, g4 = lane >> 4;
-  const int wm = wave & 1, wn = wave >> 1;
-  const int n_tn = (a.N + TN - 1) / TN;
+  const int wm = wave % WM, wn = wave / WM;
+  const int n_tm = (a.M + 2 * HALF - 1) / (2 * HALF), n_tn = (a.N + TN - 1) / TN;
   int mt, nt;
-  if (!work_item<kGroupM, false>(0, (a.M + 2 * HALF - 1) / (2 * HALF), n_tn, &mt, &nt)) return;
-  const int m0 = mt * 2 * HALF, n0 = nt * TN;
+  // the shares of a tile are separate items, share by share
+  if (!work_item<kGroupM, false>(0, n_tm * a.splits, n_tn, &mt, &nt)) return;
+  const int share = mt / n_tm;
+  const int m0 = (mt - share * n_tm) * 2 * HALF, n0 = nt * TN;
 
-  // ---- loads: per half two 1 KB pieces a wave, lane offsets from a base that
-  // advances with k; rows and columns past the end read the last ones
+  // ---- loads: lane offsets from a base that advances with k; rows and columns
+  // past the end read the last ones
   auto f_of = [](int k) {
     return HALF == 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
   };
-  constexpr int LPR = HALF / 8;  // lanes of a line of the row-contiguous layout
-  auto offset = [&](bool kc, int half, int e, int at0, int end, int64_t ld) -> uint32_t {
-    const int piece = wave * 2 + e;
+  // piece e of this wave's loads of a half; its line of k (row contiguous)
+  auto line_of = [&](int piece) { return piece * (512 / HALF) + lane / (HALF / 8); };
+  auto offset = [&](bool kc, int half, int piece, int at0, int end, int64_t ld) {
     if (kc) {
       const int r = piece * 8 + (lane >> 3);
       const int row = min(at0 + half * HALF + r, end - 1) - at0;
       return (uint32_t)(row * (int)ld * 2 + ((lane & 7) ^ ((r >> 1) & 7)) * 16);
     }
-    const int k = piece * (64 / LPR) + lane / LPR, pos = lane % LPR;
+    const int k = line_of(piece), pos = lane % (HALF / 8);
     const int chunk = (((pos >> 1) ^ f_of(k)) << 1) | (pos & 1);
     const int col = min(at0 + half * HALF + chunk * 8, end - 8) - at0;
     return (uint32_t)(k * (int)ld * 2 + col * 2);
   };
-  uint32_t offA[2][2], offB[2][2];
+  uint32_t offA[2][LOADS], offB[2][LOADS];
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
+  for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      offA[h][e] = offset(A_K, h, e, m0, a.M, a.lda);
-      offB[h][e] = offset(B_K, DUAL ? 0 : h, e, n0, a.N, a.ldb);
+    for (int e = 0; e < LOADS; ++e) {
+      offA[h][e] = offset(A_K, h, wave * LOADS + e, m0, a.M, a.lda);
+      offB[h][e] = offset(B_K, DUAL ? 0 : h, wave * LOADS + e, n0, a.N, a.ldb);
     }
-  const int full = a.K / 64, S = full * a.segs;  // whole steps
+  const int full = a.K / 64;  // whole steps of a segment
+  const int s0 = (int)((int64_t)full * a.segs * share / a.splits);
+  const int S = (int)((int64_t)full * a.segs * (share + 1) / a.splits) - s0;  // this share's
   const char *baseA = (const char *)(a.A + (A_K ? m0 * a.lda : m0));
   const char *baseB0 = (const char *)(a.B0 + (B_K ? n0 * a.ldb : n0));
   const char *baseB1 = a.B1 ? (const char *)(a.B1 + (B_K ? n0 * a.ldb : n0)) : nullptr;
@@ -119,37 +182,35 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
   auto ptrB = [&](int half, int seg, int step) {
     return ((DUAL ? half : seg) ? baseB1 : baseB0) + step * stepB;
   };
-  const uint32_t lds0 = lds_offset(lds) + wave * 2048;
-  // half `which` (0 A0, 1 first B, 2 second B, 3 A1) of step s, whose parity
-  // is P; the first B half is half P
+  const uint32_t lds0 = lds_offset(lds);
+  // half `which` (0 A0, 1 first B, 2 second B, 3 A1) of the share's step s,
+  // whose parity is P; the first B half is half P
   auto issue = [&](int s, auto which, auto parity) {
     constexpr int W = decltype(which)::value, P = decltype(parity)::value;
     constexpr bool IS_A = W == 0 || W == 3;
     constexpr int H = W == 0 ? 0 : W == 3 ? 1 : W == 1 ? P : 1 - P;
-    const int from = min(s, S - 1);
+    const int from = s0 + min(s, S - 1);
     const int seg = from >= full ? 1 : 0, step = from - (seg ? full : 0);
     const char *src = uniform(IS_A ? ptrA(seg, step) : ptrB(H, seg, step));
+    const uint32_t to = lds0 + P * STAGE + (IS_A ? H : 2 + H) * HB + wave * LOADS * 1024;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      dma16_s(src, IS_A ? offA[H][e] : offB[H][e],
-              lds0 + P * STAGE + (IS_A ? H : 2 + H) * HB + e * 1024);
+    for (int e = 0; e < LOADS; ++e) dma16_s(src, IS_A ? offA[H][e] : offB[H][e], to + e * 1024);
   };
 
   // ---- fragments
   // a lane's byte offsets in a half: k contiguous, of its chunk of each 32 of
   // k (a fragment of 16 rows further on: + 2 KB); row contiguous, of its piece
   // of each fragment (4 lines of k: + 4 lines)
-  constexpr int LINE = HALF * 2;
   int ra[A_K ? 2 : MF], rb[B_K ? 2 : NF];
   auto place = [&](bool kc, int row0, int i) {
     if (kc) return (row0 + l15) * 128 + ((g4 + 4 * i) ^ (l15 >> 1)) * 16;
     const int k = g4 * 8 + (l15 >> 2);
-    return k * LINE + (((row0 >> 4) + i) ^ f_of(k)) * 32 + (l15 & 3) * 8;
+    return k * HALF * 2 + (((row0 >> 4) + i) ^ f_of(k)) * 32 + (l15 & 3) * 8;
   };
 #pragma unroll
-  for (int i = 0; i < (A_K ? 2 : MF); ++i) ra[i] = place(A_K, wm * (HALF / 2), i);
+  for (int i = 0; i < (A_K ? 2 : MF); ++i) ra[i] = place(A_K, wm * MF * 16, i);
 #pragma unroll
-  for (int i = 0; i < (B_K ? 2 : NF); ++i) rb[i] = place(B_K, wn * 32, i);
+  for (int i = 0; i < (B_K ? 2 : NF); ++i) rb[i] = place(B_K, wn * NF * 16, i);
   auto read = [&](bool kc, const int *r, int base, int i, int ks) {
     if (kc) return *(const bf16x8 *)(lds + r[ks] + (base + i * 2048));
     union { bf16x8 v; bf16x4 h[2]; } o;
@@ -157,7 +218,7 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
     for (int h = 0; h < 2; ++h)
       o.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
           (__attribute__((address_space(3))) bf16x4 *)(lds + r[i] +
-                                                        (base + (ks * 32 + h * 4) * LINE)));
+                                                        (base + (ks * 32 + h * 4) * HALF * 2)));
     return o.v;
   };
   bf16x8 fa[MF][2], fb[2][NF][2];
@@ -214,7 +275,7 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
       if (Q == 3) read_a(0, 1 - P, ks);
       __builtin_amdgcn_sched_barrier(0);
     }
-    wait_vmcnt<8>();
+    wait_vmcnt<4 * LOADS>();
     sync();
   };
   auto whole_step = [&](int t, auto parity) {
@@ -231,12 +292,12 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
     issue(1, I0{}, I1{});
     issue(1, I1{}, I1{});
     issue(1, I2{}, I1{});
-    wait_vmcnt<10>();
+    wait_vmcnt<5 * LOADS>();
     sync();
     read_a(0, 0, 0);
     read_a(0, 0, 1);
     read_b(I0{}, 0);
-    wait_vmcnt<8>();
+    wait_vmcnt<4 * LOADS>();
     sync();
     for (int t = 0;;) {
       whole_step(t, I0{});
@@ -247,24 +308,21 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
     wait_vmcnt<0>();
     sync();
   }
-  if (a.K % 64) {  // the last, shorter step of each segment, zeros past K
+  if (a.K % 64 && share == a.splits - 1) {  // each segment's last, shorter step: zeros past K
     for (int seg = 0; seg < a.segs; ++seg) {
+      auto piece_in = [&](bool kc, int piece, const char *src, int half) {
+        const int r = piece * 8 + (lane >> 3);
+        const int k = full * 64 + (kc ? ((lane & 7) ^ ((r >> 1) & 7)) * 8 : line_of(piece));
+        const uint4 v = k < a.K ? *(const uint4 *)src : make_uint4(0u, 0u, 0u, 0u);
+        *(uint4 *)(lds + half * HB + piece * 1024 + lane * 16) = v;
+      };
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const bool is_a = h < 2;
-        const bool kc = is_a ? A_K : B_K;
-        const char *src = is_a ? ptrA(seg, full) : ptrB(h & 1, seg, full);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int piece = wave * 2 + e;
-          const int r = piece * 8 + (lane >> 3);
-          const int k = full * 64 + (kc ? ((lane & 7) ^ ((r >> 1) & 7)) * 8
-                                        : piece * (64 / LPR) + lane / LPR);
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (k < a.K) v = *(const uint4 *)(src + (is_a ? offA[h & 1][e] : offB[h & 1][e]));
-          *(uint4 *)(lds + h * HB + piece * 1024 + lane * 16) = v;
+        for (int e = 0; e < LOADS; ++e) {
+          piece_in(A_K, wave * LOADS + e, ptrA(seg, full) + offA[h][e], h);
+          piece_in(B_K, wave * LOADS + e, ptrB(h, seg, full) + offB[h][e], 2 + h);
         }
-      }
       __syncthreads();
       read_b(I0{}, 0);
       read_b(I1{}, 0);
@@ -282,71 +340,80 @@ __global__ __launch_bounds__(HALF * 4, 2) void k_dense(DenseArgs a) {
   }
 
   // lane: row lane % 16 of a fragment, four columns from 4 (lane / 16)
-  auto store4 = [](__bf16 *p, const f32x4 &v) {
-    *(uint2 *)p = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
-  };
 #pragma unroll
   for (int mh = 0; mh < 2; ++mh)
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      const int64_t m = m0 + mh * HALF + wm * (HALF / 2) + i * 16 + l15;
+      const int64_t m = m0 + mh * HALF + (wm * MF + i) * 16 + l15;
       if (m >= a.M) continue;
 #pragma unroll
       for (int nh = 0; nh < (DUAL ? 1 : 2); ++nh)
 #pragma unroll
         for (int j = 0; j < NF; ++j) {
-          const int n = n0 + nh * HALF + wn * 32 + j * 16 + g4 * 4;
+          const int n = n0 + nh * HALF + (wn * NF + j) * 16 + g4 * 4;
           if (n >= a.N) continue;
-          const f32x4 v = acc[mh][nh][i][j];
-          if (EPI == kStore) store4(a.out0 + m * a.ldo + n, v);
-          if (EPI == kStore2) {
-            store4(a.out0 + m * a.ldo + n, v);
-            store4(a.out1 + m * a.ldo + n, acc[mh][1][i][j]);
-          }
-          if (EPI == kSwiGlu) {
-            const f32x4 u = acc[mh][1][i][j];
-            f32x4 h;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[r] = v[r] * sigma(v[r]) * u[r];
-            store4(a.out0 + m * a.ldo + n, h);
-            if (a.pre) {
-              *(f32x4 *)(a.pre + m * 2 * a.N + n) = v;
-              *(f32x4 *)(a.pre + m * 2 * a.N + a.N + n) = u;
-            }
-          }
-          if (EPI == kGrad) {
-            const f32x4 g = *(const f32x4 *)(a.pre + m * 2 * a.N + n);
-            const f32x4 u = *(const f32x4 *)(a.pre + m * 2 * a.N + a.N + n);
-            f32x4 dg, du, h;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float s = sigma(g[r]);
-              dg[r] = v[r] * u[r] * s * (1.0f + g[r] * (1.0f - s));
-              du[r] = v[r] * g[r] * s;
-              h[r] = g[r] * s * u[r];
-            }
-            store4(a.out0 + m * 2 * a.N + n, dg);
-            store4(a.out0 + m * 2 * a.N + a.N + n, du);
-            store4(a.out1 + m * a.N + n, h);
+          if (a.splits == 1) {
+            finish<EPI>(a, m, n, acc[mh][nh][i][j], acc[mh][1][i][j]);
+          } else {
+            float *p = a.part + ((int64_t)share * a.M + m) * (DUAL ? 2 * a.N : a.N) + n;
+            *(f32x4 *)p = acc[mh][nh][i][j];
+            if (DUAL) *(f32x4 *)(p + a.N) = acc[mh][1][i][j];
           }
         }
     }
 }
 
+// Tile and K shares of a product.
+struct DensePlan {
+  int tile;  // 0: 256 x 256, 1: 128 x 128 (of both products' columns)
+  int splits;
+};
+constexpr int kTile[2] = {256, 128};
+
+int64_t dense_tiles(int t, int M, int N) {
+  return (int64_t)((M + kTile[t] - 1) / kTile[t]) * ((N + kTile[t] - 1) / kTile[t]);
+}
+
+// Time of a K step over all tiles, in us: 1.5 a round of 256-wide tiles, one a
+// compute unit; of 128-wide ones 1.0 with two a unit (512 in a round), 0.6 with
+// one.  (A 256 x 128 tile, in four or eight waves, was no faster than two
+// 128-wide ones: 4095 x 2048 x 4096 118 and 108 us against 104.)
+//
+// Few tiles share K until 256 workgroups run, while a share keeps six steps and
+// the steps saved outweigh the second launch (4096-wide products of 65 rows: 54
+// us whole, 27.4 in six shares, 37.7 in 16; of 512 rows, 128 tiles: 54.8 whole,
+// 47.7 in two, 55.1 in three).
+DensePlan dense_plan(int M, int n, int K, bool dual) {
+  const int N = dual ? 2 * n : n, steps = K / 64;
+  const int64_t n0 = dense_tiles(0, M, N), n1 = dense_tiles(1, M, N), rest = n1 % 512;
+  const double t0 = 1.5 * ((n0 + 255) / 256);
+  const double t1 = 1.0 * (n1 / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.6 : 1.0);
+  if (t0 < t1) return {0, 1};
+  const int splits = (int)std::min<int64_t>(n1 ? 256 / n1 : 1, steps / 6);
+  return {1, splits > 1 && steps - steps / splits >= 10 ? splits : 1};
+}
+
+// Scratch of a product's shares.
+size_t part_bytes(int M, int n, int K, bool dual) {
+  const DensePlan p = dense_plan(M, n, K, dual);
+  return p.splits > 1 ? (size_t)p.splits * M * n * (dual ? 8 : 4) : 0;
+}
+
 template <bool A_K, bool B_K, int EPI>
-void launch_dense(const DenseArgs &a, hipStream_t s) {
-  constexpr bool DUAL = EPI == kStore2 || EPI == kSwiGlu;
-  auto tiles = [&](int half) {
-    const int tn = DUAL ? half : 2 * half;
-    return (long long)((a.M + 2 * half - 1) / (2 * half)) * ((a.N + tn - 1) / tn);
-  };
-  // 256-wide tiles when they occupy most compute units, else 128-wide ones
-  const bool large = tiles(128) >= 160;
-  const dim3 grid((unsigned)((tiles(large ? 128 : 64) + 7) / 8 * 8));
-  if (large)
-    hipLaunchKernelGGL((k_dense<128, A_K, B_K, EPI>), grid, dim3(512), 0, s, a);
+void launch_dense(DenseArgs a, float *part, hipStream_t s) {
+  const DensePlan p = dense_plan(a.M, a.N, a.K * a.segs, is_dual(EPI));
+  a.splits = p.splits;
+  a.part = part;
+  const int N = is_dual(EPI) ? 2 * a.N : a.N;
+  const int64_t items = dense_tiles(p.tile, a.M, N) * p.splits;
+  const dim3 grid((unsigned)((items + 7) / 8 * 8));
+  if (p.tile == 0)
+    hipLaunchKernelGGL((k_dense<128, 2, 4, A_K, B_K, EPI>), grid, dim3(512), 0, s, a);
   else
-    hipLaunchKernelGGL((k_dense<64, A_K, B_K, EPI>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_dense<64, 2, 2, A_K, B_K, EPI>), grid, dim3(256), 0, s, a);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((k_dense_finish<EPI>),
+                       dim3((unsigned)(((int64_t)a.M * (a.N / 4) + 255) / 256)), dim3(256), 0, s, a);
 }
 
 // a tile's offsets from its base stay below 2^31 bytes
@@ -363,6 +430,11 @@ const char *bad_desc(const cep_gated_ffn_desc *d) {
   return nullptr;
 }
 
+// [dg | du] and h of the backward pass, h of the forward one
+size_t hidden_bytes(const cep_gated_ffn_desc *d, int backward) {
+  return align_up((size_t)d->rows * d->d_ff * (backward ? 6 : 2), 256);
+}
+
 }  // namespace
 }  // namespace cep
 
@@ -370,10 +442,17 @@ using namespace cep;
 
 CEP_API size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *d, int backward) {
   if (bad_desc(d)) return 0;
-  // forward: h, or the row blocks' scratch; backward: [dg | du] and h
-  const RowsPlan p = rows_plan(d->rows, d->d_model, d->d_ff);
-  const size_t rows = p.use ? rows_workspace(p, d->rows, d->d_model, d->d_ff) : 0;
-  return std::max<size_t>({(size_t)d->rows * d->d_ff * (backward ? 6 : 2), rows, 256});
+  const int T = d->rows, D = d->d_model, I = d->d_ff;
+  // forward: h, or the row blocks' scratch; backward: [dg | du] and h; then the
+  // K shares of the products
+  const RowsPlan p = rows_plan(T, D, I);
+  size_t part = 0;
+  if (backward)
+    part = std::max({part_bytes(T, I, D, false), part_bytes(T, D, 2 * I, false),
+                     part_bytes(D, I, T, true), part_bytes(I, D, T, false)});
+  if (!p.use) part = std::max({part, part_bytes(T, I, D, true), part_bytes(T, D, I, false)});
+  const size_t rows = p.use ? rows_workspace(p, T, D, I) : 0;
+  return std::max(std::max<size_t>(hidden_bytes(d, backward) + part, rows), (size_t)256);
 }
 
 CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void *w_gate,
@@ -406,7 +485,8 @@ CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void
   a.out0 = (__bf16 *)workspace;
   a.ldo = I;
   a.pre = preact;
-  launch_dense<true, false, kSwiGlu>(a, s);
+  float *part = (float *)((uint8_t *)workspace + hidden_bytes(d, 0));
+  launch_dense<true, false, kSwiGlu>(a, part, s);
   DenseArgs b{};
   b.A = (const __bf16 *)workspace;
   b.B0 = (const __bf16 *)w_down;
@@ -414,7 +494,7 @@ CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void
   b.M = T, b.N = D, b.K = I, b.segs = 1;
   b.out0 = (__bf16 *)y;
   b.ldo = d->ld_y ? d->ld_y : D;
-  launch_dense<true, false, kStore>(b, s);
+  launch_dense<true, false, kStore>(b, part, s);
   return launched(fn);
 }
 
@@ -438,6 +518,7 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   const int T = d->rows, D = d->d_model, I = d->d_ff;
   const int64_t ld_x = d->ld_x ? d->ld_x : D, ld_y = d->ld_y ? d->ld_y : D;
   __bf16 *dgu = (__bf16 *)workspace, *h = dgu + (size_t)T * 2 * I;
+  float *part = (float *)((uint8_t *)workspace + hidden_bytes(d, 1));
   if (T) {
     DenseArgs a{};  // dh, and from it dg, du and h
     a.A = (const __bf16 *)dy;
@@ -446,7 +527,7 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
     a.M = T, a.N = I, a.K = D, a.segs = 1;
     a.out0 = dgu, a.out1 = h;
     a.pre = const_cast<float *>(preact);
-    launch_dense<true, true, kGrad>(a, s);
+    launch_dense<true, true, kGrad>(a, part, s);
     DenseArgs b{};  // dx
     b.A = dgu;
     b.B0 = (const __bf16 *)w_gate;
@@ -455,7 +536,7 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
     b.M = T, b.N = D, b.K = I, b.segs = 2;
     b.out0 = (__bf16 *)dx;
     b.ldo = d->ld_dx ? d->ld_dx : D;
-    launch_dense<true, true, kStore>(b, s);
+    launch_dense<true, true, kStore>(b, part, s);
   }
   DenseArgs c{};  // dWg, dWu
   c.A = (const __bf16 *)x;
@@ -465,7 +546,7 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   c.M = D, c.N = I, c.K = T, c.segs = 1;
   c.out0 = (__bf16 *)dw_gate, c.out1 = (__bf16 *)dw_up;
   c.ldo = I;
-  launch_dense<false, false, kStore2>(c, s);
+  launch_dense<false, false, kStore2>(c, part, s);
   DenseArgs e{};  // dWd
   e.A = h;
   e.B0 = (const __bf16 *)dy;
@@ -473,6 +554,6 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   e.M = I, e.N = D, e.K = T, e.segs = 1;
   e.out0 = (__bf16 *)dw_down;
   e.ldo = D;
-  launch_dense<false, false, kStore>(e, s);
+  launch_dense<false, false, kStore>(e, part, s);
   return launched(fn);
 }

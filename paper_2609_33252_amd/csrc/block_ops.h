@@ -36,28 +36,27 @@ inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) =
 inline size_t dtype_bytes(int t) { return t == CEP_F32 ? 4 : 2; }
 
 // 16 bytes at an address of any alignment (one global access either way).
-struct __attribute__((packed, aligned(1))) Any16 {
-  uint32_t v[4];
-};
+typedef uint32_t Vec16 __attribute__((ext_vector_type(4)));
+typedef Vec16 Any16 __attribute__((aligned(1)));
 
 // Eight consecutive values of a float32 or bf16 row, n of them inside it (the
 // others read as zero and are not stored).
 __device__ inline void load8(const void *row, int dtype, int64_t at, int n, float v[8]) {
   if (n >= 8) {
     if (dtype == CEP_BF16) {
-      const Any16 u = *(const Any16 *)((const char *)row + at * 2);
+      const Vec16 u = *(const Any16 *)((const char *)row + at * 2);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        v[2 * j] = __uint_as_float(u.v[j] << 16);
-        v[2 * j + 1] = __uint_as_float(u.v[j] & 0xffff0000u);
+        v[2 * j] = __uint_as_float(u[j] << 16);
+        v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
       }
     } else {
-      const Any16 lo = *(const Any16 *)((const char *)row + at * 4);
-      const Any16 hi = *(const Any16 *)((const char *)row + at * 4 + 16);
+      const Vec16 lo = *(const Any16 *)((const char *)row + at * 4);
+      const Vec16 hi = *(const Any16 *)((const char *)row + at * 4 + 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        v[j] = __uint_as_float(lo.v[j]);
-        v[4 + j] = __uint_as_float(hi.v[j]);
+        v[j] = __uint_as_float(lo[j]);
+        v[4 + j] = __uint_as_float(hi[j]);
       }
     }
     return;
@@ -79,16 +78,16 @@ __device__ inline uint32_t bf16_pair(float a, float b) {
 
 __device__ inline void store8(void *row, int dtype, int64_t at, int n, const float v[8]) {
   if (n >= 8) {
-    Any16 u;
+    Vec16 u;
     if (dtype == CEP_BF16) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u.v[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
+      for (int j = 0; j < 4; ++j) u[j] = bf16_pair(v[2 * j], v[2 * j + 1]);
       *(Any16 *)((char *)row + at * 2) = u;
     } else {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) u.v[j] = __float_as_uint(v[4 * h + j]);
+        for (int j = 0; j < 4; ++j) u[j] = __float_as_uint(v[4 * h + j]);
         *(Any16 *)((char *)row + at * 4 + 16 * h) = u;
       }
     }

@@ -2,11 +2,13 @@
 // for gfx950 (Appendix C, "Asynchronous dispatch": a source lane's rows travel
 // to the rank that holds their experts).
 //
-// The tokens of a rank keep their order.  A token's place in a rank's segment
-// is the number of earlier tokens that go there too: k_send_count writes it
-// per tile of tokens and block, k_send adds the blocks before it, and copies
-// each row once from memory to all of its places.  Bound by HBM: every row is
-// read once and written once per rank it goes to.
+// The tokens of a rank keep their order: a token's place in a rank's segment
+// is the number of earlier tokens that go there too.  A few tokens are packed
+// by one launch, a workgroup a token, each of which counts for itself
+// (k_send_few).  More take three: the counts per block of 256 tokens
+// (k_send_count), their prefix sums and the plan (k_send_scan), and the rows
+// (k_send), a wave a token, which reads its row once, before it knows where the
+// row goes, and writes it to each of its places.  Bound by HBM.
 #include "block_ops.h"
 
 #include <algorithm>
@@ -14,8 +16,9 @@
 namespace cep {
 namespace {
 
-constexpr int kMaxRanks = 64;     // one lane each
-constexpr int kCountTokens = 256;  // tokens of a k_send_count block (one wave)
+constexpr int kMaxRanks = 64;      // one lane each
+constexpr int kFewTokens = 256;    // packed by one launch
+constexpr int kCountTokens = 256;  // tokens of a k_send_count block
 constexpr int kSendTokens = 16;    // tokens of a k_send block (a tile)
 constexpr int kTiles = kCountTokens / kSendTokens;
 
@@ -30,172 +33,264 @@ struct SendArgs {
   float *out_w;
   char *out_x;
   // tile_at [tiles][R]: earlier tokens of the tile's block that go to a rank;
-  // tot, pairs [blocks][R]; bad [blocks]
+  // tot (after the scan: of the blocks before), pairs [blocks][R]; bad [blocks]
   int32_t *tile_at, *tot, *pairs, *bad;
-  int rows, k, R, per, blocks, capacity;
+  int rows, k, R, per, blocks;
   int64_t row_bytes;
 };
 
-// The ranks (a bit each) that hold the token's experts; *bad counts ids that
-// no rank has, apart from -1 (no expert).
-__device__ inline uint64_t ranks_of(const SendArgs &a, int64_t t, int *bad) {
+// The rank that holds an expert, -1: none.
+__device__ inline int rank_of(const SendArgs &a, int id) {
+  return id >= 0 && id < a.R * a.per ? id / a.per : -1;
+}
+
+// The ranks (a bit each) that hold the experts of token t; counts its pairs
+// per rank, and its ids that no rank has (apart from -1), in LDS.
+__device__ inline uint64_t ranks_of(const SendArgs &a, int64_t t, int32_t *pairs, int32_t *bad) {
+  int32_t id[kMaxTopK];
+#pragma unroll
+  for (int j = 0; j < kMaxTopK; ++j) id[j] = j < a.k ? a.ids[t * a.k + j] : -1;
   uint64_t m = 0;
-  for (int j = 0; j < a.k; ++j) {
-    const int id = a.ids[t * a.k + j];
-    if (id >= 0 && id < a.R * a.per) m |= 1ull << (id / a.per);
-    else if (id != -1) ++*bad;
+#pragma unroll
+  for (int j = 0; j < kMaxTopK; ++j) {
+    if (j >= a.k) continue;
+    const int r = rank_of(a, id[j]);
+    if (r >= 0) {
+      m |= 1ull << r;
+      atomicAdd(&pairs[r], 1);
+    } else if (id[j] != -1) {
+      atomicAdd(bad, 1);
+    }
   }
   return m;
 }
 
-// Wave: the tokens [256 b, 256 b + 256), 64 at a time.  Lane r keeps rank r's
-// count.
-__device__ inline void count_block(const SendArgs &a, int b, int32_t *tile_at, int32_t *tot,
-                                   int32_t *pairs, int32_t *bad_out, int32_t *lds_pairs) {
+// Sum over the lanes before this one.
+__device__ inline int wave_before(int v) {
   const int lane = threadIdx.x & 63;
-  lds_pairs[lane] = 0;
-  int run = 0, bad = 0;
-  for (int q = 0; q < kCountTokens / 64; ++q) {
-    const int64_t t = (int64_t)b * kCountTokens + q * 64 + lane;
-    uint64_t m = 0;
-    if (t < a.rows) {
-      m = ranks_of(a, t, &bad);
-      for (int j = 0; j < a.k; ++j) {
-        const int id = a.ids[t * a.k + j];
-        if (id >= 0 && id < a.R * a.per) atomicAdd(&lds_pairs[id / a.per], 1);
-      }
-    }
-    uint64_t there = 0;  // of rank `lane`: the round's tokens that go there
-    for (int r = 0; r < a.R; ++r) {
-      const uint64_t v = __ballot((m >> r) & 1);
-      if (lane == r) there = v;
-    }
-    if (lane < a.R) {
+  int s = v;
 #pragma unroll
-      for (int i = 0; i < 64 / kSendTokens; ++i)
-        tile_at[(q * (64 / kSendTokens) + i) * a.R + lane] =
-            run + (int)__popcll(there & ((1ull << (i * kSendTokens)) - 1));
-    }
-    run += (int)__popcll(there);
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(s, o);
+    if (lane >= o) s += u;
   }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) bad += __shfl_xor(bad, o);
-  if (lane < a.R) {
-    tot[lane] = run;
-    pairs[lane] = lds_pairs[lane];
-  }
-  if (lane == 0) *bad_out = bad;
+  return s - v;
 }
 
-__global__ __launch_bounds__(64) void k_send_count(SendArgs a) {
-  __shared__ int32_t lds_pairs[64];
-  const size_t b = blockIdx.x;
-  count_block(a, b, a.tile_at + b * kTiles * a.R, a.tot + b * a.R, a.pairs + b * a.R, a.bad + b,
-              lds_pairs);
-}
-
-// One block per tile of tokens.  ONE: all tokens are one counting block, which
-// every workgroup counts for itself (one launch).
-template <bool ONE>
-__global__ __launch_bounds__(256) void k_send(SendArgs a) {
-  __shared__ int32_t all[kMaxRanks], before[kMaxRanks], pairs[kMaxRanks], first[kMaxRanks + 1];
-  __shared__ int32_t at[kMaxRanks];
-  __shared__ int32_t one_at[ONE ? kTiles * kMaxRanks : 1], one_pairs[64], n_bad;
-  __shared__ uint64_t mask[kSendTokens];
+// Thread t counts token t of a block; lane r of a wave keeps rank r's count.
+__global__ __launch_bounds__(kCountTokens) void k_send_count(SendArgs a) {
+  __shared__ int32_t pairs[kMaxRanks], bad, sent[4][kMaxRanks];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tile = blockIdx.x, block = tile / kTiles;
-  if (tid < a.R) all[tid] = before[tid] = pairs[tid] = 0;
-  if (tid == 0) n_bad = 0;
+  const int64_t b = blockIdx.x, t = b * kCountTokens + tid;
+  if (tid < kMaxRanks) pairs[tid] = 0;
+  if (tid == 0) bad = 0;
   __syncthreads();
-  if (ONE) {
-    if (wave == 0) count_block(a, 0, one_at, all, pairs, &n_bad, one_pairs);
-  } else {
-    for (int i = tid; i < a.blocks * a.R; i += 256) {
-      const int r = i % a.R, v = a.tot[i];
-      atomicAdd(&all[r], v);
-      if (i < block * a.R) atomicAdd(&before[r], v);
-      if (tile == 0) atomicAdd(&pairs[r], a.pairs[i]);
-    }
-    if (tile == 0)
-      for (int i = tid; i < a.blocks; i += 256) atomicAdd(&n_bad, a.bad[i]);
+  const uint64_t m = t < a.rows ? ranks_of(a, t, pairs, &bad) : 0;
+  uint64_t there = 0;  // the wave's tokens that go to rank `lane`
+  for (int r = 0; r < a.R; ++r) {
+    const uint64_t v = __ballot((m >> r) & 1);
+    if (lane == r) there = v;
   }
-  // the tile's tokens: where each goes
-  const int64_t t0 = (int64_t)tile * kSendTokens;
-  if (wave == 1 && lane < kSendTokens) {
-    int bad = 0;
-    mask[lane] = t0 + lane < a.rows ? ranks_of(a, t0 + lane, &bad) : 0;
-  }
+  sent[wave][lane] = (int)__popcll(there);
   __syncthreads();
-  if (tid == 0) {
-    int n = 0;
-    for (int r = 0; r < a.R; ++r) {
-      first[r] = n;
-      n += all[r];
-    }
-    first[a.R] = n;
-  }
-  __syncthreads();
-  if (tid < a.R)
-    at[tid] = first[tid] + before[tid] +
-              (ONE ? one_at[tile * a.R + tid] : a.tile_at[(size_t)tile * a.R + tid]);
-  if (tile == 0) {
-    if (tid <= a.R) a.plan[tid] = first[tid];
-    if (tid < a.R) a.plan[a.R + 1 + tid] = pairs[tid];
-    if (tid == 0) a.plan[2 * a.R + 1] = n_bad;
-  }
-  __syncthreads();
-  const int64_t chunks = a.row_bytes / 16;
-  const int tail = (int)(a.row_bytes % 16);
-  for (int i = wave; i < kSendTokens; i += 4) {
-    const int64_t t = t0 + i;
-    if (t >= a.rows) return;
-    const uint64_t m = mask[i];
-    if (!m) continue;
-    // lane r: the token's place in rank r's segment, -1 if it does not go there
-    int place = -1;
-    if (lane < a.R && ((m >> lane) & 1)) {
-      place = at[lane];
-      for (int j = 0; j < i; ++j) place += (int)((mask[j] >> lane) & 1);
-      if (place >= a.capacity) place = -1;
-    }
-    const uint64_t go = __ballot(place >= 0);
-    for (uint64_t g = go; g; g &= g - 1) {
-      const int r = __builtin_ctzll(g);
-      const int64_t p = __shfl(place, r);
-      if (lane == 0) a.token[p] = (int32_t)t;
-      if (lane < a.k) {
-        const int id = a.ids[t * a.k + lane];
-        const bool here = id >= 0 && id / a.per == r;
-        a.out_id[p * a.k + lane] = here ? id - r * a.per : -1;
-        a.out_w[p * a.k + lane] = here ? a.w[t * a.k + lane] : 0.f;
-      }
-    }
-    const char *src = a.x + t * a.ld_x;
-    constexpr int U = 8;
-    for (int64_t c0 = 0; c0 < chunks; c0 += 64 * U) {
-      Any16 v[U];
+  int run = 0;
+  for (int i = 0; i < wave; ++i) run += sent[i][lane];
+  if (lane < a.R) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t c = c0 + u * 64 + lane;
-        if (c < chunks) v[u] = *(const Any16 *)(src + c * 16);
-      }
-      for (uint64_t g = go; g; g &= g - 1) {
-        char *dst = a.out_x + (int64_t)__shfl(place, __builtin_ctzll(g)) * a.row_bytes;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int64_t c = c0 + u * 64 + lane;
-          if (c < chunks) *(Any16 *)(dst + c * 16) = v[u];
-        }
-      }
-    }
-    if (tail) {
-      const char v = lane < tail ? src[chunks * 16 + lane] : 0;
-      for (uint64_t g = go; g; g &= g - 1) {
-        const int64_t p = __shfl(place, __builtin_ctzll(g));  // every lane takes part
-        if (lane < tail) a.out_x[p * a.row_bytes + chunks * 16 + lane] = v;
-      }
+    for (int i = 0; i < 64 / kSendTokens; ++i)
+      a.tile_at[(b * kTiles + wave * (64 / kSendTokens) + i) * a.R + lane] =
+          run + (int)__popcll(there & ((1ull << (i * kSendTokens)) - 1));
+    if (wave == 3) {
+      a.tot[b * a.R + lane] = run + sent[3][lane];
+      a.pairs[b * a.R + lane] = pairs[lane];
     }
   }
+  if (tid == 0) a.bad[b] = bad;
+}
+
+// The plan from its counts (one block): wave 0 of a workgroup.
+__device__ inline void write_plan(const SendArgs &a, const int32_t *sent, const int32_t *pairs,
+                                  int bad) {
+  const int lane = threadIdx.x & 63;
+  const int n = lane < a.R ? sent[lane] : 0, at = wave_before(n);
+  if (lane < a.R) {
+    a.plan[lane] = at;
+    a.plan[a.R + 1 + lane] = pairs[lane];
+  }
+  if (lane == a.R - 1) a.plan[a.R] = at + n;
+  if (lane == 0) a.plan[2 * a.R + 1] = bad;
+}
+
+// Per rank (a wave takes every 16th): the block counts become the sums of the
+// blocks before; then the plan.
+__global__ __launch_bounds__(1024) void k_send_scan(SendArgs a) {
+  __shared__ int32_t sent[kMaxRanks], pairs[kMaxRanks], bad;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  for (int r = wave; r < a.R; r += 16) {
+    int run = 0, p = 0;
+    for (int64_t b0 = 0; b0 < a.blocks; b0 += 64) {
+      const bool in = b0 + lane < a.blocks;
+      const int v = in ? a.tot[(b0 + lane) * a.R + r] : 0;
+      p += in ? a.pairs[(b0 + lane) * a.R + r] : 0;
+      const int before = wave_before(v);
+      if (in) a.tot[(b0 + lane) * a.R + r] = run + before;
+      run += __shfl(before + v, 63);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) p += __shfl_xor(p, o);
+    if (lane == 0) {
+      sent[r] = run;
+      pairs[r] = p;
+    }
+  }
+  for (int b = threadIdx.x; b < a.blocks; b += 1024) atomicAdd(&bad, a.bad[b]);
+  __syncthreads();
+  if (wave == 0) write_plan(a, sent, pairs, bad);
+}
+
+// The token's metadata at its places: lane r holds the place in rank r's
+// segment, `go` the ranks it goes to; lanes below k its ids and weights.
+__device__ inline void write_meta(const SendArgs &a, int t, int place, uint64_t go, int id,
+                                  float w) {
+  const int lane = threadIdx.x & 63, r_id = rank_of(a, id);
+  for (uint64_t g = go; g; g &= g - 1) {
+    const int r = __builtin_ctzll(g);
+    const int64_t p = __shfl(place, r);
+    if (lane == 0) a.token[p] = t;
+    if (lane < a.k) {
+      a.out_id[p * a.k + lane] = r_id == r ? id - r * a.per : -1;
+      a.out_w[p * a.k + lane] = r_id == r ? w : 0.f;
+    }
+  }
+}
+
+// A row's 16-byte chunks [c0, c0 + 64 U), U a lane (past the row's last whole
+// chunk the lane reads that one again).
+constexpr int kChunks = 8;
+__device__ inline void load_row(const SendArgs &a, const char *src, int c0, Vec16 (&v)[kChunks]) {
+  const int lane = threadIdx.x & 63, n = (int)(a.row_bytes / 16);
+  if (n == 0) return;
+#pragma unroll
+  for (int u = 0; u < kChunks; ++u)
+    v[u] = *(const Any16 *)(src + (int64_t)min(c0 + u * 64 + lane, n - 1) * 16);
+}
+__device__ inline void store_row(const SendArgs &a, int place, uint64_t go, int c0,
+                                 const Vec16 (&v)[kChunks]) {
+  const int lane = threadIdx.x & 63, n = (int)(a.row_bytes / 16);
+  for (uint64_t g = go; g; g &= g - 1) {
+    char *dst = a.out_x + (int64_t)__shfl(place, __builtin_ctzll(g)) * a.row_bytes;
+#pragma unroll
+    for (int u = 0; u < kChunks; ++u) {
+      const int c = c0 + u * 64 + lane;
+      if (c < n) *(Any16 *)(dst + (int64_t)c * 16) = v[u];
+    }
+  }
+}
+__device__ inline void copy_tail(const SendArgs &a, const char *src, int place, uint64_t go) {
+  const int lane = threadIdx.x & 63, tail = (int)(a.row_bytes % 16);
+  if (!tail) return;  // uniform
+  const int64_t at = a.row_bytes - tail + lane;
+  const char v = lane < tail ? src[at] : 0;
+  for (uint64_t g = go; g; g &= g - 1) {
+    const int64_t p = __shfl(place, __builtin_ctzll(g));  // every lane takes part
+    if (lane < tail) a.out_x[p * a.row_bytes + at] = v;
+  }
+}
+
+// A wave a token.
+__global__ __launch_bounds__(64 * kSendTokens) void k_send(SendArgs a) {
+  __shared__ uint64_t mask[kSendTokens];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t tile = blockIdx.x, t = tile * kSendTokens + wave;
+  const bool live = t < a.rows;
+  const char *src = a.x + (live ? t : 0) * a.ld_x;
+  Vec16 v[kChunks] = {};
+  if (live) load_row(a, src, 0, v);
+  const int id = live && lane < a.k ? a.ids[t * a.k + lane] : -1;
+  const float w = live && lane < a.k ? a.w[t * a.k + lane] : 0.f;
+  int place = 0;
+  if (lane < a.R)
+    place = a.plan[lane] + a.tot[tile / kTiles * a.R + lane] + a.tile_at[tile * a.R + lane];
+  const int r_id = rank_of(a, id);
+  uint64_t go = 0;
+  for (int j = 0; j < a.k; ++j) {
+    const int r = __shfl(r_id, j);
+    if (r >= 0) go |= 1ull << r;
+  }
+  if (lane == 0) mask[wave] = go;
+  __syncthreads();
+  if (!live) return;
+  for (int i = 0; i < wave; ++i) place += (int)((mask[i] >> lane) & 1);
+  write_meta(a, (int)t, place, go, id, w);
+  store_row(a, place, go, 0, v);
+  for (int c0 = 64 * kChunks; c0 < a.row_bytes / 16; c0 += 64 * kChunks) {
+    load_row(a, src, c0, v);
+    store_row(a, place, go, c0, v);
+  }
+  copy_tail(a, src, place, go);
+}
+
+// Up to 256 tokens: workgroup i packs token i, its four waves a share of the
+// row each; thread t counts token t.
+__global__ __launch_bounds__(kFewTokens) void k_send_few(SendArgs a) {
+  __shared__ int32_t sent[4][kMaxRanks], before[4][kMaxRanks], pairs[kMaxRanks], bad;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int token = blockIdx.x;
+  const bool live = token < a.rows;  // a grid of one for no rows
+  const char *src = a.x + (live ? token : 0) * a.ld_x;
+  const int chunks = (int)(a.row_bytes / 16);
+  Vec16 v[kChunks] = {};
+  const int first = wave * 64 * kChunks;
+  if (live) load_row(a, src, first, v);
+  const int id = live && lane < a.k ? a.ids[(int64_t)token * a.k + lane] : -1;
+  const float w = live && lane < a.k ? a.w[(int64_t)token * a.k + lane] : 0.f;
+  if (tid < kMaxRanks) pairs[tid] = 0;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  const uint64_t m = tid < a.rows ? ranks_of(a, tid, pairs, &bad) : 0;
+  int n_sent = 0, n_before = 0;
+  const int rel = token - wave * 64;  // this workgroup's token among the wave's
+  const uint64_t earlier = rel <= 0 ? 0 : rel >= 64 ? ~0ull : (1ull << rel) - 1;
+  for (int r = 0; r < a.R; ++r) {
+    const uint64_t there = __ballot((m >> r) & 1);
+    if (lane == r) {
+      n_sent = (int)__popcll(there);
+      n_before = (int)__popcll(there & earlier);
+    }
+  }
+  sent[wave][lane] = n_sent;
+  before[wave][lane] = n_before;
+  __syncthreads();
+  int all = 0, place = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    all += sent[i][lane];
+    place += before[i][lane];
+  }
+  place += wave_before(all);
+  if (token == 0) {
+    __syncthreads();  // before wave 0 replaces its counts by the sums
+    if (wave == 0) {
+      sent[0][lane] = all;
+      write_plan(a, sent[0], pairs, bad);
+    }
+  }
+  if (!live) return;
+  const int r_id = rank_of(a, id);
+  uint64_t go = 0;
+  for (int j = 0; j < a.k; ++j) {
+    const int r = __shfl(r_id, j);
+    if (r >= 0) go |= 1ull << r;
+  }
+  if (wave == 0) write_meta(a, token, place, go, id, w);
+  store_row(a, place, go, first, v);
+  for (int c0 = first + 4 * 64 * kChunks; c0 < chunks; c0 += 4 * 64 * kChunks) {
+    load_row(a, src, c0, v);
+    store_row(a, place, go, c0, v);
+  }
+  if (wave == 3) copy_tail(a, src, place, go);
 }
 
 const char *bad_desc(const cep_dispatch_desc *d) {
@@ -249,13 +344,14 @@ CEP_API int cep_dispatch(const cep_dispatch_desc *d, const int32_t *topk_id, con
   SendArgs a{topk_id, topk_w, (const char *)x, d->ld_x ? d->ld_x : d->row_bytes, plan, token_idx,
              out_id, out_w, (char *)out_x, ws, ws + (size_t)blocks * kTiles * R,
              ws + (size_t)blocks * (kTiles + 1) * R, ws + (size_t)blocks * (kTiles + 2) * R,
-             d->rows, d->top_k, R, d->experts_per_rank, blocks, d->capacity, d->row_bytes};
-  const dim3 grid(std::max(1, (d->rows + kSendTokens - 1) / kSendTokens));
-  if (blocks <= 1) {
-    hipLaunchKernelGGL(k_send<true>, grid, dim3(256), 0, s, a);
+             d->rows, d->top_k, R, d->experts_per_rank, blocks, d->row_bytes};
+  if (d->rows <= kFewTokens) {
+    hipLaunchKernelGGL(k_send_few, dim3(std::max(1, d->rows)), dim3(kFewTokens), 0, s, a);
   } else {
-    hipLaunchKernelGGL(k_send_count, dim3(blocks), dim3(64), 0, s, a);
-    hipLaunchKernelGGL(k_send<false>, grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_send_count, dim3(blocks), dim3(kCountTokens), 0, s, a);
+    hipLaunchKernelGGL(k_send_scan, dim3(1), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL(k_send, dim3((d->rows + kSendTokens - 1) / kSendTokens),
+                       dim3(64 * kSendTokens), 0, s, a);
   }
   return launched(fn);
 }

@@ -102,17 +102,18 @@ __device__ inline void sort_desc(double (&v)[N]) {
   }
 }
 
+// NaN: as masked; +inf: the largest number
+__device__ inline float unmasked(float l) { return l != l ? -INFINITY : fminf(l, FLT_MAX); }
 __device__ inline float logit(const GateArgs &a, int64_t row, int e) {
-  const float l = a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
-                                      : ((const float *)a.logits)[row * a.ld + e];
-  // NaN: as masked; +inf: the largest number
-  return l != l ? -INFINITY : fminf(l, FLT_MAX);
+  return unmasked(a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
+                                      : ((const float *)a.logits)[row * a.ld + e]);
 }
-__device__ inline float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
+// (the reciprocal instruction is within one unit of the last place)
+__device__ inline float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + expf(-l)); }
 
 // LPR lanes a row, V experts a lane (V a multiple of 4: chunk j of a lane is
 // the four experts from (j * LPR + lane) * 4), at most KM chosen.
-template <int LPR, int V, int KM, bool GROUPS>
+template <int LPR, int V, int KM, bool SIGMOID, bool GROUPS>
 __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
   constexpr int ROWS = 256 / LPR;  // rows of a block
   const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
@@ -123,42 +124,54 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
 #pragma unroll
   for (int j = 0; j < V / 4; ++j) {
     const int e0 = (j * LPR + lane) * 4;
-    float l[4];
-    if (a.dtype == CEP_F32 && e0 + 4 <= a.E) {
-      const Any16 u = *(const Any16 *)((const float *)a.logits + row * a.ld + e0);
+    Vec16 l = {}, b = {};
+    if (e0 + 4 <= a.E) {
+      if (a.dtype == CEP_F32) {
+        l = *(const Any16 *)((const float *)a.logits + row * a.ld + e0);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        l[i] = __uint_as_float(u.v[i]);
-        l[i] = l[i] != l[i] ? -INFINITY : fminf(l[i], FLT_MAX);
+        for (int i = 0; i < 4; ++i)
+          l[i] = (uint32_t)((const uint16_t *)a.logits)[row * a.ld + e0 + i] << 16;
       }
+      if (SIGMOID && a.bias) b = *(const Any16 *)(a.bias + e0);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) l[i] = e0 + i < a.E ? logit(a, row, e0 + i) : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        l[i] = __float_as_uint(e0 + i < a.E ? logit(a, row, e0 + i) : -INFINITY);
+        if (SIGMOID && a.bias && e0 + i < a.E) b[i] = __float_as_uint(a.bias[e0 + i]);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float v = l[i];
-      if (a.sigmoid && v > -INFINITY) {
-        v = sigmoid(v);
-        if (a.bias) {
-          v += a.bias[e0 + i];
-          if (v != v) v = -INFINITY;
-        }
+      const float v = unmasked(__uint_as_float(l[i]));
+      float q = v;
+      if (SIGMOID) {
+        q = sigmoid(v) + __uint_as_float(b[i]);
+        if (v == -INFINITY || q != q) q = -INFINITY;
       }
-      key[4 * j + i] = v;
+      key[4 * j + i] = q;
     }
   }
   if (GROUPS) {
-    __shared__ float keys[ROWS][LPR * V + 1];
-    __shared__ float total[ROWS][kMaxGroups];
-#pragma unroll
-    for (int j = 0; j < V; ++j) keys[sub][(j / 4 * LPR + lane) * 4 + j % 4] = key[j];
-    __syncthreads();
+    // rows 8 words apart modulo the banks, and one word between groups, so that
+    // the lanes of a wave, at the same place of their groups, read 64 banks
+    __shared__ float keys[ROWS][LPR * V + kMaxGroups + 8];
+    __shared__ float total[ROWS][kMaxGroups + 1];
     const int per = a.E / a.groups;
+    const float inv = 1.0f / (float)per;
+    // e / per: exact, the quotient of e + 1/2 lies 1 / (2 per) off a whole number
+    auto group_of = [&](int e) { return (int)(((float)e + 0.5f) * inv); };
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int e = (j / 4 * LPR + lane) * 4 + j % 4;
+      if (e < a.E) keys[sub][e + group_of(e)] = key[j];
+    }
+    __syncthreads();
     for (int g = lane; g < a.groups; g += LPR) {
       float best = -INFINITY, second = -INFINITY;
+#pragma unroll 8
       for (int e = g * per; e < (g + 1) * per; ++e) {
-        const float v = keys[sub][e];
+        const float v = keys[sub][e + g];
         second = fmaxf(second, fminf(best, v));
         best = fmaxf(best, v);
       }
@@ -166,17 +179,20 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
       total[sub][g] = second > -INFINITY ? best + second : best;
     }
     __syncthreads();
-    uint64_t keep = 0;  // this row's kept groups, the same in each of its lanes
-    for (int g = 0; g < a.groups; ++g) {
+    uint64_t keep = 0;  // this row's kept groups
+    for (int g = lane; g < a.groups; g += LPR) {
       const float v = total[sub][g];
       int rank = 0;
+#pragma unroll 8
       for (int h = 0; h < a.groups; ++h) rank += total[sub][h] > v || (total[sub][h] == v && h < g);
       keep |= (uint64_t)(rank < a.topg) << g;
     }
 #pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) keep |= __shfl_xor((unsigned long long)keep, o);
+#pragma unroll
     for (int j = 0; j < V; ++j) {
       const int e = (j / 4 * LPR + lane) * 4 + j % 4;
-      if (e < a.E && !((keep >> (e / per)) & 1)) key[j] = -INFINITY;
+      if (e < a.E && !((keep >> group_of(e)) & 1)) key[j] = -INFINITY;
     }
   }
   double s[V];
@@ -209,10 +225,10 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
     const int r = i * LPR + lane;
     const bool some = r < a.k && key_of(mine[i]) > -INFINITY;
     w[i] = 0.f;
-    if (some) w[i] = a.sigmoid ? sigmoid(logit(a, row, expert_of(mine[i]))) : expf(key_of(mine[i]) - top);
+    if (some) w[i] = SIGMOID ? sigmoid(logit(a, row, expert_of(mine[i]))) : expf(key_of(mine[i]) - top);
     sum += w[i];
   }
-  if (!a.sigmoid && !a.normalize) {
+  if (!SIGMOID && !a.normalize) {
     sum = 0.f;
     for (int e = lane; e < a.E; e += LPR) {
       const float l = logit(a, row, e);
@@ -220,7 +236,7 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
     }
   }
   sum = row_add<LPR>(sum);
-  const bool over = a.normalize || !a.sigmoid;
+  const bool over = a.normalize || !SIGMOID;
 #pragma unroll
   for (int i = 0; i < OWN; ++i) {
     const int r = i * LPR + lane;
@@ -234,15 +250,20 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
 template <int LPR, int V, int KM>
 void launch_gate(const GateArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)a.rows * LPR + 255) / 256));
-  if (a.groups > 1)
-    hipLaunchKernelGGL((k_gate<LPR, V, KM, true>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_gate<LPR, V, KM, false>), grid, dim3(256), 0, s, a);
+  auto *k = !a.sigmoid ? k_gate<LPR, V, KM, false, false>
+            : a.groups > 1 ? k_gate<LPR, V, KM, true, true> : k_gate<LPR, V, KM, true, false>;
+  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
 }
 
+// Few rows: a wave a row, four experts a lane, for the latency of one row;
+// more rows: eight lanes a row, which takes fewer instructions a row.  256
+// experts, k 8, us a call of 64 / 4096 / 8192 / 65536 rows: softmax 3.7 / 5.1 /
+// 7.6 / 42.8 with a wave, 4.0 / 4.4 / 4.4 / 16.1 with eight lanes; sigmoid in
+// eight groups 6.9 / 8.9 / 13.7 / 76.8 and 9.7 / 10.3 / 10.5 / 39.1.
 template <int KM>
 void launch_by_experts(const GateArgs &a, hipStream_t s) {
-  if (a.E <= 64) launch_gate<8, 8, KM>(a, s);
+  if (a.E <= 256 && a.rows <= (a.groups > 1 ? 4096 : 2048)) launch_gate<64, 4, KM>(a, s);
+  else if (a.E <= 64) launch_gate<8, 8, KM>(a, s);
   else if (a.E <= 128) launch_gate<8, 16, KM>(a, s);
   else if (a.E <= 160) launch_gate<8, 20, KM>(a, s);
   else if (a.E <= 256) launch_gate<8, 32, KM>(a, s);

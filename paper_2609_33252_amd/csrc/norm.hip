@@ -123,43 +123,96 @@ struct NormGradArgs {
   float eps;
 };
 
+// Eight values of a row as they are in memory (BF: bf16, else widened).
+template <bool BF>
+struct Raw8 {
+  Vec16 v[BF ? 1 : 2];
+  __device__ void load(const void *row, int dtype, int64_t at, int n) {
+    if (BF && n >= 8) {
+      v[0] = *(const Any16 *)((const char *)row + at * 2);
+      return;
+    }
+    float f[8];
+    load8(row, dtype, at, n, f);
+    if (BF)
+      v[0] = Vec16{bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3]), bf16_pair(f[4], f[5]),
+                   bf16_pair(f[6], f[7])};
+    else
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j / 4][j % 4] = __float_as_uint(f[j]);
+  }
+  __device__ float operator[](int j) const {
+    if (!BF) return __uint_as_float(v[j / 4][j % 4]);
+    const uint32_t u = v[0][j / 2];
+    return __uint_as_float(j % 2 ? u & 0xffff0000u : u << 16);
+  }
+};
+// A row of the backward pass in registers.
+template <bool BF, int NV>
+struct GradRow {
+  Raw8<BF> s[NV], dy[NV], dres[NV];
+};
+
 // Block b takes rows b, b + gridDim.x, ... and keeps its part of dw in
 // registers; the parts are summed in block order by k_rms_norm_dw, so dw does
-// not depend on which block ran first.
-template <int LANES, int NV>
+// not depend on which block ran first.  AHEAD: the next row is loaded while
+// this one's sums meet, and the weight stays in registers.  BF: the rows are all bf16 and are kept so until they
+// are used.
+template <int LANES, int NV, bool BF, bool AHEAD>
 __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
-  __shared__ float lds[2][LANES / 64];
+  __shared__ float lds[2][2][LANES / 64];
   const int lane = threadIdx.x;
-  float dw[NV][8] = {};
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float s[NV][8], dy[NV][8];
-    float sq = 0.f, dot = 0.f;
+  auto load = [&](GradRow<BF, NV> &r, int64_t row) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int c = (u * LANES + lane) * 8;
-      float w[8];
-      load8(a.s, a.s_dtype, row * a.ld_s + c, a.d - c, s[u]);
-      load8(a.dy, a.dy_dtype, row * a.ld_dy + c, a.d - c, dy[u]);
-      load8(a.w, a.w_dtype, c, a.d - c, w);
+      r.s[u].load(a.s, a.s_dtype, row * a.ld_s + c, a.d - c);
+      r.dy[u].load(a.dy, a.dy_dtype, row * a.ld_dy + c, a.d - c);
+      if (AHEAD && a.dres) r.dres[u].load(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c);
+    }
+  };
+  float w[NV][8], dw[NV][8] = {};
+  auto load_w = [&](int u) {
+    const int c = (u * LANES + lane) * 8;
+    load8(a.w, a.w_dtype, c, a.d - c, w[u]);
+  };
+  if (AHEAD)
+#pragma unroll
+    for (int u = 0; u < NV; ++u) load_w(u);
+  GradRow<BF, NV> cur = {}, next = {};
+  if (AHEAD) load(next, blockIdx.x);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    if (AHEAD) {
+      cur = next;
+      if (row + gridDim.x < a.rows) load(next, row + gridDim.x);
+    } else {
+      load(cur, row);
+    }
+    float sq = 0.f, dot = 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      if (!AHEAD) load_w(u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        sq = fmaf(s[u][j], s[u][j], sq);
-        dot = fmaf(dy[u][j] * w[j], s[u][j], dot);
+        sq = fmaf(cur.s[u][j], cur.s[u][j], sq);
+        dot = fmaf(cur.dy[u][j] * w[u][j], cur.s[u][j], dot);
       }
     }
     sq = wave_sum(sq);
     dot = wave_sum(dot);
-    __syncthreads();  // the row before has read its sums
-    if ((lane & 63) == 0) {
-      lds[0][lane >> 6] = sq;
-      lds[1][lane >> 6] = dot;
-    }
-    __syncthreads();
-    sq = dot = 0.f;
+    if (LANES > 64) {  // two places in turn: one barrier a row
+      if ((lane & 63) == 0) {
+        lds[turn][0][lane >> 6] = sq;
+        lds[turn][1][lane >> 6] = dot;
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      sq = dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < LANES / 64; ++i) {
-      sq += lds[0][i];
-      dot += lds[1][i];
+      for (int i = 0; i < LANES / 64; ++i) {
+        sq += lds[turn][0][i];
+        dot += lds[turn][1][i];
+      }
     }
     const float inv = 1.0f / sqrtf(sq / (float)a.d + a.eps);
     const float mean = dot * inv / (float)a.d;  // of a * n
@@ -167,14 +220,17 @@ __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
     for (int u = 0; u < NV; ++u) {
       const int c = (u * LANES + lane) * 8;
       if (c >= a.d) continue;
-      float w[8], dx[8], dres[8] = {};
-      load8(a.w, a.w_dtype, c, a.d - c, w);
-      if (a.dres) load8(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c, dres);
+      float dx[8];
+      if (!AHEAD) {
+        asm volatile("" ::: "memory");  // not kept from the sums above
+        load_w(u);
+        if (a.dres) cur.dres[u].load(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = s[u][j] * inv;
-        dx[j] = inv * (dy[u][j] * w[j] - n * mean) + dres[j];
-        dw[u][j] = fmaf(dy[u][j], n, dw[u][j]);
+        const float n = cur.s[u][j] * inv;
+        dx[j] = inv * (cur.dy[u][j] * w[u][j] - n * mean) + cur.dres[u][j];
+        dw[u][j] = fmaf(cur.dy[u][j], n, dw[u][j]);
       }
       store8(a.dx, a.dx_dtype, row * a.ld_dx + c, a.d - c, dx);
     }
@@ -186,20 +242,22 @@ __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
   }
 }
 
-// dw: 32 columns a block, eight strands of the parts each, summed in a fixed
+// dw: 64 columns a block, 16 strands of the parts each, summed in a fixed
 // order.
-__global__ __launch_bounds__(256) void k_rms_norm_dw(const float *part, int n, int d, int w_dtype,
-                                                     void *dw) {
-  __shared__ float lds[8][32];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), strand = threadIdx.x >> 5;
+__global__ __launch_bounds__(1024) void k_rms_norm_dw(const float *part, int n, int d, int w_dtype,
+                                                      void *dw) {
+  __shared__ float lds[16][64];
+  const int col = blockIdx.x * 64 + (threadIdx.x & 63), strand = threadIdx.x >> 6;
   float v = 0.f;
-  if (col < d)
-    for (int i = strand; i < n; i += 8) v += part[(size_t)i * d + col];
-  lds[strand][threadIdx.x & 31] = v;
+  if (col < d) {
+#pragma unroll 8
+    for (int i = strand; i < n; i += 16) v += part[(size_t)i * d + col];
+  }
+  lds[strand][threadIdx.x & 63] = v;
   __syncthreads();
   if (strand == 0 && col < d) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += lds[i][threadIdx.x];
+    for (int i = 1; i < 16; ++i) v += lds[i][threadIdx.x];
     if (w_dtype == CEP_BF16) ((__bf16 *)dw)[col] = (__bf16)v;
     else ((float *)dw)[col] = v;
   }
@@ -220,7 +278,27 @@ void by_width(int d, F f) {
   else f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
 }
 
-int grad_blocks(int rows) { return std::min(rows, 1024); }
+// Blocks of the backward pass: the most that run at once are two a compute
+// unit (512), and each writes a part of dw.
+int grad_blocks(int rows) { return std::min(rows, 512); }
+
+// Threads and groups of the backward pass, which keeps three rows, the weight
+// and dw: float32 rows, and ones past 8192 channels, are not loaded ahead (the
+// registers of two rows would not hold four waves a unit).
+template <class F>
+void by_width_grad(int d, bool bf, F f) {
+  using std::integral_constant;
+  auto with = [&](auto lanes, auto nv, auto ahead) {
+    if (bf) f(lanes, nv, std::true_type{}, ahead);
+    else f(lanes, nv, std::false_type{}, std::false_type{});
+  };
+  if (d <= 512) with(integral_constant<int, 64>{}, integral_constant<int, 1>{}, std::true_type{});
+  else if (d <= 2048) with(integral_constant<int, 256>{}, integral_constant<int, 1>{}, std::true_type{});
+  else if (d <= 4096) with(integral_constant<int, 512>{}, integral_constant<int, 1>{}, std::true_type{});
+  else if (d <= 8192) with(integral_constant<int, 512>{}, integral_constant<int, 2>{}, std::true_type{});
+  else if (d <= 16384) with(integral_constant<int, 1024>{}, integral_constant<int, 2>{}, std::false_type{});
+  else with(integral_constant<int, 1024>{}, integral_constant<int, 4>{}, std::false_type{});
+}
 
 // nullptr, or what is wrong with a descriptor
 const char *bad_desc(const cep_norm_desc *n) {
@@ -299,11 +377,15 @@ CEP_API int cep_rms_norm_backward(const cep_norm_desc *n, const void *x, const v
                        stride_of(n->ld_y, n->d), stride_of(n->ld_res, n->d), n->rows, n->d,
                        n->x_dtype, n->res_dtype, n->w_dtype, n->y_dtype, n->eps};
   if (blocks)
-    by_width(n->d, [&](auto lanes, auto nv) {
-      constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
-      hipLaunchKernelGGL((k_rms_norm_grad<L, NV>), dim3(blocks), dim3(L), 0, s, a);
-    });
-  hipLaunchKernelGGL(k_rms_norm_dw, dim3((n->d + 31) / 32), dim3(256), 0, s, a.part, blocks, n->d,
+    by_width_grad(n->d, n->x_dtype == CEP_BF16 && n->y_dtype == CEP_BF16 &&
+                            (!dres || n->res_dtype == CEP_BF16),
+                  [&](auto lanes, auto nv, auto bf, auto ahead) {
+                    constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
+                    hipLaunchKernelGGL(
+                        (k_rms_norm_grad<L, NV, decltype(bf)::value, decltype(ahead)::value>),
+                        dim3(blocks), dim3(L), 0, s, a);
+                  });
+  hipLaunchKernelGGL(k_rms_norm_dw, dim3((n->d + 63) / 64), dim3(1024), 0, s, a.part, blocks, n->d,
                      n->w_dtype, dw);
   return launched(fn);
 }

@@ -111,12 +111,12 @@ __device__ inline const char *uniform(const char *p) {
 // each, in which a wave multiplies HALF/WM x HALF/WN outputs (16 matrix
 // instructions in the larger tiles).  Quadrants follow a snake (A0 B0, A0 B1, A1 B1,
 // A1 B0, then B swapped in the next step), so that only one operand half
-// changes from phase to phase.  A half of A is read into the registers of the
-// one before as soon as their last matrix instruction has issued, a half of B
-// one phase ahead; a phase also loads one half, four to five phases ahead of
-// its use.  A barrier ends each phase: behind it, the loads the next phase
-// reads have landed in every wave, and the halves read in the phase before
-// have been consumed and may be refilled.
+// changes from phase to phase.  Fragments are read at least half a phase ahead
+// and spread over the phases (LDS reads fill three quarters of the time that
+// the matrix instructions take); a phase also loads one half, three to five
+// phases ahead of its use.  A barrier ends each phase: behind it, the loads the
+// next phase reads have landed in every wave, and the halves read in the phase
+// before have been consumed and may be refilled.
 //
 // LDS layout of a half, in 16-byte chunks so that every fragment read spreads
 // over all banks:
@@ -131,10 +131,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
   constexpr bool DUAL = is_dual(EPI);
   constexpr int MF = HALF / 16 / WM, NF = HALF / 16 / WN;  // fragments of a wave in a half
   constexpr int HB = HALF * 128;                           // bytes of a half
-  constexpr int STAGE = 4 * HB;                            // A0, A1, B0, B1
+  constexpr int STAGE = 2 * HB;                            // one operand's two halves
   constexpr int LOADS = HB / 1024 / (WM * WN);             // 1 KB loads of a wave of a half
   constexpr int TN = DUAL ? HALF : 2 * HALF;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * STAGE];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l15 = lane & 15, g4 = lane >> 4;
   const int wm = wave % WM, wn = wave / WM;
@@ -183,18 +183,21 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
     return ((DUAL ? half : seg) ? baseB1 : baseB0) + step * stepB;
   };
   const uint32_t lds0 = lds_offset(lds);
-  // half `which` (0 A0, 1 first B, 2 second B, 3 A1) of the share's step s,
-  // whose parity is P; the first B half is half P
-  auto issue = [&](int s, auto which, auto parity) {
+  // piece e of half `which` (0 A0, 1 first B, 2 second B, 3 A1) of the share's
+  // step s, whose parity is P; the first B half is half P
+  auto issue = [&](int s, auto which, auto parity, int e) {
     constexpr int W = decltype(which)::value, P = decltype(parity)::value;
     constexpr bool IS_A = W == 0 || W == 3;
     constexpr int H = W == 0 ? 0 : W == 3 ? 1 : W == 1 ? P : 1 - P;
     const int from = s0 + min(s, S - 1);
     const int seg = from >= full ? 1 : 0, step = from - (seg ? full : 0);
     const char *src = uniform(IS_A ? ptrA(seg, step) : ptrB(H, seg, step));
-    const uint32_t to = lds0 + P * STAGE + (IS_A ? H : 2 + H) * HB + wave * LOADS * 1024;
+    const uint32_t to = lds0 + (IS_A ? P : 2 + P) * STAGE + H * HB + wave * LOADS * 1024;
+    dma16_s(src, IS_A ? offA[H][e] : offB[H][e], to + e * 1024);
+  };
+  auto issue_half = [&](int s, auto which, auto parity) {
 #pragma unroll
-    for (int e = 0; e < LOADS; ++e) dma16_s(src, IS_A ? offA[H][e] : offB[H][e], to + e * 1024);
+    for (int e = 0; e < LOADS; ++e) issue(s, which, parity, e);
   };
 
   // ---- fragments
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
 #pragma unroll
   for (int i = 0; i < (A_K ? 2 : MF); ++i) ra[i] = place(A_K, wm * MF * 16, i);
 #pragma unroll
-  for (int i = 0; i < (B_K ? 2 : NF); ++i) rb[i] = place(B_K, wn * NF * 16, i);
+  for (int i = 0; i < (B_K ? 2 : NF); ++i) rb[i] = 2 * STAGE + place(B_K, wn * NF * 16, i);
   auto read = [&](bool kc, const int *r, int base, int i, int ks) {
     if (kc) return *(const bf16x8 *)(lds + r[ks] + (base + i * 2048));
     union { bf16x8 v; bf16x4 h[2]; } o;
@@ -221,33 +224,24 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
                                                         (base + (ks * 32 + h * 4) * HALF * 2)));
     return o.v;
   };
-  bf16x8 fa[MF][2], fb[2][NF][2];
+  // Fragments: of A three sets of a half's 32 of k, taken in turn by the pieces
+  // A0 (first and second 32 of k), A1, A0 of the next step, ...; of B two halves.
+  bf16x8 fa[3][MF], fb[2][NF][2];
   f32x4 acc[2][2][MF][NF] = {};
-  auto read_a = [&](int half, int stage, int ks) {
-#pragma unroll
-    for (int i = 0; i < MF; ++i)
-      fa[i][ks] = read(A_K, ra, stage * STAGE + half * HB, i, ks);
+  auto read_a = [&](auto set, int half, int stage, int ks, int i) {
+    fa[decltype(set)::value][i] = read(A_K, ra, stage * STAGE + half * HB, i, ks);
   };
-  auto read_b = [&](auto half, int stage) {
+  auto read_b = [&](auto half, int stage, int item) {  // item: fragment and 32 of k
     constexpr int H = decltype(half)::value;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int j = 0; j < NF; ++j)
-        fb[H][j][ks] = read(B_K, rb, stage * STAGE + (2 + H) * HB, j, ks);
+    fb[H][item % NF][item / NF] = read(B_K, rb, stage * STAGE + H * HB, item % NF, item / NF);
   };
-  // half of a quadrant's products
-  auto mul = [&](auto mh, auto nh, int ks) {
-    constexpr int P = decltype(mh)::value, Q = decltype(nh)::value;
-    __builtin_amdgcn_s_setprio(1);
+  // the products of one fragment of A in a quadrant
+  auto mul = [&](auto mh, auto nh, auto set, int ks, int i) {
+    constexpr int P = decltype(mh)::value, Q = decltype(nh)::value, Z = decltype(set)::value;
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
-#pragma unroll
-      for (int j = 0; j < NF; ++j)
-        acc[P][Q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[Q][j][ks], fa[i][ks],
-                                                                  acc[P][Q][i][j], 0, 0, 0);
-    __builtin_amdgcn_s_setprio(0);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int j = 0; j < NF; ++j)
+      acc[P][Q][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[Q][j][ks], fa[Z][i],
+                                                                acc[P][Q][i][j], 0, 0, 0);
   };
   using I0 = std::integral_constant<int, 0>;
   using I1 = std::integral_constant<int, 1>;
@@ -256,53 +250,82 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
   auto sync = [&] { asm volatile("s_barrier" ::: "memory"); };
   // Halves are loaded in the order A0, first B, second B, A1 of each step;
   // phase n (four a step) loads half n + 7, and the phase after it reads up
-  // to half n + 3.  Past the last step the loads repeat it, unread, so that
-  // the count in flight stays the same.
-  auto phase = [&](int t, auto phase_c, auto parity_c) {
-    constexpr int Q = decltype(phase_c)::value, P = decltype(parity_c)::value;
+  // to half n + 4.  Past the last step the loads repeat it, unread, so that
+  // the count in flight stays the same.  TURN: the step modulo 6, the period
+  // of the stages and the fragment sets.
+  auto phase = [&](int t, auto phase_c, auto turn_c) {
+    constexpr int Q = decltype(phase_c)::value, TURN = decltype(turn_c)::value, P = TURN % 2;
     using M = std::integral_constant<int, Q / 2>;
     using G = std::integral_constant<int, 1 - P>;  // this step's second B half, the next one's first
     using N = std::integral_constant<int, Q == 0 || Q == 3 ? P : 1 - P>;
-    if (Q == 0) read_b(G{}, P);
-    if (Q == 3) read_b(G{}, 1 - P);
-    issue(t + (Q == 0 ? 1 : 2), std::integral_constant<int, (Q + 3) % 4>{},
-          std::integral_constant<int, Q == 0 ? 1 - P : P>{});
-    __builtin_amdgcn_sched_barrier(0);
+    using Z0 = std::integral_constant<int, (TURN + Q / 2 * 2) % 3>;      // this half's sets
+    using Z1 = std::integral_constant<int, (TURN + Q / 2 * 2 + 1) % 3>;
+    using Z2 = std::integral_constant<int, (TURN + Q / 2 * 2 + 2) % 3>;  // the free one
+    const int to = t + (Q == 0 ? 1 : 2);
+    using W = std::integral_constant<int, (Q + 3) % 4>;
+    using TO = std::integral_constant<int, Q == 0 ? 1 - P : P>;
+    // The reads and loads are dealt out between the matrix instructions: at the
+    // head of the phase they would hold up the instructions behind them for as
+    // long as the LDS queue is full.
+    constexpr int NG = 2 * MF, NB = 2 * NF;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      mul(M{}, N{}, ks);
-      if (Q == 1) read_a(1, P, ks);
-      if (Q == 3) read_a(0, 1 - P, ks);
+    for (int g = 0; g < NG; ++g) {
+      if (g < MF) mul(M{}, N{}, Z0{}, 0, g);
+      else mul(M{}, N{}, Z1{}, 1, g - MF);
+      if (Q == 0 || Q == 3) {
+#pragma unroll
+        for (int r = 0; r < NB; ++r)
+          if (r * MF / NB == g) read_b(G{}, Q == 0 ? P : 1 - P, r);
+        if (Q == 0 && g >= MF) read_a(Z2{}, 1, P, 0, g - MF);
+        if (Q == 3 && g >= MF) read_a(Z0{}, 0, 1 - P, 1, g - MF);
+      }
+      if (Q == 1 && g % 2 == 1) read_a(Z0{}, 1, P, 1, g / 2);
+      if (Q == 2 && g % 2 == 1) read_a(Z2{}, 0, 1 - P, 0, g / 2);
+#pragma unroll
+      for (int e = 0; e < LOADS; ++e)
+        if ((2 * e + 1) * NG / (2 * LOADS) == g) issue(to, W{}, TO{}, e);
       __builtin_amdgcn_sched_barrier(0);
     }
-    wait_vmcnt<4 * LOADS>();
+    wait_vmcnt<3 * LOADS>();
     sync();
   };
-  auto whole_step = [&](int t, auto parity) {
-    phase(t, I0{}, parity);
-    phase(t, I1{}, parity);
-    phase(t, I2{}, parity);
-    phase(t, I3{}, parity);
+  auto whole_step = [&](int t, auto turn) {
+    phase(t, I0{}, turn);
+    phase(t, I1{}, turn);
+    phase(t, I2{}, turn);
+    phase(t, I3{}, turn);
   };
   if (S > 0) {
-    issue(0, I0{}, I0{});
-    issue(0, I1{}, I0{});
-    issue(0, I2{}, I0{});
-    issue(0, I3{}, I0{});
-    issue(1, I0{}, I1{});
-    issue(1, I1{}, I1{});
-    issue(1, I2{}, I1{});
+    issue_half(0, I0{}, I0{});
+    issue_half(0, I1{}, I0{});
+    issue_half(0, I2{}, I0{});
+    issue_half(0, I3{}, I0{});
+    issue_half(1, I0{}, I1{});
+    issue_half(1, I1{}, I1{});
+    issue_half(1, I2{}, I1{});
     wait_vmcnt<5 * LOADS>();
     sync();
-    read_a(0, 0, 0);
-    read_a(0, 0, 1);
-    read_b(I0{}, 0);
-    wait_vmcnt<4 * LOADS>();
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      read_a(I0{}, 0, 0, 0, i);
+      read_a(I1{}, 0, 0, 1, i);
+    }
+#pragma unroll
+    for (int r = 0; r < 2 * NF; ++r) read_b(I0{}, 0, r);
+    wait_vmcnt<3 * LOADS>();
     sync();
     for (int t = 0;;) {
       whole_step(t, I0{});
       if (++t == S) break;
       whole_step(t, I1{});
+      if (++t == S) break;
+      whole_step(t, I2{});
+      if (++t == S) break;
+      whole_step(t, I3{});
+      if (++t == S) break;
+      whole_step(t, std::integral_constant<int, 4>{});
+      if (++t == S) break;
+      whole_step(t, std::integral_constant<int, 5>{});
       if (++t == S) break;
     }
     wait_vmcnt<0>();
@@ -321,20 +344,25 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
 #pragma unroll
         for (int e = 0; e < LOADS; ++e) {
           piece_in(A_K, wave * LOADS + e, ptrA(seg, full) + offA[h][e], h);
-          piece_in(B_K, wave * LOADS + e, ptrB(h, seg, full) + offB[h][e], 2 + h);
+          piece_in(B_K, wave * LOADS + e, ptrB(h, seg, full) + offB[h][e], 4 + h);
         }
       __syncthreads();
-      read_b(I0{}, 0);
-      read_b(I1{}, 0);
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        read_a(0, 0, ks);
-        mul(I0{}, I0{}, ks);
-        mul(I0{}, I1{}, ks);
-        read_a(1, 0, ks);
-        mul(I1{}, I0{}, ks);
-        mul(I1{}, I1{}, ks);
+      for (int r = 0; r < 2 * NF; ++r) {
+        read_b(I0{}, 0, r);
+        read_b(I1{}, 0, r);
       }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < MF; ++i) {
+          read_a(I0{}, 0, 0, ks, i);
+          read_a(I1{}, 1, 0, ks, i);
+          mul(I0{}, I0{}, I0{}, ks, i);
+          mul(I0{}, I1{}, I0{}, ks, i);
+          mul(I1{}, I0{}, I1{}, ks, i);
+          mul(I1{}, I1{}, I1{}, ks, i);
+        }
       __syncthreads();
     }
   }

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
   auto sync = [&] { asm volatile("s_barrier" ::: "memory"); };
   // Halves are loaded in the order A0, first B, second B, A1 of each step;
   // phase n (four a step) loads half n + 7, and the phase after it reads up
-  // to half n + 4.  Past the last step the loads repeat it, unread, so that
+  // to half n + 3 (n + 4 after a step's last phase).  Past the last step the loads repeat it, unread, so that
   // the count in flight stays the same.  TURN: the step modulo 6, the period
   // of the stages and the fragment sets.
   auto phase = [&](int t, auto phase_c, auto turn_c) {
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
         if ((2 * e + 1) * NG / (2 * LOADS) == g) issue(to, W{}, TO{}, e);
       __builtin_amdgcn_sched_barrier(0);
     }
-    wait_vmcnt<3 * LOADS>();
+    wait_vmcnt<(Q == 3 ? 3 : 4) * LOADS>();
     sync();
   };
   auto whole_step = [&](int t, auto turn) {
@@ -402,23 +402,40 @@ int64_t dense_tiles(int t, int M, int N) {
   return (int64_t)((M + kTile[t] - 1) / kTile[t]) * ((N + kTile[t] - 1) / kTile[t]);
 }
 
-// Time of a K step over all tiles, in us: 1.5 a round of 256-wide tiles, one a
-// compute unit; of 128-wide ones 1.0 with two a unit (512 in a round), 0.6 with
-// one.  (A 256 x 128 tile, in four or eight waves, was no faster than two
-// 128-wide ones: 4095 x 2048 x 4096 118 and 108 us against 104.)
-//
-// Few tiles share K until 256 workgroups run, while a share keeps six steps and
-// the steps saved outweigh the second launch (4096-wide products of 65 rows: 54
-// us whole, 27.4 in six shares, 37.7 in 16; of 512 rows, 128 tiles: 54.8 whole,
-// 47.7 in two, 55.1 in three).
+// Tile and shares by an estimate of the time, in us, from these measurements
+// (a product alone, steps of 64 of K):
+//   256-wide tiles, one a compute unit: 12 and 1.4 a step, a round of up to 256
+//     (777 x 5120 x 6144, 80 tiles: in two shares 71, in three 57)
+//   128-wide ones: 3 and a step of 0.55 with one a unit (777 x 4096 x 4096, 224
+//     tiles: 37), 0.85 to 1.0 with two (280 tiles of 96 steps 84, 512 tiles of
+//     64 steps 64), 1.2 a round of several (1024 tiles of 64 steps 146)
+//   the shares' second launch: 4, and their sums at 9 TB/s (three of 777 x 5120: 9)
+// Shares have six steps at least and fit one round; they have to win by a tenth.
+// (A 256 x 128 tile, in four or eight waves, was no faster than two 128-wide
+// ones: 4095 x 2048 x 4096 118 and 108 against 104.)
 DensePlan dense_plan(int M, int n, int K, bool dual) {
   const int N = dual ? 2 * n : n, steps = K / 64;
-  const int64_t n0 = dense_tiles(0, M, N), n1 = dense_tiles(1, M, N), rest = n1 % 512;
-  const double t0 = 1.5 * ((n0 + 255) / 256);
-  const double t1 = 1.0 * (n1 / 512) + (rest == 0 ? 0.0 : rest <= 256 ? 0.6 : 1.0);
-  if (t0 < t1) return {0, 1};
-  const int splits = (int)std::min<int64_t>(n1 ? 256 / n1 : 1, steps / 6);
-  return {1, splits > 1 && steps - steps / splits >= 10 ? splits : 1};
+  DensePlan best{1, 1};
+  double least = 0;
+  for (int t = 0; t < 2; ++t) {
+    const int64_t tiles = dense_tiles(t, M, N);
+    for (int s = 1; s <= 16; ++s) {
+      if (s > 1 && (tiles * s > 256 || steps / s < 6)) break;
+      const int64_t items = tiles * s, rest = items % 512;
+      const double step = (double)steps / s;
+      double us = t == 0 ? (double)((items + 255) / 256) * (12 + 1.4 * step)
+                         : 3 + step * ((items > 512 ? 1.2 : 1.0) * (double)(items / 512) +
+                                       (rest == 0     ? 0.0
+                                        : rest <= 256 ? 0.55
+                                                      : 0.85 + 0.15 * (double)(rest - 256) / 256));
+      if (s > 1) us = (us + 4 + (double)s * M * N * 4 / 9e6) / 0.9;
+      if ((t == 0 && s == 1) || us < least) {
+        best = {t, s};
+        least = us;
+      }
+    }
+  }
+  return best;
 }
 
 // Scratch of a product's shares.

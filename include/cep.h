@@ -365,7 +365,7 @@ int cep_ffn_noalloc(cep_ctx *ctx, int replica, int n_rows, int n_pairs, const in
 size_t cep_row_bytes(int d, int x_dtype);
 
 typedef struct {
-  int rows;               /* 0..2^24                                          */
+  int rows;               /* 0..2^21                                          */
   int d;                  /* 1..32768; a multiple of 32 for MXFP8 output      */
   int x_dtype, res_dtype, w_dtype, y_dtype; /* CEP_F32 or CEP_BF16            */
   float eps;
@@ -404,7 +404,7 @@ enum cep_score {
 };
 
 typedef struct {
-  int rows;            /* 0..2^24                                             */
+  int rows;            /* 0..2^21                                             */
   int n_experts;       /* 1..1024                                             */
   int top_k;           /* 1..16, at most n_experts                            */
   int logit_dtype;     /* CEP_F32 or CEP_BF16                                 */
@@ -429,7 +429,7 @@ int cep_gate_topk(const cep_gate_desc *desc, const void *logits, const float *bi
                   int32_t *topk_id, float *topk_w, hipStream_t s);
 
 typedef struct {
-  int rows;              /* 0..2^24                                           */
+  int rows;              /* 0..2^21                                           */
   int top_k;             /* 1..16                                             */
   int n_ranks;           /* 1..64; rank r holds experts                       */
   int experts_per_rank;  /*   [r, r + 1) * experts_per_rank                   */
@@ -454,7 +454,7 @@ int cep_dispatch(const cep_dispatch_desc *desc, const int32_t *topk_id, const fl
                  void *out_x, void *workspace, size_t workspace_bytes, hipStream_t s);
 
 typedef struct {
-  int rows;              /* 0..2^24                                           */
+  int rows;              /* 0..2^21                                           */
   int d_model, d_ff;     /* multiples of 8, 8..32768                          */
   int64_t ld_x;          /* row strides in elements, multiples of 8, up to    */
   int64_t ld_y;          /*   2^21: x; y and dy;                              */

@@ -13,8 +13,9 @@
 
 namespace cep {
 
-// largest row count of the operators' descriptors
-constexpr int kMaxOpRows = 1 << 24;
+// largest row count of the operators' descriptors (a launch holds fewer than
+// 2^32 threads, and a row takes up to 1024)
+constexpr int kMaxOpRows = 1 << 21;
 
 // Records the message of a refused or failed call (cep_last_error(NULL)).
 __attribute__((format(printf, 2, 3))) inline int refuse(int code, const char *fmt, ...) {

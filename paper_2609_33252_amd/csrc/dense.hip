@@ -466,7 +466,7 @@ constexpr int64_t kMaxStride = 1 << 21;
 
 const char *bad_desc(const cep_gated_ffn_desc *d) {
   if (!d) return "desc is NULL";
-  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^24";
+  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^21";
   for (int w : {d->d_model, d->d_ff})
     if (w < 8 || w > kMaxDim || w % 8) return "d_model and d_ff must be multiples of 8, up to 32768";
   for (int64_t ld : {d->ld_x, d->ld_y, d->ld_dx})

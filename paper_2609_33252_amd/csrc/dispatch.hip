@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kFewTokens) void k_send_few(SendArgs a) {
 
 const char *bad_desc(const cep_dispatch_desc *d) {
   if (!d) return "desc is NULL";
-  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^24";
+  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^21";
   if (d->top_k < 1 || d->top_k > kMaxTopK) return "top_k must be in 1..16";
   if (d->n_ranks < 1 || d->n_ranks > kMaxRanks) return "n_ranks must be in 1..64";
   if (d->experts_per_rank < 1 || d->experts_per_rank > 1 << 20)

@@ -280,7 +280,7 @@ CEP_API int cep_gate_topk(const cep_gate_desc *g, const void *logits, const floa
                           int32_t *topk_id, float *topk_w, hipStream_t s) {
   const char *fn = "cep_gate_topk";
   if (!g) return refuse(CEP_EINVAL, "%s: desc is NULL", fn);
-  if (g->rows < 0 || g->rows > kMaxOpRows) return refuse(CEP_EINVAL, "%s: rows must be in 0..2^24", fn);
+  if (g->rows < 0 || g->rows > kMaxOpRows) return refuse(CEP_EINVAL, "%s: rows must be in 0..2^21", fn);
   if (g->n_experts < 1 || g->n_experts > kMaxGateExperts)
     return refuse(CEP_EINVAL, "%s: n_experts must be in 1..1024", fn);
   if (g->top_k < 1 || g->top_k > kMaxTopK || g->top_k > g->n_experts)

@@ -66,31 +66,34 @@ __device__ inline uint2 mxfp8_block(const float v[8], int *code) {
   return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
 }
 
-// LANES threads a row, NV groups of eight channels each.
+// LANES threads a row, NV groups of eight channels each.  With one group of
+// 1024 threads (a few rows) the weight is loaded before the sum, so that the row
+// waits for memory once; elsewhere the registers are worth more as waves (8192
+// rows of 7168: 109 us, 114 with the weight ahead).
 template <int LANES, int NV>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs a) {
+  constexpr bool AHEAD = LANES == 1024 && NV == 1;
   __shared__ float lds[LANES > 64 ? LANES / 64 : 1];
   const int lane = threadIdx.x % LANES;
   const int row = LANES < 256 ? blockIdx.x * (256 / LANES) + threadIdx.x / LANES : blockIdx.x;
   if (row >= a.rows) return;  // uniform over the row's threads
-  float s[NV][8];
-  float sq = 0.f;
+  auto col = [&](int u) { return (u * LANES + lane) * 8; };
+  float s[NV][8], ahead[8];
 #pragma unroll
-  for (int u = 0; u < NV; ++u) {
-    const int c = (u * LANES + lane) * 8;
-    load8(a.x, a.x_dtype, row * a.ld_x + c, a.d - c, s[u]);
-  }
+  for (int u = 0; u < NV; ++u) load8(a.x, a.x_dtype, row * a.ld_x + col(u), a.d - col(u), s[u]);
+  if (AHEAD) load8(a.w, a.w_dtype, col(0), a.d - col(0), ahead);
   if (a.res) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (u * LANES + lane) * 8;
       float r[8];
-      load8(a.res, a.res_dtype, row * a.ld_res + c, a.d - c, r);
+      load8(a.res, a.res_dtype, row * a.ld_res + col(u), a.d - col(u), r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[u][j] += r[j];
-      if (a.res_out) store8(a.res_out, a.res_dtype, row * a.ld_res + c, a.d - c, s[u]);
+      if (a.res_out)
+        store8(a.res_out, a.res_dtype, row * a.ld_res + col(u), a.d - col(u), s[u]);
     }
   }
+  float sq = 0.f;
 #pragma unroll
   for (int u = 0; u < NV; ++u)
 #pragma unroll
@@ -98,12 +101,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_rms_norm(NormArgs
   const float inv = 1.0f / sqrtf(row_sum<LANES>(sq, lds) / (float)a.d + a.eps);
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    const int c = (u * LANES + lane) * 8;
+    const int c = col(u);
     if (c >= a.d) continue;
     float w[8], y[8];
-    load8(a.w, a.w_dtype, c, a.d - c, w);
+    if (!AHEAD) load8(a.w, a.w_dtype, c, a.d - c, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = s[u][j] * inv * w[j];
+    for (int j = 0; j < 8; ++j) y[j] = s[u][j] * inv * (AHEAD ? ahead[j] : w[j]);
     if (a.y) store8(a.y, a.y_dtype, row * a.ld_y + c, a.d - c, y);
     if (a.codes) {  // d is a multiple of 32: whole blocks
       int code;
@@ -264,14 +267,18 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dw(const float *part, int n, 
 }
 
 // Calls f with the threads a row takes and the groups of eight channels each
-// of them holds: a wave up to 1024 channels (no barrier), else 256 threads, or
-// 1024 for the widest rows.
+// of them holds: a wave up to 1024 channels (no barrier), else 256 threads.
+// Rows beyond 8192 channels take 1024, as do up to 256 rows, one workgroup a
+// compute unit (7168 channels, one row 6.3 us with 256 threads, 4.6 with 1024;
+// 256 rows 8.4 and 5.9).
 template <class F>
-void by_width(int d, F f) {
+void by_width(int d, int rows, F f) {
   using std::integral_constant;
+  const bool few = rows <= 256;
   if (d <= 512) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   else if (d <= 1024) f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   else if (d <= 2048) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  else if (d <= 8192 && few) f(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
   else if (d <= 4096) f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (d <= 8192) f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   else if (d <= 16384) f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
@@ -303,7 +310,7 @@ void by_width_grad(int d, bool bf, F f) {
 // nullptr, or what is wrong with a descriptor
 const char *bad_desc(const cep_norm_desc *n) {
   if (!n) return "desc is NULL";
-  if (n->rows < 0 || n->rows > kMaxOpRows) return "rows must be in 0..2^24";
+  if (n->rows < 0 || n->rows > kMaxOpRows) return "rows must be in 0..2^21";
   if (n->d < 1 || n->d > kMaxDim) return "d must be in 1..32768";
   if (!is_float_dtype(n->x_dtype) || !is_float_dtype(n->res_dtype) ||
       !is_float_dtype(n->w_dtype) || !is_float_dtype(n->y_dtype))
@@ -344,7 +351,7 @@ CEP_API int cep_rms_norm(const cep_norm_desc *n, const void *x, const void *resi
                    stride_of(n->ld_res, n->d), stride_of(n->ld_y, n->d), ld_codes,
                    stride_of(n->ld_scales, n->d / kMxBlock), n->rows, n->d, n->x_dtype,
                    n->res_dtype, n->w_dtype, n->y_dtype, n->eps};
-  by_width(n->d, [&](auto lanes, auto nv) {
+  by_width(n->d, n->rows, [&](auto lanes, auto nv) {
     constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
     const int per = L < 256 ? 256 / L : 1;
     hipLaunchKernelGGL((k_rms_norm<L, NV>), dim3((n->rows + per - 1) / per),

@@ -130,9 +130,22 @@ struct NormGradArgs {
 template <bool BF>
 struct Raw8 {
   Vec16 v[BF ? 1 : 2];
-  __device__ void load(const void *row, int dtype, int64_t at, int n) {
+  // whole: the row has eight values at least
+  template <bool SHIFT>
+  __device__ void load(const void *row, int dtype, int64_t at, int n, bool whole) {
     if (BF && n >= 8) {
       v[0] = *(const Any16 *)((const char *)row + at * 2);
+      return;
+    }
+    if (BF && SHIFT && whole) {  // the row's last few: its last eight, shifted down
+      v[0] = Vec16{};
+      if (n <= 0) return;
+      const Vec16 t = *(const Any16 *)((const char *)row + (at + n - 8) * 2);
+      const int bits = (8 - n) * 16;
+      uint64_t lo = t[0] | (uint64_t)t[1] << 32, hi = t[2] | (uint64_t)t[3] << 32;
+      lo = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits);
+      hi = bits >= 64 ? 0 : hi >> bits;
+      v[0] = Vec16{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
       return;
     }
     float f[8];
@@ -158,20 +171,26 @@ struct GradRow {
 
 // Block b takes rows b, b + gridDim.x, ... and keeps its part of dw in
 // registers; the parts are summed in block order by k_rms_norm_dw, so dw does
-// not depend on which block ran first.  AHEAD: the next row is loaded while
+// not depend on which block ran first.  Rows of one wave go to the four waves of
+// a block in turn, whose parts meet in LDS.  AHEAD: the next row is loaded while
 // this one's sums meet, and the weight stays in registers.  BF: the rows are all bf16 and are kept so until they
 // are used.
 template <int LANES, int NV, bool BF, bool AHEAD>
-__global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES,
+                             LANES == 512 && !AHEAD ? 4 : 1) void k_rms_norm_grad(NormGradArgs a) {
+  constexpr int SIDE = LANES == 64 ? 4 : 1;  // rows side by side in a block
   __shared__ float lds[2][2][LANES / 64];
-  const int lane = threadIdx.x;
+  const int lane = SIDE > 1 ? threadIdx.x % LANES : threadIdx.x;
+  const int64_t first = (int64_t)blockIdx.x * SIDE + (SIDE > 1 ? threadIdx.x / LANES : 0);
+  const int64_t stride = (int64_t)gridDim.x * SIDE;
+  const bool whole = a.d >= 8;
   auto load = [&](GradRow<BF, NV> &r, int64_t row) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int c = (u * LANES + lane) * 8;
-      r.s[u].load(a.s, a.s_dtype, row * a.ld_s + c, a.d - c);
-      r.dy[u].load(a.dy, a.dy_dtype, row * a.ld_dy + c, a.d - c);
-      if (AHEAD && a.dres) r.dres[u].load(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c);
+      r.s[u].template load<AHEAD>(a.s, a.s_dtype, row * a.ld_s + c, a.d - c, whole);
+      r.dy[u].template load<AHEAD>(a.dy, a.dy_dtype, row * a.ld_dy + c, a.d - c, whole);
+      if (AHEAD && a.dres) r.dres[u].template load<AHEAD>(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c, whole);
     }
   };
   float w[NV][8], dw[NV][8] = {};
@@ -183,12 +202,12 @@ __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
 #pragma unroll
     for (int u = 0; u < NV; ++u) load_w(u);
   GradRow<BF, NV> cur = {}, next = {};
-  if (AHEAD) load(next, blockIdx.x);
+  if (AHEAD && first < a.rows) load(next, first);
   int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+  for (int64_t row = first; row < a.rows; row += stride, turn ^= 1) {
     if (AHEAD) {
       cur = next;
-      if (row + gridDim.x < a.rows) load(next, row + gridDim.x);
+      if (row + stride < a.rows) load(next, row + stride);
     } else {
       load(cur, row);
     }
@@ -227,7 +246,7 @@ __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
       if (!AHEAD) {
         asm volatile("" ::: "memory");  // not kept from the sums above
         load_w(u);
-        if (a.dres) cur.dres[u].load(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c);
+        if (a.dres) cur.dres[u].template load<AHEAD>(a.dres, a.dx_dtype, row * a.ld_dx + c, a.d - c, whole);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -237,6 +256,16 @@ __global__ __launch_bounds__(LANES) void k_rms_norm_grad(NormGradArgs a) {
       }
       store8(a.dx, a.dx_dtype, row * a.ld_dx + c, a.d - c, dx);
     }
+  }
+  if (SIDE > 1) {
+    __shared__ float sums[SIDE > 1 ? SIDE : 1][SIDE > 1 ? LANES * 8 : 1];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[threadIdx.x / LANES][lane * 8 + j] = dw[0][j];
+    __syncthreads();
+    if (threadIdx.x >= LANES) return;
+    for (int i = 1; i < SIDE; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dw[0][j] += sums[i][lane * 8 + j];
   }
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -287,7 +316,7 @@ void by_width(int d, int rows, F f) {
 
 // Blocks of the backward pass: the most that run at once are two a compute
 // unit (512), and each writes a part of dw.
-int grad_blocks(int rows) { return std::min(rows, 512); }
+int grad_blocks(int rows, int d) { return std::min(d <= 512 ? (rows + 3) / 4 : rows, 512); }
 
 // Threads and groups of the backward pass, which keeps three rows, the weight
 // and dw: float32 rows, and ones past 8192 channels, are not loaded ahead (the
@@ -362,7 +391,7 @@ CEP_API int cep_rms_norm(const cep_norm_desc *n, const void *x, const void *resi
 
 CEP_API size_t cep_rms_norm_workspace(const cep_norm_desc *n) {
   if (bad_desc(n)) return 0;
-  return std::max<size_t>((size_t)grad_blocks(n->rows) * n->d * 4, 256);
+  return std::max<size_t>((size_t)grad_blocks(n->rows, n->d) * n->d * 4, 256);
 }
 
 CEP_API int cep_rms_norm_backward(const cep_norm_desc *n, const void *x, const void *w,
@@ -379,7 +408,7 @@ CEP_API int cep_rms_norm_backward(const cep_norm_desc *n, const void *x, const v
       !aligned(dx, dtype_bytes(n->res_dtype)) || !aligned(w, dtype_bytes(n->w_dtype)) ||
       !aligned(dw, dtype_bytes(n->w_dtype)) || !aligned(dy, dtype_bytes(n->y_dtype)))
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
-  const int blocks = grad_blocks(n->rows);
+  const int blocks = grad_blocks(n->rows, n->d);
   const NormGradArgs a{x, w, dy, dres, dx, (float *)workspace, stride_of(n->ld_x, n->d),
                        stride_of(n->ld_y, n->d), stride_of(n->ld_res, n->d), n->rows, n->d,
                        n->x_dtype, n->res_dtype, n->w_dtype, n->y_dtype, n->eps};
@@ -390,7 +419,7 @@ CEP_API int cep_rms_norm_backward(const cep_norm_desc *n, const void *x, const v
                     constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
                     hipLaunchKernelGGL(
                         (k_rms_norm_grad<L, NV, decltype(bf)::value, decltype(ahead)::value>),
-                        dim3(blocks), dim3(L), 0, s, a);
+                        dim3(blocks), dim3(L == 64 ? 256 : L), 0, s, a);
                   });
   hipLaunchKernelGGL(k_rms_norm_dw, dim3((n->d + 63) / 64), dim3(1024), 0, s, a.part, blocks, n->d,
                      n->w_dtype, dw);

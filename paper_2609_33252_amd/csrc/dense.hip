@@ -109,14 +109,15 @@ __device__ inline const char *uniform(const char *p) {
 // Each operand's 64-wide step is two halves of HALF rows (columns), loaded
 // straight to LDS; the operands' halves meet in four quadrants, one phase
 // each, in which a wave multiplies HALF/WM x HALF/WN outputs (16 matrix
-// instructions in the larger tiles).  Quadrants follow a snake (A0 B0, A0 B1, A1 B1,
-// A1 B0, then B swapped in the next step), so that only one operand half
+// instructions in the larger tile).  Quadrants follow a snake (A0 B0, A0 B1,
+// A1 B1, A1 B0, then B swapped in the next step), so that only one operand half
 // changes from phase to phase.  Fragments are read at least half a phase ahead
-// and spread over the phases (LDS reads fill three quarters of the time that
-// the matrix instructions take); a phase also loads one half, three to five
-// phases ahead of its use.  A barrier ends each phase: behind it, the loads the
-// next phase reads have landed in every wave, and the halves read in the phase
-// before have been consumed and may be refilled.
+// and spread over the phases; a phase also loads one half, three to five phases
+// ahead of its use.  A barrier ends each phase: behind it, the loads the next
+// phase reads have landed in every wave, and the halves read in the phase before
+// have been consumed and may be refilled.  (The scheduling barriers keep the
+// matrix instructions, and with them the waits for their fragments, on their
+// side of the phase's end.)
 //
 // LDS layout of a half, in 16-byte chunks so that every fragment read spreads
 // over all banks:
@@ -124,8 +125,11 @@ __device__ inline const char *uniform(const char *p) {
 //     is one 16-byte read a lane
 //   row contiguous: [64 k][row], chunk pair p (16 rows) of line k at p ^ f(k);
 //     a fragment is two transposing 8-byte reads of four lines of k
-// Measured (kernel alone): 8192 x 7168 x 2 x 2048 with SwiGLU 337 us, 1.43
-// PFLOP/s; bound by the matrix cores' issue and the loads that miss L2.
+//
+// Measured (kernel alone, 256-wide): 8192 x 7168 x 2 x 2048 with SwiGLU 321 us,
+// 1.50 PFLOP/s, the matrix pipe busy 65 % of the time at 2.1 GHz.  Bound inside
+// the CU: without the loads the pass is 15 % shorter, without the LDS reads 18 %,
+// with neither 31 %, with every load an L2 hit 4 %.
 template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
   constexpr bool DUAL = is_dual(EPI);
@@ -250,9 +254,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
   auto sync = [&] { asm volatile("s_barrier" ::: "memory"); };
   // Halves are loaded in the order A0, first B, second B, A1 of each step;
   // phase n (four a step) loads half n + 7, and the phase after it reads up
-  // to half n + 3 (n + 4 after a step's last phase).  Past the last step the loads repeat it, unread, so that
-  // the count in flight stays the same.  TURN: the step modulo 6, the period
-  // of the stages and the fragment sets.
+  // to half n + 3 (n + 4 after a step's last phase).  Past the last step the
+  // loads repeat it, unread, so that the count in flight stays the same.  TURN:
+  // the step modulo 6, the period of the stages and the fragment sets.
   auto phase = [&](int t, auto phase_c, auto turn_c) {
     constexpr int Q = decltype(phase_c)::value, TURN = decltype(turn_c)::value, P = TURN % 2;
     using M = std::integral_constant<int, Q / 2>;

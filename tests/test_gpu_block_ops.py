@@ -366,7 +366,9 @@ SHAPES = [(1, 8, 8), (1, 256, 128), (2, 264, 136), (16, 512, 2048), (17, 1000, 5
           (64, 2304, 1408), (65, 256, 128), (129, 520, 72), (256, 1024, 256), (300, 264, 1032),
           (513, 512, 384), (1500, 776, 520), (5, 4096, 16), (33, 16, 4096), (700, 2048, 1024),
           # enough outputs for the 256-wide tiles, in each of the six products
-          (3001, 3080, 1544), (3001, 1544, 3080), (300, 3080, 3080)]
+          (3001, 3080, 1544), (3001, 1544, 3080), (300, 3080, 3080),
+          # 256-wide tiles that share K
+          (2047, 9224, 1024)]
 
 
 def _ffn_tols(x, wg, wu, wd):

@@ -1,9 +1,9 @@
 // Dense gated feed-forward of few rows for gfx950: the weights are streamed
 // once, at HBM rate, and the rows ride along.
 //
-// A workgroup takes a row block of up to 64 rows, 128 columns (64 of the gate
-// and the same 64 of the up projection, or 128 of the down projection) and a
-// share of K; its four waves take the share's 32-wide units in turn, each with
+// A workgroup takes all rows (up to 64), 128 columns (64 of the gate and the
+// same 64 of the up projection, or 128 of the down projection) and a share of
+// K; its four waves take the share's 32-wide units in turn, each with
 // a ring of its own in LDS and no barrier between them.  The waves' sums meet
 // in LDS, the shares' in a float32 scratch.  The shares are added in order by
 // the launch that follows: those of g and u by k_rows_hidden, which applies
@@ -35,7 +35,7 @@ struct RowsArgs {
   const __bf16 *B0, *B1;
   int64_t lda, ldb;
   int M, N, K;
-  int splits, col_blocks, row_blocks;
+  int splits, col_blocks;
   float *part;  // [splits][M][columns]; unused with one share of a plain product
   __bf16 *y;    // its output
   int64_t ldy;
@@ -82,18 +82,13 @@ __global__ __launch_bounds__(256) void k_rows(RowsArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t terms[SRC == kFused ? kFusedBytes : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l15 = lane & 15, g4 = lane >> 4;
-  // the row blocks of a piece of the weights run on one XCD, next to each other
-  const int pieces = a.col_blocks * a.splits;
-  const int j = blockIdx.x >> 3;
-  const int piece = (j / a.row_blocks) * 8 + (blockIdx.x & 7), rb = j % a.row_blocks;
-  if (piece >= pieces) return;
-  const int cb = piece % a.col_blocks, sp = piece / a.col_blocks;
-  const int row0 = rb * MF * 16, n0 = cb * (DUAL ? 64 : kCols);
+  const int cb = blockIdx.x % a.col_blocks, sp = blockIdx.x / a.col_blocks;
+  const int n0 = cb * (DUAL ? 64 : kCols);
   const int units = a.K / kUnit;
   const int u0 = (int)((int64_t)units * sp / a.splits), u1 = (int)((int64_t)units * (sp + 1) / a.splits);
   const int mine = u1 - u0 > wave ? (u1 - u0 - wave + 3) / 4 : 0;  // units u0 + wave + 4 i
 
-  // Loads of a unit: 8 lines pieces of B, four lines of k x 128 columns each
+  // Loads of a unit: 8 pieces of B, four lines of k x 128 columns each
   // (16-byte chunk pair p of line k at p ^ (k % 4 + k / 8 % 2 * 4)), then 16
   // rows x 32 of k a piece of A (chunk c of row r at c ^ (r / 4 % 4)).
   const char *srcB[2];
@@ -108,7 +103,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsArgs a) {
 #pragma unroll
   for (int i = 0; i < (SRC == kFused ? 0 : NA); ++i) {
     const int r = lane >> 2;
-    const int row = min(row0 + (i % MF) * 16 + r, a.M - 1);
+    const int row = min((i % MF) * 16 + r, a.M - 1);
     srcA[i] = (const char *)(a.A[i / MF] + row * a.lda + ((lane & 3) ^ ((r >> 2) & 3)) * 8);
   }
   uint8_t *ring = lds + wave * RING;
@@ -208,7 +203,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsArgs a) {
   // four columns of a row each; returns false outside the product
   auto place = [&](int q, int *row, int *col) {
     const int c = (q % (kCols / 4)) * 4;
-    *row = row0 + q / (kCols / 4);
+    *row = q / (kCols / 4);
     const int n = n0 + (DUAL ? c & 63 : c);
     *col = DUAL && c >= 64 ? a.N + n : n;
     return *row < a.M && n < a.N;
@@ -265,7 +260,7 @@ int row_frags(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 template <Source SRC, bool DUAL>
 void launch_rows(const RowsArgs &a, hipStream_t s) {
   const int mf = row_frags(a.M);
-  const dim3 grid(blocks_of(a.col_blocks * a.splits, 8) * 8 * a.row_blocks);
+  const dim3 grid(a.col_blocks * a.splits);
   auto *k = k_rows<1, SRC, DUAL>;
   if constexpr (SRC != kFused)
     if (mf > 1) k = mf == 2 ? k_rows<2, SRC, DUAL> : k_rows<4, SRC, DUAL>;
@@ -286,11 +281,10 @@ RowsPlan rows_plan(int rows, int d, int I) {
   RowsPlan p{};
   p.use = rows > 0 && rows <= kRowsMost;
   if (!p.use) return p;
-  const int rb = blocks_of(rows, row_frags(rows) * 16);
   // one workgroup a compute unit (a ring takes most of its LDS), at least a
   // unit for each wave
   auto splits = [&](int cols, int K) {
-    return std::max(1, std::min(256 / (cols * rb), K / kUnit / 4));
+    return std::max(1, std::min(256 / cols, K / kUnit / 4));
   };
   p.splits1 = splits(blocks_of(I, 64), d);
   p.splits2 = splits(blocks_of(d, kCols), I);
@@ -319,7 +313,6 @@ void launch_rows_ffn(const RowsPlan &p, int rows, int d, int I, const __bf16 *x,
                      const __bf16 *wg, const __bf16 *wu, const __bf16 *wd, __bf16 *y, int64_t ld_y,
                      float *pre, uint8_t *workspace, hipStream_t s) {
   const RowsSpace w = rows_space(p, rows, d, I);
-  const int rb = blocks_of(rows, row_frags(rows) * 16);
   float *part = (float *)workspace, *part2 = (float *)(workspace + w.part2);
   __bf16 *hi = (__bf16 *)(workspace + w.hi), *lo = (__bf16 *)(workspace + w.lo);
   RowsArgs a{};
@@ -327,7 +320,7 @@ void launch_rows_ffn(const RowsPlan &p, int rows, int d, int I, const __bf16 *x,
   a.B0 = wg, a.B1 = wu;
   a.lda = ld_x, a.ldb = I;
   a.M = rows, a.N = I, a.K = d;
-  a.splits = p.splits1, a.col_blocks = blocks_of(I, 64), a.row_blocks = rb;
+  a.splits = p.splits1, a.col_blocks = blocks_of(I, 64);
   a.part = part;
   launch_rows<kRows, true>(a, s);
   RowsArgs b{};
@@ -335,7 +328,7 @@ void launch_rows_ffn(const RowsPlan &p, int rows, int d, int I, const __bf16 *x,
   b.B0 = wd;
   b.lda = I, b.ldb = d;
   b.M = rows, b.N = d, b.K = I;
-  b.splits = p.splits2, b.col_blocks = blocks_of(d, kCols), b.row_blocks = rb;
+  b.splits = p.splits2, b.col_blocks = blocks_of(d, kCols);
   b.part = part2;
   b.y = y, b.ldy = ld_y;
   b.gu = part, b.gu_splits = p.splits1;

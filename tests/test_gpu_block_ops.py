@@ -368,7 +368,10 @@ SHAPES = [(1, 8, 8), (1, 256, 128), (2, 264, 136), (16, 512, 2048), (17, 1000, 5
           # enough outputs for the 256-wide tiles, in each of the six products
           (3001, 3080, 1544), (3001, 1544, 3080), (300, 3080, 3080),
           # 256-wide tiles that share K
-          (2047, 9224, 1024)]
+          (2047, 9224, 1024),
+          # the last gradients in one launch of one round; in a launch each, with
+          # 256-wide tiles, with shares of dx, and with shares of the weights'
+          (2621, 2304, 1328), (4095, 4096, 2048), (100, 520, 4104), (5000, 264, 264)]
 
 
 def _ffn_tols(x, wg, wu, wd):

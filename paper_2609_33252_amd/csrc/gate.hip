@@ -13,8 +13,8 @@
 // the low word, so that one v_max_f64 compares both.
 //
 // Measured: 65536 rows of 160 logits, k 8, softmax 11.5 us, 4 TB/s, bound by
-// the sorts' instructions; 9 rows of 256 in eight groups, sigmoid, 6.3 us, the
-// latency of the groups' sums and of eight rounds.
+// the sorts' instructions; 9 rows of 256 in eight groups, sigmoid, 4.2 us, where
+// an empty launch takes 3.5 to 4.
 #include "block_ops.h"
 
 #include <cfloat>
@@ -79,6 +79,19 @@ __device__ inline double row_max(double v) {
   }
   return v;
 }
+// The two largest of eight lanes' pairs best >= second, in each of them.
+template <int CTRL>
+__device__ inline void dpp_top2(float *best, float *second) {
+  const float b = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(*best), CTRL, 0xf, 0xf, false));
+  const float s = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(*second), CTRL, 0xf, 0xf, false));
+  *second = fmaxf(fminf(*best, b), fmaxf(*second, s));
+  *best = fmaxf(*best, b);
+}
+__device__ inline void lanes_top2(float *best, float *second) {
+  dpp_top2<0xB1>(best, second);
+  dpp_top2<0x4E>(best, second);
+  dpp_top2<0x141>(best, second);
+}
 template <int LPR>
 __device__ inline float row_add(float v) {
 #pragma unroll
@@ -112,12 +125,23 @@ __device__ inline float logit(const GateArgs &a, int64_t row, int e) {
   return unmasked(a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
                                       : ((const float *)a.logits)[row * a.ld + e]);
 }
-// (the reciprocal instruction is within one unit of the last place)
-__device__ inline float sigmoid(float l) { return __builtin_amdgcn_rcpf(1.0f + expf(-l)); }
+// 1 / (1 + 2^t), t = -l log2(e), with t's rounding error r put back as 2^r ~ 1 +
+// r ln(2): the exponential and reciprocal instructions are within one unit of
+// the last place.  Beyond +-90 it is 0 or 1.
+__device__ inline float sigmoid(float l) {
+  constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;
+  const float c = fminf(fmaxf(-l, -90.0f), 90.0f), t = c * kLog2e;
+  const float r = fmaf(c, kLog2eRest, fmaf(c, kLog2e, -t));
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(r, 0.693147182f, 1.0f));
+}
+
+// How groups are found: none; any size, through LDS; 32 experts, in eight lanes'
+// registers.
+enum Groups { kNoGroups, kAnyGroups, kGroupsOf32 };
 
 // LPR lanes a row, V experts a lane (V a multiple of 4: chunk j of a lane is
 // the four experts from (j * LPR + lane) * 4), at most KM chosen.
-template <int LPR, int V, int KM, bool SIGMOID, bool GROUPS>
+template <int LPR, int V, int KM, bool SIGMOID, Groups GROUPS>
 __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
   constexpr int ROWS = 256 / LPR;  // rows of a block
   const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
@@ -156,7 +180,45 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
       key[4 * j + i] = q;
     }
   }
-  if (GROUPS) {
+  if constexpr (GROUPS == kGroupsOf32) {
+    // a chunk of 32 experts is a group: chunk j of the row's eight lanes, or (a
+    // wave a row, one chunk) of the eight lanes around this one
+    static_assert(LPR == 8 || V == 4, "one chunk a lane");
+    float total[V / 4];
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j) {
+      const float *v = key + 4 * j;
+      const float lo = fminf(v[0], v[1]), hi = fminf(v[2], v[3]);
+      const float a0 = fmaxf(v[0], v[1]), a1 = fmaxf(v[2], v[3]);
+      float best = fmaxf(a0, a1), second = fmaxf(fminf(a0, a1), fmaxf(lo, hi));
+      lanes_top2(&best, &second);
+      total[j] = second > -INFINITY ? best + second : best;
+    }
+    // the groups past the last have nothing and come last
+    if (LPR == 8) {
+      float own = -INFINITY;  // group `lane`
+#pragma unroll
+      for (int c = 0; c < V / 4; ++c) own = lane == c ? total[c] : own;
+      int rank = 0;
+#pragma unroll
+      for (int c = 0; c < V / 4; ++c) rank += total[c] > own || (total[c] == own && c < lane);
+      const uint64_t keep = __ballot(rank < a.topg) >> (threadIdx.x & 56);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (!((keep >> (j / 4)) & 1)) key[j] = -INFINITY;
+    } else {
+      int rank = 0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float t = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(total[0]), 8 * c));
+        rank += t > total[0] || (t == total[0] && c < lane / 8);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (rank >= a.topg) key[j] = -INFINITY;
+    }
+  }
+  if constexpr (GROUPS == kAnyGroups) {
     // rows 8 words apart modulo the banks, and one word between groups, so that
     // the lanes of a wave, at the same place of their groups, read 64 banks
     __shared__ float keys[ROWS][LPR * V + kMaxGroups + 8];
@@ -254,19 +316,25 @@ __global__ __launch_bounds__(256) void k_gate(GateArgs a) {
 template <int LPR, int V, int KM>
 void launch_gate(const GateArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)(((int64_t)a.rows * LPR + 255) / 256));
-  auto *k = !a.sigmoid ? k_gate<LPR, V, KM, false, false>
-            : a.groups > 1 ? k_gate<LPR, V, KM, true, true> : k_gate<LPR, V, KM, true, false>;
+  auto *k = !a.sigmoid ? k_gate<LPR, V, KM, false, kNoGroups>
+            : a.groups > 1 ? k_gate<LPR, V, KM, true, kAnyGroups>
+                           : k_gate<LPR, V, KM, true, kNoGroups>;
+  if constexpr (LPR == 8 || V == 4)
+    if (a.groups > 1 && a.E == 32 * a.groups) k = k_gate<LPR, V, KM, true, kGroupsOf32>;
   hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
 }
 
 // Few rows: a wave a row, four experts a lane, for the latency of one row;
 // more rows: eight lanes a row, which takes fewer instructions a row.  256
-// experts, k 8, us a call of 64 / 4096 / 8192 / 65536 rows: softmax 3.7 / 5.1 /
-// 7.6 / 42.8 with a wave, 4.0 / 4.4 / 4.4 / 16.1 with eight lanes; sigmoid in
-// eight groups 6.9 / 8.9 / 13.7 / 76.8 and 9.7 / 10.3 / 10.5 / 39.1.
+// experts, k 8, us a call of 64 / 2048 / 4096 / 65536 rows: softmax 3.7 / 4.0 /
+// 5.2 / 41.5 with a wave, 4.3 / 4.4 / 4.5 / 16.3 with eight lanes; sigmoid in
+// eight groups of 32 4.3 / 4.9 / 6.5 / 55.8 and 5.5 / 5.8 / 5.8 / 24.0; 96 in
+// four of 24, through LDS, 6.2 / 6.3 / 8.0 / 66.8 and 7.7 / 8.0 / 8.1 / 29.9.
+// (Groups of 32 through LDS, as those of any size are: 6.7 and 6.7 with a wave,
+// 38.3 us for 65536 rows with eight lanes.)
 template <int KM>
 void launch_by_experts(const GateArgs &a, hipStream_t s) {
-  if (a.E <= 256 && a.rows <= (a.groups > 1 ? 4096 : 2048)) launch_gate<64, 4, KM>(a, s);
+  if (a.E <= 256 && a.rows <= (a.groups > 1 && a.E != 32 * a.groups ? 4096 : 2048)) launch_gate<64, 4, KM>(a, s);
   else if (a.E <= 64) launch_gate<8, 8, KM>(a, s);
   else if (a.E <= 128) launch_gate<8, 16, KM>(a, s);
   else if (a.E <= 160) launch_gate<8, 20, KM>(a, s);

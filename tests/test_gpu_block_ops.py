@@ -282,6 +282,41 @@ def test_gate_sigmoid_groups(E, groups, topg, k):
     _gate_check(logits, k, "sigmoid", None, groups, topg, normalize=False, scale=0.5)
 
 
+@pytest.mark.parametrize("T", [1, 7, 4097])
+@pytest.mark.parametrize("E,groups,topg,k", [(256, 8, 4, 8), (256, 8, 1, 16), (160, 5, 2, 6),
+                                             (64, 2, 1, 1), (32, 1, 1, 8), (128, 4, 4, 8),
+                                             (256, 4, 2, 8), (96, 4, 2, 6)])
+def test_gate_sigmoid_groups_of_many_rows(T, E, groups, topg, k):
+    """A row a wave and eight rows a wave; groups of 32 experts and others."""
+    g = _gen(E + groups + T)
+    logits = _spaced(g, 7, E, groups)[torch.arange(T, device="cuda") % 7]
+    some = torch.arange(T, device="cuda") % 17
+    logits[some == 3, E // groups:] = -float("inf")  # one group is left
+    logits[some == 4, 1::2] = -float("inf")
+    logits[some == 5, 0::E // groups] = float("nan")
+    logits[some == 6, 3:] = -float("inf")
+    logits[some == 8] = -float("inf")
+    _gate_check(logits, k, "sigmoid", None, groups, topg)
+    _gate_check(logits, k, "sigmoid", None, groups, topg, normalize=False, scale=0.5)
+
+
+@pytest.mark.parametrize("E", [64, 100, 160, 256])
+def test_gate_softmax_of_many_rows(E):
+    logits = _randn(_gen(E), 2049, E, dtype=torch.float32)
+    logits[3::17, 5:] = -float("inf")
+    for normalize in (True, False):
+        _gate_check(logits, 8, normalize=normalize)
+
+
+def test_gate_sigmoid_range():
+    """Scores of logits far below zero, down to where float32 ends their
+    exponential, and above it."""
+    l = torch.linspace(-85, 5, 256, device="cuda")
+    for lo in range(0, 256, 16):
+        _gate_check(l[None, lo:lo + 16].contiguous(), 16, "sigmoid", normalize=False)
+    _gate_check(torch.full((1, 4), 1000.0, device="cuda"), 4, "sigmoid", normalize=False)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_gate_ties_and_masks(dtype):
     g = _gen(3)

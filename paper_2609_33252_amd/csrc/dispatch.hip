@@ -9,8 +9,8 @@
 // (k_send_count), their prefix sums and the plan (k_send_scan), and the rows
 // (k_send), a wave a token, which reads its row once, before it knows where the
 // row goes, and writes it to each of its places.  Bound by HBM: 8192
-// rows of 6336 bytes to ten ranks, 5.8 places each, 86 us, 4.1 TB/s, of which
-// k_send 74; 13 rows of 14336 bytes 7.3 us, the latency of ids, counts and
+// rows of 6336 bytes to ten ranks, 5.8 places each, 85 us, 4.2 TB/s, of which
+// k_send 74; 13 rows of 14336 bytes 6.2 us, the latency of ids, counts and
 // places.  (One launch for all with four tokens a wave: 189 us for 8192
 // rows, 78 us for 13, too few loads in flight.)
 #include "block_ops.h"
@@ -21,7 +21,10 @@ namespace cep {
 namespace {
 
 constexpr int kMaxRanks = 64;      // one lane each
-constexpr int kFewTokens = 256;    // packed by one launch
+// Packed by one launch.  Rows of 6336 bytes to eight ranks, us in one launch and in
+// three: 300 rows 10.4, 18.3; 512 11.9, 19.1; 1024 25.8, 20.0; 512 rows to 64
+// ranks 17.1, 20.7.
+constexpr int kFewTokens = 512;
 constexpr int kCountTokens = 256;  // tokens of a k_send_count block
 constexpr int kSendTokens = 16;    // tokens of a k_send block (a tile)
 constexpr int kTiles = kCountTokens / kSendTokens;
@@ -41,15 +44,19 @@ struct SendArgs {
   int32_t *tile_at, *tot, *pairs, *bad;
   int rows, k, R, per, blocks;
   int64_t row_bytes;
+  uint32_t mul, shift;  // id / per = id * mul >> shift
 };
 
-// The rank that holds an expert, -1: none.
+// The rank that holds an expert, -1: none.  mul = 2^shift / per rounded up and
+// shift = 26 + log2(per) rounded up give the whole quotient of any id below
+// 2^26, which those of 64 ranks of 2^20 experts are.
 __device__ inline int rank_of(const SendArgs &a, int id) {
-  return id >= 0 && id < a.R * a.per ? id / a.per : -1;
+  return id >= 0 && id < a.R * a.per ? (int)(((uint64_t)(uint32_t)id * a.mul) >> a.shift) : -1;
 }
 
-// The ranks (a bit each) that hold the experts of token t; counts its pairs
-// per rank, and its ids that no rank has (apart from -1), in LDS.
+// The ranks (a bit each) that hold the experts of token t; COUNT: counts its
+// pairs per rank, and its ids that no rank has (apart from -1), in LDS.
+template <bool COUNT>
 __device__ inline uint64_t ranks_of(const SendArgs &a, int64_t t, int32_t *pairs, int32_t *bad) {
   int32_t id[kMaxTopK];
 #pragma unroll
@@ -61,8 +68,8 @@ __device__ inline uint64_t ranks_of(const SendArgs &a, int64_t t, int32_t *pairs
     const int r = rank_of(a, id[j]);
     if (r >= 0) {
       m |= 1ull << r;
-      atomicAdd(&pairs[r], 1);
-    } else if (id[j] != -1) {
+      if (COUNT) atomicAdd(&pairs[r], 1);
+    } else if (COUNT && id[j] != -1) {
       atomicAdd(bad, 1);
     }
   }
@@ -89,7 +96,7 @@ __global__ __launch_bounds__(kCountTokens) void k_send_count(SendArgs a) {
   if (tid < kMaxRanks) pairs[tid] = 0;
   if (tid == 0) bad = 0;
   __syncthreads();
-  const uint64_t m = t < a.rows ? ranks_of(a, t, pairs, &bad) : 0;
+  const uint64_t m = t < a.rows ? ranks_of<true>(a, t, pairs, &bad) : 0;
   uint64_t there = 0;  // the wave's tokens that go to rank `lane`
   for (int r = 0; r < a.R; ++r) {
     const uint64_t v = __ballot((m >> r) & 1);
@@ -170,16 +177,18 @@ __device__ inline void write_meta(const SendArgs &a, int t, int place, uint64_t 
   }
 }
 
-// A row's 16-byte chunks [c0, c0 + 64 U), U a lane (past the row's last whole
-// chunk the lane reads that one again).
+// A row's 16-byte chunks c0 + lane, and every STEP from there, kChunks in all
+// (past the row's last whole chunk the lane reads that one again).
 constexpr int kChunks = 8;
+template <int STEP>
 __device__ inline void load_row(const SendArgs &a, const char *src, int c0, Vec16 (&v)[kChunks]) {
   const int lane = threadIdx.x & 63, n = (int)(a.row_bytes / 16);
   if (n == 0) return;
 #pragma unroll
   for (int u = 0; u < kChunks; ++u)
-    v[u] = *(const Any16 *)(src + (int64_t)min(c0 + u * 64 + lane, n - 1) * 16);
+    v[u] = *(const Any16 *)(src + (int64_t)min(c0 + u * STEP + lane, n - 1) * 16);
 }
+template <int STEP>
 __device__ inline void store_row(const SendArgs &a, int place, uint64_t go, int c0,
                                  const Vec16 (&v)[kChunks]) {
   const int lane = threadIdx.x & 63, n = (int)(a.row_bytes / 16);
@@ -187,7 +196,7 @@ __device__ inline void store_row(const SendArgs &a, int place, uint64_t go, int 
     char *dst = a.out_x + (int64_t)__shfl(place, __builtin_ctzll(g)) * a.row_bytes;
 #pragma unroll
     for (int u = 0; u < kChunks; ++u) {
-      const int c = c0 + u * 64 + lane;
+      const int c = c0 + u * STEP + lane;
       if (c < n) *(Any16 *)(dst + (int64_t)c * 16) = v[u];
     }
   }
@@ -211,7 +220,7 @@ __global__ __launch_bounds__(64 * kSendTokens) void k_send(SendArgs a) {
   const bool live = t < a.rows;
   const char *src = a.x + (live ? t : 0) * a.ld_x;
   Vec16 v[kChunks] = {};
-  if (live) load_row(a, src, 0, v);
+  if (live) load_row<64>(a, src, 0, v);
   const int id = live && lane < a.k ? a.ids[t * a.k + lane] : -1;
   const float w = live && lane < a.k ? a.w[t * a.k + lane] : 0.f;
   int place = 0;
@@ -228,40 +237,45 @@ __global__ __launch_bounds__(64 * kSendTokens) void k_send(SendArgs a) {
   if (!live) return;
   for (int i = 0; i < wave; ++i) place += (int)((mask[i] >> lane) & 1);
   write_meta(a, (int)t, place, go, id, w);
-  store_row(a, place, go, 0, v);
+  store_row<64>(a, place, go, 0, v);
   for (int c0 = 64 * kChunks; c0 < a.row_bytes / 16; c0 += 64 * kChunks) {
-    load_row(a, src, c0, v);
-    store_row(a, place, go, c0, v);
+    load_row<64>(a, src, c0, v);
+    store_row<64>(a, place, go, c0, v);
   }
   copy_tail(a, src, place, go);
 }
 
-// Up to 256 tokens: workgroup i packs token i, its four waves a share of the
-// row each; thread t counts token t.
-__global__ __launch_bounds__(kFewTokens) void k_send_few(SendArgs a) {
+// Workgroup i packs token i, its four waves every fourth 1 KB of the row; its
+// threads count every token first.  One workgroup more writes the plan.
+__global__ __launch_bounds__(256) void k_send_few(SendArgs a) {
   __shared__ int32_t sent[4][kMaxRanks], before[4][kMaxRanks], pairs[kMaxRanks], bad;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int token = blockIdx.x;
-  const bool live = token < a.rows;  // a grid of one for no rows
-  const char *src = a.x + (live ? token : 0) * a.ld_x;
+  const bool packs = token < a.rows;  // the same in the whole workgroup
+  const char *src = a.x + (packs ? token : 0) * a.ld_x;
   const int chunks = (int)(a.row_bytes / 16);
   Vec16 v[kChunks] = {};
-  const int first = wave * 64 * kChunks;
-  if (live) load_row(a, src, first, v);
-  const int id = live && lane < a.k ? a.ids[(int64_t)token * a.k + lane] : -1;
-  const float w = live && lane < a.k ? a.w[(int64_t)token * a.k + lane] : 0.f;
-  if (tid < kMaxRanks) pairs[tid] = 0;
-  if (tid == 0) bad = 0;
-  __syncthreads();
-  const uint64_t m = tid < a.rows ? ranks_of(a, tid, pairs, &bad) : 0;
-  int n_sent = 0, n_before = 0;
-  const int rel = token - wave * 64;  // this workgroup's token among the wave's
-  const uint64_t earlier = rel <= 0 ? 0 : rel >= 64 ? ~0ull : (1ull << rel) - 1;
-  for (int r = 0; r < a.R; ++r) {
-    const uint64_t there = __ballot((m >> r) & 1);
-    if (lane == r) {
-      n_sent = (int)__popcll(there);
-      n_before = (int)__popcll(there & earlier);
+  if (packs) load_row<256>(a, src, wave * 64, v);
+  const int id = packs && lane < a.k ? a.ids[(int64_t)token * a.k + lane] : -1;
+  const float w = packs && lane < a.k ? a.w[(int64_t)token * a.k + lane] : 0.f;
+  if (!packs) {
+    if (tid < kMaxRanks) pairs[tid] = 0;
+    if (tid == 0) bad = 0;
+    __syncthreads();
+  }
+  int n_sent = 0, n_before = 0;  // of the wave's tokens, to rank `lane`
+  for (int t0 = 0; t0 < a.rows; t0 += 256) {
+    const int t = t0 + tid, rel = token - t0 - wave * 64;  // this token among the wave's
+    uint64_t m = 0;
+    if (t < a.rows)
+      m = packs ? ranks_of<false>(a, t, pairs, &bad) : ranks_of<true>(a, t, pairs, &bad);
+    const uint64_t earlier = rel <= 0 ? 0 : rel >= 64 ? ~0ull : (1ull << rel) - 1;
+    for (int r = 0; r < a.R; ++r) {
+      const uint64_t there = __ballot((m >> r) & 1);
+      if (lane == r) {
+        n_sent += (int)__popcll(there);
+        n_before += (int)__popcll(there & earlier);
+      }
     }
   }
   sent[wave][lane] = n_sent;
@@ -273,15 +287,15 @@ __global__ __launch_bounds__(kFewTokens) void k_send_few(SendArgs a) {
     all += sent[i][lane];
     place += before[i][lane];
   }
-  place += wave_before(all);
-  if (token == 0) {
+  if (!packs) {
     __syncthreads();  // before wave 0 replaces its counts by the sums
     if (wave == 0) {
       sent[0][lane] = all;
       write_plan(a, sent[0], pairs, bad);
     }
+    return;
   }
-  if (!live) return;
+  place += wave_before(all);
   const int r_id = rank_of(a, id);
   uint64_t go = 0;
   for (int j = 0; j < a.k; ++j) {
@@ -289,10 +303,10 @@ __global__ __launch_bounds__(kFewTokens) void k_send_few(SendArgs a) {
     if (r >= 0) go |= 1ull << r;
   }
   if (wave == 0) write_meta(a, token, place, go, id, w);
-  store_row(a, place, go, first, v);
-  for (int c0 = first + 4 * 64 * kChunks; c0 < chunks; c0 += 4 * 64 * kChunks) {
-    load_row(a, src, c0, v);
-    store_row(a, place, go, c0, v);
+  for (int c0 = wave * 64;; c0 += 256 * kChunks) {
+    store_row<256>(a, place, go, c0, v);
+    if (c0 + 256 * kChunks >= chunks) break;
+    load_row<256>(a, src, c0 + 256 * kChunks, v);
   }
   if (wave == 3) copy_tail(a, src, place, go);
 }
@@ -348,9 +362,11 @@ CEP_API int cep_dispatch(const cep_dispatch_desc *d, const int32_t *topk_id, con
   SendArgs a{topk_id, topk_w, (const char *)x, d->ld_x ? d->ld_x : d->row_bytes, plan, token_idx,
              out_id, out_w, (char *)out_x, ws, ws + (size_t)blocks * kTiles * R,
              ws + (size_t)blocks * (kTiles + 1) * R, ws + (size_t)blocks * (kTiles + 2) * R,
-             d->rows, d->top_k, R, d->experts_per_rank, blocks, d->row_bytes};
+             d->rows, d->top_k, R, d->experts_per_rank, blocks, d->row_bytes, 0, 26};
+  while ((1 << (a.shift - 26)) < a.per) ++a.shift;
+  a.mul = (uint32_t)(((uint64_t)1 << a.shift) / a.per + 1);
   if (d->rows <= kFewTokens) {
-    hipLaunchKernelGGL(k_send_few, dim3(std::max(1, d->rows)), dim3(kFewTokens), 0, s, a);
+    hipLaunchKernelGGL(k_send_few, dim3(d->rows + 1), dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL(k_send_count, dim3(blocks), dim3(kCountTokens), 0, s, a);
     hipLaunchKernelGGL(k_send_scan, dim3(1), dim3(1024), 0, s, a);

@@ -354,6 +354,8 @@ def test_gate_strided_rows_and_unaligned_start():
     (16, 16, 64, 3, 17, 1), (255, 4, 5, 12, 33, 0), (256, 6, 10, 16, 272, 0),
     (257, 8, 10, 16, 1000, 24), (1000, 2, 64, 1, 16, 0), (3001, 8, 8, 8, 48, 0),
     (5000, 1, 3, 7, 2, 3), (300, 8, 2, 20, 131072, 0),
+    (511, 8, 8, 32, 1056, 0), (512, 16, 64, 5, 130, 6), (513, 8, 8, 32, 48, 0),
+    (2, 8, 64, 1 << 20, 4112, 0), (40, 4, 63, 1048575, 20, 4),
 ])
 def test_dispatch(T, k, ranks, per, row, pad):
     g = np.random.default_rng(T * 7 + row)

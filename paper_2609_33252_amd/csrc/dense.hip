@@ -87,6 +87,7 @@ __global__ __launch_bounds__(256) void k_dense_finish(DenseArgs a) {
   if (m >= a.M) return;
   const int64_t width = is_dual(EPI) ? 2 * a.N : a.N;
   f32x4 v = {}, w = {};
+#pragma unroll 4
   for (int i = 0; i < a.splits; ++i) {
     const float *p = a.part + ((int64_t)i * a.M + m) * width + n;
     v += *(const f32x4 *)p;

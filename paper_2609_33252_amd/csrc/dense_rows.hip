@@ -1,7 +1,7 @@
 // Dense gated feed-forward of few rows for gfx950: the weights are streamed
 // once, at HBM rate, and the rows ride along.
 //
-// A workgroup takes all rows (up to 64), 128 columns (64 of the gate and the
+// A workgroup takes all rows (up to 32), 128 columns (64 of the gate and the
 // same 64 of the up projection, or 128 of the down projection) and a share of
 // K; its four waves take the share's 32-wide units in turn, each with
 // a ring of its own in LDS and no barrier between them.  The waves' sums meet
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void k_rows(RowsArgs a) {
   constexpr int NF = kCols / 16;
   constexpr int NA = SRC == kRows ? MF : 2 * MF;            // fragments of A
   constexpr int LOADS = 8 + (SRC == kFused ? 0 : NA);       // 1 KB loads of a unit
-  constexpr int DEPTH = LOADS > 12 ? 2 : 3;
+  constexpr int DEPTH = 3;                                  // units on the way
   constexpr int RING = LOADS * 1024 * DEPTH;
   constexpr int SUMS = MF * 16 * kPitch * 4;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[4 * (RING > SUMS ? RING : SUMS)];
@@ -269,15 +269,13 @@ __global__ __launch_bounds__(256) void k_rows_sum(const float *part, int splits,
 }
 
 int blocks_of(int n, int per) { return (n + per - 1) / per; }
-int row_frags(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 
 template <Source SRC, bool DUAL>
 void launch_rows(const RowsArgs &a, hipStream_t s) {
-  const int mf = row_frags(a.M);
   const dim3 grid(a.col_blocks * a.splits);
   auto *k = k_rows<1, SRC, DUAL>;
   if constexpr (SRC != kFused)
-    if (mf > 1) k = mf == 2 ? k_rows<2, SRC, DUAL> : k_rows<4, SRC, DUAL>;
+    if (a.M > 16) k = k_rows<2, SRC, DUAL>;
   hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
 }
 
@@ -286,10 +284,10 @@ unsigned grid_of(int64_t elements) { return (unsigned)((elements / 4 + 255) / 25
 }  // namespace
 
 // Rows up to which the weights are streamed.  Above it the tiled product with
-// K shares is as fast (both products; d 4096, d_ff 2048: 16 rows 21.9 us here,
-// 23.7 tiled; 64 rows 28.9, 27.9; d 7168: 16 rows 28.7, 31.0; 128 rows 49.0,
-// 45.1).
-constexpr int kRowsMost = 64;
+// K shares is as fast (both products, us here and tiled; d 4096, d_ff 2048: 1
+// row 15.8, 19.9; 16 rows 19.2, 21.3; 32 rows 21.3, 22.7; 33 rows 23.7, 22.5;
+// d 7168: 16 rows 27.1, 26.9; 32 rows 30.8, 29.0; 64 rows 37.5, 33.5).
+constexpr int kRowsMost = 32;
 
 RowsPlan rows_plan(int rows, int d, int I) {
   RowsPlan p{};
@@ -346,10 +344,13 @@ void launch_rows_ffn(const RowsPlan &p, int rows, int d, int I, const __bf16 *x,
   b.part = part2;
   b.y = y, b.ldy = ld_y;
   b.gu = part, b.gu_splits = p.splits1;
-  // each workgroup of the down projection adds its share's g and u itself
-  // while that is little (one token: 16 KB), which saves a launch
+  // Each workgroup of the down projection adds its share's g and u itself while
+  // that reads up to 128 KB, which saves a launch (us, saved and not: one row of
+  // 4096 x 2048, 18 KB, 15.9, 17.7; one of 7168 x 2048, 35 KB, 23.4, 25.1; four,
+  // 139 KB, 26.0, 25.7; eight, 279 KB, 28.6, 26.0).
   const int share = (blocks_of(I / kUnit, p.splits2) + 1) * kUnit;
-  if (rows <= 8 && rows * share * 4 <= kFusedBytes && !pre) {
+  if (rows <= 16 && rows * share * 4 <= kFusedBytes &&
+      (int64_t)rows * share * 8 * p.splits1 <= 128 << 10 && !pre) {
     launch_rows<kFused, false>(b, s);
   } else {
     hipLaunchKernelGGL(k_rows_hidden, dim3(grid_of((int64_t)rows * I)), dim3(256), 0, s, part,

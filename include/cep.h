@@ -424,7 +424,8 @@ typedef struct {
  * largest sum of their two best keys are chosen.  A logit of -inf or NaN masks
  * its expert; a slot that no expert fills gets id -1 and coefficient 0.
  * Coefficients: CEP_SOFTMAX the softmax over all experts, CEP_SIGMOID the
- * sigmoid; with normalize over the chosen's sum (0 where that is 0). */
+ * sigmoid; with normalize over the chosen's sum (0 where that is 0).  Scores are
+ * float32: a sigmoid keeps its subnormal values and is 0 for logits below -104. */
 int cep_gate_topk(const cep_gate_desc *desc, const void *logits, const float *bias,
                   int32_t *topk_id, float *topk_w, hipStream_t s);
 

@@ -127,12 +127,17 @@ __device__ inline float logit(const GateArgs &a, int64_t row, int e) {
 }
 // 1 / (1 + 2^t), t = -l log2(e), with t's rounding error r put back as 2^r ~ 1 +
 // r ln(2): the exponential and reciprocal instructions are within one unit of
-// the last place.  Beyond +-90 it is 0 or 1.
+// the last place.  Past 2^125, where the reciprocal would be subnormal, both are
+// taken of 2^(t - 64) (an exact difference, beside which the 1 is nothing), and
+// the last factor keeps the steps of subnormal numbers: experts are told apart
+// down to where float32 has no smaller score (a logit of -104).
 __device__ inline float sigmoid(float l) {
   constexpr float kLog2e = 1.44269502f, kLog2eRest = 1.92596303e-8f;
-  const float c = fminf(fmaxf(-l, -90.0f), 90.0f), t = c * kLog2e;
+  const float c = fminf(fmaxf(-l, -90.0f), 105.0f), t = c * kLog2e;
   const float r = fmaf(c, kLog2eRest, fmaf(c, kLog2e, -t));
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t) * fmaf(r, 0.693147182f, 1.0f));
+  const bool far = t > 125.0f;
+  const float q = __builtin_amdgcn_exp2f(t - (far ? 64.0f : 0.0f)) * fmaf(r, 0.693147182f, 1.0f);
+  return __builtin_amdgcn_rcpf(1.0f + q) * (far ? 0x1p-64f : 1.0f);
 }
 
 // How groups are found: none; any size, through LDS; 32 experts, in eight lanes'

@@ -586,3 +586,34 @@ def test_operators_replay_in_a_graph():
         torch.cuda.synchronize()
         for n, t in o.items():
             assert torch.equal(t, eager[n]), (i, n)
+
+
+def _tail_check(logits, k, normalize):
+    """Scores near and below 2^-126, float32's least normal number: they come in
+    steps of 2^-149, each within one of them (and 2^-16) of the exact one."""
+    ids, w = _run_gate(logits, k, n_experts=logits.shape[1], score=cep.CEP_SIGMOID,
+                       normalize=int(normalize), scale=1.0)
+    l = logits.cpu().numpy()
+    rid, rw = R.gate(l, k, "sigmoid", normalize=normalize)
+    assert np.array_equal(ids, rid)
+    err = 2.0 ** -149
+    if normalize:  # of a coefficient's own score, and k of the sum's
+        total = R.gate(l, k, "sigmoid", normalize=False)[1].sum(1, keepdims=True)
+        err = err * (1 + k * rw) / (total - k * err)
+    assert np.all(np.abs(w - rw) <= 2.0 ** -16 * rw + err)
+
+
+@pytest.mark.parametrize("T", [1, 40, 4097])
+def test_gate_sigmoid_far_below_zero(T):
+    """Experts are told apart while float32 has steps between their scores (at
+    -100 a tenth of a logit is 2.6 of them), in rows with nothing above, too."""
+    l = -85 - 0.1 * torch.rand(T, 151, device="cuda", generator=_gen(T)).argsort(-1).float()
+    l[::2] = torch.where(l[::2] > -95, -float("inf"), l[::2])
+    for normalize in (True, False):
+        _tail_check(l, 8, normalize)
+
+
+def test_gate_sigmoid_ends_at_the_least_float():
+    l = torch.linspace(-84, -115, 256, device="cuda")  # equal scores: the lower expert
+    for lo in range(0, 256, 16):
+        _tail_check(l[None, lo:lo + 16].contiguous(), 16, False)

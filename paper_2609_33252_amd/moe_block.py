@@ -12,8 +12,10 @@ the experts take as they are.  A block of an expert-parallel job sends the other
 ranks' segments of the send buffer to them; here they are only packed.  The
 gate's projection is a plain product and goes to the library.
 
-``backward`` gives the gradients of the shared expert and of the norm's weight,
-for training these beside frozen routed experts.
+``backward`` gives the gradients of the shared expert's weights, the norm's weight
+and the block's input.  The routed experts and the gate have no gradients of
+their own here, but y reaches the output through them too: a program that trains
+the norm, or anything before the block, passes that part of the gradient of y in.
 
 Run ``python -m paper_2609_33252_amd.moe_block`` for a small block on cuda:0.
 """
@@ -130,11 +132,14 @@ class MoEBlock:
         cep.cep_combine(self.ctx, s)
         return routed.add_(self.shared_y[:T])
 
-    def backward(self, d_out, d_residual=None):
-        """Gradients of a forward(train=True) through the shared expert and the
-        norm: d_out bf16 [T][d] of the output, d_residual (bf16 or None) of the
-        updated residual.  Returns d_x (bf16, also the residual's), d_norm, and
-        the shared expert's three weight gradients."""
+    def backward(self, d_out, d_residual=None, d_y=None):
+        """Gradients of a forward(train=True): d_out bf16 [T][d] of the output,
+        d_residual (bf16 or None) of the updated residual, d_y (float32, bf16 or
+        None) what the paths of y through the routed experts and the gate add to
+        the gradient of y = ``self.y[:T]``.  Returns d_x (bf16, also the
+        residual's), d_norm, and the shared expert's three weight gradients.
+        d_x and d_norm are the output's gradients if d_y is complete; without it
+        they leave those paths out, as one addend of the gradients."""
         residual, y, pre = self.saved
         T, d, s = y.shape[0], self.d, torch.cuda.current_stream()
         ffn = cep.make_gated_ffn(rows=T, d_model=d, d_ff=self.d_shared)
@@ -142,8 +147,11 @@ class MoEBlock:
         dw = [torch.empty_like(w) for w in self.shared]
         cep.cep_gated_ffn_backward(ffn, d_out, y, *self.shared, pre, dy, *dw,
                                    self._ffn_space(ffn, True), stream=s)
+        if d_y is not None:
+            dy = dy.float().add_(d_y)  # not rounded again
         desc = cep.make_norm(rows=T, d=d, x_dtype=cep.CEP_BF16, res_dtype=cep.CEP_BF16,
-                             w_dtype=cep.CEP_F32, y_dtype=cep.CEP_BF16, eps=EPS)
+                             w_dtype=cep.CEP_F32, eps=EPS,
+                             y_dtype=cep.CEP_BF16 if d_y is None else cep.CEP_F32)
         ws = torch.empty(cep.cep_rms_norm_workspace(desc), dtype=torch.uint8, device=y.device)
         dx, d_norm = torch.empty_like(y), torch.empty_like(self.norm)
         cep.cep_rms_norm_backward(desc, residual, self.norm, dy, d_residual, dx, d_norm, ws,
@@ -175,7 +183,7 @@ def main():
         dx, d_norm, _ = block.backward(normal(T, d))
         torch.cuda.synchronize()
         print(f"{T} tokens: output rms {float(out.square().mean().sqrt()):.4f}, "
-              f"{int(block.plan[1])} rows sent, gradient rms of x "
+              f"{int(block.plan[1])} rows sent, gradient rms of x through the shared expert "
               f"{float(dx.float().square().mean().sqrt()):.6f}")
     block.close()
 

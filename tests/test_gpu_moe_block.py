@@ -173,3 +173,37 @@ def test_mxfp8_rows_need_quantised_experts():
         assert cep.cep_packed_expert_bytes(cep.make_config(w_dtype=w, **base)) == 0
     for w in (cep.CEP_FP8_E4M3_B128, cep.CEP_MXFP4):
         assert cep.cep_packed_expert_bytes(cep.make_config(w_dtype=w, **base)) > 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_block_gradients_of_every_path(dtype):
+    """With the gradient of y along the routed experts and the gate, the block's
+    gradients are those of its output: differentiated here as a whole, from the
+    updated residual, in float64."""
+    b, experts, n = _block(11, 1, 0)
+    T = 90
+    x, res, dout, dres = (n(T, b.d, std=1.0) for _ in range(4))
+    b.forward(x, res, train=True)
+    ids = b.ids[:T].long()
+
+    def routed(y):  # coefficients: the softmax over the chosen
+        w = torch.softmax((y @ b.gate.double()).gather(1, ids), 1)
+        out = torch.zeros_like(y)
+        for e in range(8):
+            at = torch.where(ids == e, w, 0.0).sum(1, keepdim=True)
+            out = out + at * R.gated_ffn(y, *(t[e] for t in experts))[3]
+        return out
+
+    y = b.y[:T].double().requires_grad_()
+    d_y, = torch.autograd.grad((routed(y) * dout.double()).sum(), y)
+    dx, d_norm, _ = b.backward(dout, dres, d_y=d_y.to(dtype))
+
+    s, norm = res.double().requires_grad_(), b.norm.double().requires_grad_()
+    y = s * torch.rsqrt((s * s).mean(-1, keepdim=True) + moe_block.EPS) * norm
+    out = routed(y) + R.gated_ffn(y, *b.shared)[3]
+    want = torch.autograd.grad((out * dout.double()).sum() + (s * dres.double()).sum(), (s, norm))
+    for got, ref in zip((dx, d_norm), want):
+        # six bf16 roundings of random signs at most: s, y, the hidden gradients,
+        # dy, d_y and dx
+        assert (got.double() - ref).norm() / ref.norm() < 6 * 2.0 ** -8 / 3 ** 0.5
+    b.close()

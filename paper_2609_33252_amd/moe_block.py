@@ -28,16 +28,35 @@ from . import cep
 EPS = 1e-6
 
 
+def _expect(name, t, device, dtypes, shape, dense=True):
+    """The operators get plain pointers: t has to be what they read."""
+    if (not isinstance(t, torch.Tensor) or t.device != device or t.dtype not in dtypes
+            or t.shape != shape or (dense and not t.is_contiguous())):
+        kinds = " or ".join(str(d).removeprefix("torch.") for d in dtypes)
+        raise ValueError(f"{name} must be a {'contiguous ' if dense else ''}{kinds} tensor of "
+                         f"shape {list(shape)} on {device}")
+
+
 class MoEBlock:
-    """weights: norm [d] float32, gate [d][n_experts], shared (w_gate, w_up
-    [d][d_shared], w_down [d_shared][d]) bf16, experts a cep_weights of this
-    rank's n_experts / n_ranks experts in w_dtype."""
+    """weights: norm [d] and gate [d][n_experts] float32, bias (CEP_SIGMOID)
+    [n_experts] float32, shared (w_gate, w_up [d][d_shared], w_down
+    [d_shared][d]) bf16, experts a cep_weights of this rank's n_experts / n_ranks
+    experts in w_dtype."""
 
     def __init__(self, *, d, d_ff, d_shared, n_experts, top_k, n_ranks, rank, max_tokens, norm,
                  gate, shared, experts, w_dtype, score=cep.CEP_SOFTMAX, bias=None, n_groups=0,
                  topk_groups=0):
         if n_experts % n_ranks or not 0 <= rank < n_ranks:
             raise ValueError("n_ranks must divide n_experts and hold rank")
+        dev, F32, BF16 = norm.device, (torch.float32,), (torch.bfloat16,)
+        _expect("norm", norm, dev, F32, (d,))
+        _expect("gate", gate, dev, F32, (d, n_experts), dense=False)  # torch's product reads it
+        if bias is not None:
+            _expect("bias", bias, dev, F32, (n_experts,))
+        if len(shared) != 3:
+            raise ValueError("shared must hold w_gate, w_up and w_down")
+        for w, shape in zip(shared, ((d, d_shared), (d, d_shared), (d_shared, d))):
+            _expect("a weight of shared", w, dev, BF16, shape)
         self.d, self.top_k, self.n_ranks, self.rank = d, top_k, n_ranks, rank
         self.max_tokens, self.d_shared = max_tokens, d_shared
         self.norm, self.gate, self.shared, self.bias = norm, gate, shared, bias
@@ -52,7 +71,6 @@ class MoEBlock:
                             max_replicas=1, max_tokens_per_replica=max_tokens, w_dtype=w_dtype,
                             x_dtype=self.row_dtype, n_streams=1),
             experts, None, torch.cuda.current_stream())
-        dev = norm.device
         T, sent = max_tokens, max_tokens * min(top_k, n_ranks)
 
         def buf(*shape, dtype=torch.bfloat16):
@@ -73,6 +91,7 @@ class MoEBlock:
                                dtype=torch.uint8)
         self.ffn_ws = buf(0, dtype=torch.uint8)
         self.generation = 0
+        self.saved = None  # of the last forward pass, if that was a training one
 
     def _dispatch_desc(self, T):
         return cep.make_dispatch(rows=T, top_k=self.top_k, n_ranks=self.n_ranks,
@@ -87,11 +106,13 @@ class MoEBlock:
 
     def forward(self, x, residual, train=False):
         """x [T][d] (float32 or bf16: the block before's output), residual [T][d]
-        bf16, updated in place.  Returns this rank's part of the block's output,
-        float32 [T][d], valid until the next call."""
+        bf16, updated in place; both contiguous.  Returns this rank's part of the
+        block's output, float32 [T][d], valid until the next call."""
         T, d, s = x.shape[0], self.d, torch.cuda.current_stream()
         if T > self.max_tokens:
             raise ValueError(f"{T} tokens, the block holds {self.max_tokens}")
+        _expect("x", x, self.y.device, (torch.float32, torch.bfloat16), (T, d))
+        _expect("residual", residual, self.y.device, (torch.bfloat16,), (T, d))
         mx = self.row_dtype == cep.CEP_MXFP8
         desc = cep.make_norm(rows=T, d=d, res_dtype=cep.CEP_BF16, w_dtype=cep.CEP_F32,
                              x_dtype=cep.CEP_F32 if x.dtype == torch.float32 else cep.CEP_BF16,
@@ -140,8 +161,16 @@ class MoEBlock:
         residual's), d_norm, and the shared expert's three weight gradients.
         d_x and d_norm are the output's gradients if d_y is complete; without it
         they leave those paths out, as one addend of the gradients."""
+        if self.saved is None:
+            raise ValueError("backward without a forward(train=True) before it")
         residual, y, pre = self.saved
         T, d, s = y.shape[0], self.d, torch.cuda.current_stream()
+        BF16 = (torch.bfloat16,)
+        _expect("d_out", d_out, y.device, BF16, (T, d))
+        if d_residual is not None:
+            _expect("d_residual", d_residual, y.device, BF16, (T, d))
+        if d_y is not None:
+            _expect("d_y", d_y, y.device, BF16 + (torch.float32,), (T, d))
         ffn = cep.make_gated_ffn(rows=T, d_model=d, d_ff=self.d_shared)
         dy = torch.empty_like(y)
         dw = [torch.empty_like(w) for w in self.shared]

@@ -207,3 +207,53 @@ def test_block_gradients_of_every_path(dtype):
         # dy, d_y and dx
         assert (got.double() - ref).norm() / ref.norm() < 6 * 2.0 ** -8 / 3 ** 0.5
     b.close()
+
+
+def test_block_refuses_what_it_would_misread():
+    b, _, n = _block(13, 1, 0, T=40)
+    T, d = 24, b.d
+    x, res, dout = n(T, d), n(T, d), n(T, d)
+    wide = n(T, 2 * d)
+    kept = wide.clone()
+    for bad in (x.half(), x.double(), x[:, :d - 1], wide[:, :d], x[None], x.cpu(),
+                x.t().contiguous().t()):
+        with pytest.raises(ValueError, match="^x "):
+            b.forward(bad, res)
+    for bad in (res.float(), res.half(), wide[:, :d], res[:T - 1], res.cpu()):
+        with pytest.raises(ValueError, match="residual"):
+            b.forward(x, bad)
+    b.forward(x, res)
+    with pytest.raises(ValueError, match="train"):
+        b.backward(dout)
+    b.forward(x, res, train=True)
+    for bad in (dout.float(), dout.half(), wide[:, :d], dout[:T - 1], dout.cpu()):
+        with pytest.raises(ValueError, match="d_out"):
+            b.backward(bad)
+        with pytest.raises(ValueError, match="d_residual"):
+            b.backward(dout, bad)
+    for bad in (dout.half(), wide[:, :d], dout[:T - 1], dout.cpu()):
+        with pytest.raises(ValueError, match="d_y"):
+            b.backward(dout, None, bad)
+    b.backward(dout, res)
+    torch.cuda.synchronize()
+    assert torch.equal(wide, kept)
+    b.close()
+
+
+@pytest.mark.parametrize("name,wrong", [
+    ("norm", lambda t: t.bfloat16()), ("norm", lambda t: t[:-1]), ("gate", lambda t: t[:, :4]),
+    ("gate", lambda t: t.bfloat16()), ("bias", lambda t: t.double()), ("bias", lambda t: t[:7]),
+    ("bias", lambda t: t.repeat(2)[::2]), ("shared", lambda t: (t[0].float(), *t[1:])),
+    ("shared", lambda t: (t[0], t[1], t[2].t())), ("shared", lambda t: t[:2])])
+def test_block_refuses_weights_it_would_misread(name, wrong):
+    d, I, E = 256, 128, 8
+    g = torch.Generator(device="cuda").manual_seed(0)
+    n = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()
+    a = dict(norm=torch.ones(d, device="cuda"), gate=n(d, E).float(), bias=n(E).float(),
+             shared=(n(d, 64), n(d, 64), n(64, d)))
+    experts = [n(E, d, I), n(E, d, I), n(E, I, d)]
+    a[name] = wrong(a[name])
+    with pytest.raises(ValueError, match=name):
+        moe_block.MoEBlock(d=d, d_ff=I, d_shared=64, n_experts=E, top_k=2, n_ranks=1, rank=0,
+                           max_tokens=16, experts=cep.make_weights(*experts),
+                           w_dtype=cep.CEP_BF16, score=cep.CEP_SIGMOID, **a)

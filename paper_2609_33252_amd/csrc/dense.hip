@@ -22,7 +22,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 enum Epilogue {
   kStore,   // bf16 to out0
   kStore2,  // two products over the same A: bf16 to out0 and out1
-  kSwiGlu,  // two products g, u: h = silu(g) u to out0, g and u to pre
+  kSwiGlu,  // two products g, u: h = silu(g) u to out0 (what that rounds off to out1),
+            // g and u to pre
   kGrad     // dh: with g, u from pre, [dg | du] to out0 and h to out1
 };
 constexpr bool is_dual(int epi) { return epi == kStore2 || epi == kSwiGlu; }
@@ -31,7 +32,7 @@ struct DenseArgs {
   const __bf16 *A, *B0, *B1;
   int64_t lda, ldb;
   int M, N, K;
-  int segs;       // K segments: A advances by K columns, B0 then B1 (dx)
+  int segs;       // K segments: A advances by K columns, B0 then B1 (dx; h in two terms)
   __bf16 *out0, *out1;
   int64_t ldo;
   float *pre;     // [M][2][N]
@@ -56,6 +57,14 @@ __device__ inline void finish(const DenseArgs &a, int64_t m, int n, const f32x4 
 #pragma unroll
     for (int r = 0; r < 4; ++r) h[r] = v[r] * sigma(v[r]) * w[r];
     store_bf16(a.out0 + m * a.ldo + n, h);
+    if (a.out1) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float hi = (float)(__bf16)h[r];
+        h[r] = __builtin_isinf(hi) ? 0.f : h[r] - hi;
+      }
+      store_bf16(a.out1 + m * a.ldo + n, h);
+    }
     if (a.pre) {
       *(f32x4 *)(a.pre + m * 2 * a.N + n) = v;
       *(f32x4 *)(a.pre + m * 2 * a.N + a.N + n) = w;
@@ -615,9 +624,19 @@ const char *bad_desc(const cep_gated_ffn_desc *d) {
   return nullptr;
 }
 
-// [dg | du] and h of the backward pass, h of the forward one
+// bf16 terms of h in the forward pass.  Up to 64 rows a call is bound by its
+// weights, and h goes to the down projection as hi + lo (16 bits of mantissa), as
+// two segments of K over the same weights, so that of y only its own rounding is
+// left (relative RMS error 1.7e-3, 2.4e-3 with one term).  us with two and one: 33
+// rows of 4096 x 2048 24.2, 22.8; 61 of 7168 x 2048 36.1, 32.9; 54 of 4096 x 264
+// 19.9, 17.5.  Larger calls round h once: bound by matrix instructions, they would
+// pay a third more of them.
+constexpr int kTwoTermRows = 64;
+int hidden_terms(int rows) { return rows <= kTwoTermRows ? 2 : 1; }
+
+// [dg | du] and h of the backward pass, the terms of h of the forward one
 size_t hidden_bytes(const cep_gated_ffn_desc *d, int backward) {
-  return align_up((size_t)d->rows * d->d_ff * (backward ? 6 : 2), 256);
+  return align_up((size_t)d->rows * d->d_ff * (backward ? 6 : 2 * hidden_terms(d->rows)), 256);
 }
 
 }  // namespace
@@ -635,7 +654,9 @@ CEP_API size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *d, int backward
   if (backward)
     part = std::max({part_bytes(T, I, D, false), part_bytes(T, D, 2 * I, false),
                      part_bytes(D, I, T, true), part_bytes(I, D, T, false)});
-  if (!p.use) part = std::max({part, part_bytes(T, I, D, true), part_bytes(T, D, I, false)});
+  if (!p.use)
+    part = std::max({part, part_bytes(T, I, D, true),
+                     part_bytes(T, D, I * hidden_terms(T), false)});
   const size_t rows = p.use ? rows_workspace(p, T, D, I) : 0;
   return std::max(std::max<size_t>(hidden_bytes(d, backward) + part, rows), (size_t)256);
 }
@@ -667,16 +688,18 @@ CEP_API int cep_gated_ffn(const cep_gated_ffn_desc *d, const void *x, const void
   a.lda = d->ld_x ? d->ld_x : D;
   a.ldb = I;
   a.M = T, a.N = I, a.K = D, a.segs = 1;
+  const int terms = hidden_terms(T);
   a.out0 = (__bf16 *)workspace;
-  a.ldo = I;
+  if (terms == 2) a.out1 = a.out0 + I;
+  a.ldo = terms * I;
   a.pre = preact;
   float *part = (float *)((uint8_t *)workspace + hidden_bytes(d, 0));
   launch_dense<true, false, kSwiGlu>(a, part, s);
   DenseArgs b{};
   b.A = (const __bf16 *)workspace;
-  b.B0 = (const __bf16 *)w_down;
-  b.lda = I, b.ldb = D;
-  b.M = T, b.N = D, b.K = I, b.segs = 1;
+  b.B0 = b.B1 = (const __bf16 *)w_down;
+  b.lda = terms * I, b.ldb = D;
+  b.M = T, b.N = D, b.K = I, b.segs = terms;
   b.out0 = (__bf16 *)y;
   b.ldo = d->ld_y ? d->ld_y : D;
   launch_dense<true, false, kStore>(b, part, s);

@@ -14,7 +14,7 @@
 //
 // The hidden row is kept as two bf16 terms, h = hi + lo (16 bits of mantissa):
 // the second costs matrix instructions that a weight-bound product has to
-// spare, and with so few rows the one rounding of h would show in y.
+// spare, and the one rounding of h would show in y.
 #include "block_ops.h"
 #include "dense.h"
 #include "gemm_common.h"
@@ -284,9 +284,10 @@ unsigned grid_of(int64_t elements) { return (unsigned)((elements / 4 + 255) / 25
 }  // namespace
 
 // Rows up to which the weights are streamed.  Above it the tiled product with
-// K shares is as fast (both products, us here and tiled; d 4096, d_ff 2048: 1
-// row 15.8, 19.9; 16 rows 19.2, 21.3; 32 rows 21.3, 22.7; 33 rows 23.7, 22.5;
-// d 7168: 16 rows 27.1, 26.9; 32 rows 30.8, 29.0; 64 rows 37.5, 33.5).
+// K shares is as fast (both products, us here and tiled, h in two terms; d 4096,
+// d_ff 2048: 1 row 15.9, 21.4; 16 rows 19.0, 22.4; 32 rows 21.1, 23.8; 33 rows 23.8,
+// 24.0; d 7168: 16 rows 27.2, 29.4; 32 rows 30.3, 31.4; 64 rows 37.0, 35.8; 32 rows
+// of 256 x 128 11.3, 10.3).
 constexpr int kRowsMost = 32;
 
 RowsPlan rows_plan(int rows, int d, int I) {

@@ -617,3 +617,24 @@ def test_gate_sigmoid_ends_at_the_least_float():
     l = torch.linspace(-84, -115, 256, device="cuda")  # equal scores: the lower expert
     for lo in range(0, 256, 16):
         _tail_check(l[None, lo:lo + 16].contiguous(), 16, False)
+
+
+FEW = [(1, 512, 2048), (8, 1000, 504), (16, 4096, 2048), (17, 2304, 1408), (31, 1000, 504),
+       (32, 2304, 1408), (33, 1000, 504), (48, 776, 2056), (63, 512, 128), (64, 2304, 1408)]
+
+
+@pytest.mark.parametrize("T,d,I", FEW)
+def test_ffn_of_few_rows_rounds_only_its_output(T, d, I):
+    """Up to 64 rows the hidden row is two bf16 terms, so y is the exact result
+    rounded to bf16 but where that lies next to a tie.  Two terms leave 2^-16 of
+    h, and the sums less, which moves y by less than 2^-13 of its size, 1/32 of
+    the distance of two bf16 numbers; an h of one term moves it by a quarter of
+    that distance on average."""
+    x, wg, wu, wd, _ = _ffn_inputs(T, d, I, T + d + 7)
+    desc = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc), dtype=torch.uint8, device="cuda")
+    exact = R.gated_ffn(x, wg, wu, wd)[3].to(torch.bfloat16)
+    for pre in (None, torch.empty(T, 2, I, device="cuda")):
+        y = torch.empty_like(x)
+        cep.cep_gated_ffn(desc, x, wg, wu, wd, y, ws, preact=pre)
+        assert (y != exact).double().mean() < 0.1

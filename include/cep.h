@@ -466,11 +466,12 @@ typedef struct {
  * accumulation.  x [rows][d_model]; w_gate, w_up [d_model][d_ff]; w_down
  * [d_ff][d_model] (the math orientation of cep_weights, read as they are);
  * y [rows][d_model].  For the second product the hidden row is two bf16 terms (16
- * bits of mantissa) up to 64 rows, and rounded to bf16 once above.  preact (NULL: not kept) gets x Wg and x Wu, float32
- * [rows][2][d_ff], for cep_gated_ffn_backward.  All pointers 16-byte aligned;
- * y may not overlap x.  workspace: cep_gated_ffn_workspace(desc, 0) bytes for
- * this call alone, (desc, 1) bytes for this call and the backward one (one after
- * the other; nothing in it is kept between them). */
+ * bits of mantissa) up to 64 rows, and rounded to bf16 once above.  preact (NULL:
+ * not kept) gets x Wg and x Wu, float32 [rows][2][d_ff], for
+ * cep_gated_ffn_backward.  All pointers 16-byte aligned; y may not overlap x.
+ * workspace: cep_gated_ffn_workspace(desc, 0) bytes for this call alone, (desc, 1)
+ * bytes for this call and the backward one (one after the other; nothing in it is
+ * kept between them). */
 size_t cep_gated_ffn_workspace(const cep_gated_ffn_desc *desc, int backward);
 int cep_gated_ffn(const cep_gated_ffn_desc *desc, const void *x, const void *w_gate,
                   const void *w_up, const void *w_down, void *y, float *preact, void *workspace,

@@ -638,3 +638,39 @@ def test_ffn_of_few_rows_rounds_only_its_output(T, d, I):
         y = torch.empty_like(x)
         cep.cep_gated_ffn(desc, x, wg, wu, wd, y, ws, preact=pre)
         assert (y != exact).double().mean() < 0.1
+
+
+def _biased(g, T, E, groups):
+    """Logits and a bias of the size of the scores, whose keys (scores + bias)
+    lie 0.18 / E apart at least and the sums of a group's two best 1e-5; every
+    eighth row has one group left, every other expert, or a few."""
+    n = 16 * T + 64
+    key = torch.rand(n, E, device="cuda", generator=g).argsort(-1).double()
+    key = 0.35 + 0.3 * (key + 0.4 * torch.rand(n, E, device="cuda", generator=g).double()) / E
+    bias = (0.6 * torch.rand(E, device="cuda", generator=g) - 0.3).float()
+    p = key - bias.double()
+    l = torch.log(p / (1 - p)).float()
+    l[3::8, E // groups:] = -float("inf")
+    l[4::8, 1::2] = -float("inf")
+    l[5::8, 3:] = float("nan")
+    key = torch.sigmoid(l.double()) + bias.double()
+    key = key.masked_fill(~torch.isfinite(l), -float("inf")).view(n, groups, -1)
+    two = key.topk(min(2, E // groups), -1)[0]
+    total = two.masked_fill(two == -float("inf"), 0.0).sum(-1)
+    total = total.masked_fill(two[..., 0] == -float("inf"), -float("inf"))
+    gap = total.sort(-1)[0].diff(dim=-1)  # NaN between two groups with nothing
+    l = l[~(gap <= 1e-5).any(-1)]
+    assert len(l) >= T
+    return l[:T].contiguous(), bias
+
+
+@pytest.mark.parametrize("T", [1, 7, 4097])
+@pytest.mark.parametrize("E,groups,topg,k", [(256, 8, 4, 8), (256, 8, 1, 16), (160, 5, 2, 6),
+                                             (64, 2, 1, 1), (96, 4, 2, 6), (160, 8, 3, 6),
+                                             (512, 64, 7, 8), (1024, 4, 1, 8), (160, 1, 1, 8)])
+def test_gate_sigmoid_bias(T, E, groups, topg, k):
+    """The bias counts in the choice, of groups too, and not in the coefficients."""
+    l, bias = _biased(_gen(E + groups + T), min(T, 48), E, groups)
+    l = l[torch.arange(T, device="cuda") % len(l)]
+    _gate_check(l, k, "sigmoid", bias, groups, topg)
+    _gate_check(l, k, "sigmoid", bias, groups, topg, normalize=False, scale=0.5)

@@ -674,3 +674,24 @@ def test_gate_sigmoid_bias(T, E, groups, topg, k):
     l = l[torch.arange(T, device="cuda") % len(l)]
     _gate_check(l, k, "sigmoid", bias, groups, topg)
     _gate_check(l, k, "sigmoid", bias, groups, topg, normalize=False, scale=0.5)
+
+
+@pytest.mark.parametrize("rows,d,x,res,y,q,pad", [
+    # both sides of the row count that decides the threads of a row
+    (256, 2304, F32, BF16, BF16, True, 0), (257, 2304, F32, BF16, BF16, True, 0),
+    (300, 4096, BF16, BF16, BF16, True, 0), (257, 4088, BF16, F32, F32, False, 3),
+    (300, 6144, F32, BF16, BF16, True, 32), (256, 8191, BF16, BF16, BF16, False, 1),
+    (257, 8191, BF16, BF16, BF16, False, 1), (259, 7168, BF16, None, None, True, 0),
+])
+def test_norm_of_many_wide_rows(rows, d, x, res, y, q, pad):
+    test_norm(rows, d, x, res, y, q, pad)
+
+
+@pytest.mark.parametrize("rows,d,s,dres,dy,wdt,pad", [
+    # rows that are not all bf16, several to a block
+    (1030, 4096, F32, True, F32, F32, 0), (600, 3001, BF16, True, F32, F32, 5),
+    (1100, 7168, F32, True, BF16, F32, 8), (513, 8191, F32, False, F32, BF16, 0),
+    (700, 2048, F32, True, F32, F32, 0), (2100, 500, BF16, False, F32, F32, 0),
+])
+def test_norm_backward_of_many_wide_rows(rows, d, s, dres, dy, wdt, pad):
+    test_norm_backward(rows, d, s, dres, dy, wdt, pad)

@@ -695,3 +695,27 @@ def test_norm_of_many_wide_rows(rows, d, x, res, y, q, pad):
 ])
 def test_norm_backward_of_many_wide_rows(rows, d, s, dres, dy, wdt, pad):
     test_norm_backward(rows, d, s, dres, dy, wdt, pad)
+
+
+@pytest.mark.parametrize("T,d,I", FEW)
+def test_ffn_forward_of_few_rows(T, d, I):
+    for pad in (0, 8):
+        test_ffn_forward(T, d, I, pad)
+
+
+@pytest.mark.parametrize("T", [12, 32, 33, 64])
+def test_ffn_of_few_rows_keeps_them_apart(T):
+    d, I = 264, 136
+    x, wg, wu, wd, _ = _ffn_inputs(T, d, I, T)
+    desc = cep.make_gated_ffn(rows=T, d_model=d, d_ff=I)
+    ws = torch.empty(cep.cep_gated_ffn_workspace(desc), dtype=torch.uint8, device="cuda")
+    y, x2, y2 = torch.empty_like(x), x.clone(), torch.empty_like(x)
+    x2[3], x2[7, 7], x2[T - 1] = float("nan"), float("inf"), 0.0
+    for pre in (None, torch.empty(T, 2, I, device="cuda")):
+        cep.cep_gated_ffn(desc, x, wg, wu, wd, y, ws, preact=pre)
+        cep.cep_gated_ffn(desc, x2, wg, wu, wd, y2, ws, preact=pre)
+        same = torch.ones(T, dtype=torch.bool, device="cuda")
+        same[[3, 7, T - 1]] = False
+        assert torch.equal(y[same], y2[same])
+        assert torch.isnan(y2[3]).all() and (y2[T - 1] == 0).all()
+        assert not torch.isfinite(y2[7]).all()

@@ -176,3 +176,17 @@ def test_ffn_gradient_formula_agrees_with_differences():
         v = r(*a[name].shape)
         f = lambda z: (R.gated_ffn(**{**a, name: z})[3] * dy).sum()
         assert abs(_slope(f, a[name], v) - float((grads[key] * v).sum())) < 1e-6, name
+
+
+@pytest.mark.parametrize("rows", [(1 << 21) + 1, 2 ** 31 - 1])
+def test_rows_beyond_the_limit_are_refused(rows):
+    _refused(cep.CEP_EINVAL, cep.cep_rms_norm, _norm(rows=rows), PTR, PTR, y=PTR)
+    _refused(cep.CEP_EINVAL, cep.cep_rms_norm_backward, _norm(rows=rows), PTR, PTR, PTR, None, PTR,
+             PTR, None)
+    _refused(cep.CEP_EINVAL, cep.cep_gate_topk, _gate(rows=rows), PTR, None, PTR, PTR)
+    _refused(cep.CEP_EINVAL, cep.cep_dispatch, _send(rows=rows), *[PTR] * 8, None)
+    _refused(cep.CEP_EINVAL, cep.cep_gated_ffn, _ffn(rows=rows), *[PTR] * 5, None)
+    _refused(cep.CEP_EINVAL, cep.cep_gated_ffn_backward, _ffn(rows=rows), *[PTR] * 10, None)
+    for f, desc in ((cep.cep_rms_norm_workspace, _norm), (cep.cep_dispatch_workspace, _send),
+                    (cep.cep_gated_ffn_workspace, _ffn)):
+        assert f(desc(rows=rows)) == 0 and f(desc(rows=1 << 21)) > 0

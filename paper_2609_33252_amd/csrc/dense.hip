@@ -140,8 +140,8 @@ __device__ inline int piece_of(int items, int x) { return items / 8 + (x < items
 //   row contiguous: [64 k][row], chunk pair p (16 rows) of line k at p ^ f(k);
 //     a fragment is two transposing 8-byte reads of four lines of k
 //
-// Measured (kernel alone, 256-wide): 8192 x 7168 x 2 x 2048 with SwiGLU 321 us,
-// 1.50 PFLOP/s, the matrix pipe busy 65 % of the time at 2.1 GHz.  Bound inside
+// Measured (kernel alone, 256-wide): 8192 x 7168 x 2 x 2048 with SwiGLU 321 to 329
+// us from machine to machine, 1.46 to 1.50 PFLOP/s, the matrix pipe busy 65 % of the time at 2.1 GHz.  Bound inside
 // the CU: without the loads the pass is 15 % shorter, without the LDS reads 18 %,
 // with neither 31 %, with every load an L2 hit 4 %.
 template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
@@ -468,6 +468,9 @@ int64_t dense_tiles(int t, int M, int N) {
 //     64 steps 64), 1.2 a round of several (1024 tiles of 64 steps 146)
 //   the shares' second launch: 4, and their sums at 9 TB/s (three of 777 x 5120: 9)
 // Shares have six steps at least and fit one round; they have to win by a tenth.
+// Layouts and epilogues are not told apart: of 512 128-wide tiles of 64 steps,
+// estimated at 67, dh (4095 x 2048 x 4096) takes 96 with its reads of g and u, and
+// dWd 76.
 // (A 256 x 128 tile, in four or eight waves, was no faster than two 128-wide
 // ones: 4095 x 2048 x 4096 118 and 108 against 104.)
 DensePlan dense_plan(int M, int n, int K, bool dual) {

@@ -1,5 +1,10 @@
 // Dense gated feed-forward of few rows for gfx950: the weights are streamed
-// once, at HBM rate, and the rows ride along.
+// once, and the rows ride along.
+//
+// Measured: one row of 4096 x 2048 (50 MB of weights) 17.7 us from HBM (forty sets
+// of weights in turn), 15.6 with the weights in the last-level cache (three sets):
+// of the three launches' 7.7, 5.8 and 1.8 us the start and end are the larger part,
+// not memory's rate.
 //
 // A workgroup takes all rows (up to 32), 128 columns (64 of the gate and the
 // same 64 of the up projection, or 128 of the down projection) and a share of

@@ -331,12 +331,15 @@ void launch_gate(const GateArgs &a, hipStream_t s) {
 
 // Few rows: a wave a row, four experts a lane, for the latency of one row;
 // more rows: eight lanes a row, which takes fewer instructions a row.  256
-// experts, k 8, us a call of 64 / 2048 / 4096 / 65536 rows: softmax 3.7 / 4.0 /
-// 5.2 / 41.5 with a wave, 4.3 / 4.4 / 4.5 / 16.3 with eight lanes; sigmoid in
-// eight groups of 32 4.3 / 4.9 / 6.5 / 55.8 and 5.5 / 5.8 / 5.8 / 24.0; 96 in
-// four of 24, through LDS, 6.2 / 6.3 / 8.0 / 66.8 and 7.7 / 8.0 / 8.1 / 29.9.
-// (Groups of 32 through LDS, as those of any size are: 6.7 and 6.7 with a wave,
-// 38.3 us for 65536 rows with eight lanes.)
+// experts, k 8, us a call of 64 / 2048 / 4096 / 65536 rows: softmax 4.0 / 4.2 /
+// 5.3 / 43 with a wave, 4.0 / 4.3 / 4.4 / 16.4 with eight lanes; sigmoid in
+// eight groups of 32 4.4 / 5.1 / 6.8 / 58 and 5.8 / 6.1 / 6.1 / 26; 96 in
+// four of 24, through LDS, 6.6 / 6.5 / 8.4 / 72 and 7.9 / 8.3 / 8.4 / 31.
+// (Groups of 32 through LDS, as those of any size are: 38 us for 65536 rows with
+// eight lanes, 24 so at the time.)  129 to 160 experts have 20 a lane: 65536 rows
+// of 160 11.8 us, 15.4 with 32 a lane; sigmoid 15.2, 21.4.  Above 256 every row
+// takes a wave: 65536 rows of 384 81 us, of 1024 152, where their bytes take 20
+// and 55.
 template <int KM>
 void launch_by_experts(const GateArgs &a, hipStream_t s) {
   if (a.E <= 256 && a.rows <= (a.groups > 1 && a.E != 32 * a.groups ? 4096 : 2048)) launch_gate<64, 4, KM>(a, s);

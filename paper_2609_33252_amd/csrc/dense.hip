@@ -141,9 +141,10 @@ __device__ inline int piece_of(int items, int x) { return items / 8 + (x < items
 //     a fragment is two transposing 8-byte reads of four lines of k
 //
 // Measured (kernel alone, 256-wide): 8192 x 7168 x 2 x 2048 with SwiGLU 321 to 329
-// us from machine to machine, 1.46 to 1.50 PFLOP/s, the matrix pipe busy 65 % of the time at 2.1 GHz.  Bound inside
-// the CU: without the loads the pass is 15 % shorter, without the LDS reads 18 %,
-// with neither 31 %, with every load an L2 hit 4 %.
+// us from machine to machine, 1.46 to 1.50 PFLOP/s, the matrix pipe busy 65 % of
+// the time at 2.1 GHz.  Bound inside the CU: without the loads the pass is 15 %
+// shorter, without the LDS reads 18 %, with neither 31 %, with every load an L2
+// hit 4 %.
 template <int HALF, int WM, int WN, bool A_K, bool B_K, int EPI>
 __device__ inline void dense_tile(const DenseArgs &a, int x, int at, uint8_t *lds) {
   constexpr bool DUAL = is_dual(EPI);

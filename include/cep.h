@@ -343,9 +343,10 @@ int cep_ffn_noalloc(cep_ctx *ctx, int replica, int n_rows, int n_pairs, const in
 
 /* ------------------------------------------------------------------------
  * Operators around the routed experts of one MoE block: the norm before the
- * gate, the gate's choice, the packing of tokens per expert-parallel rank, and
- * a dense gated feed-forward (a shared expert), with gradients where the
- * operator's own inputs are trained.
+ * gate, the gate's choice, the packing of tokens per expert-parallel rank, a
+ * dense gated feed-forward (a shared expert), and the sort by expert with a product
+ * per expert and the way back, with gradients where the operator's own inputs are
+ * trained.
  *
  * They need no context.  Work is enqueued on stream s of the current device
  * and nothing is allocated: an operator that needs scratch takes it from the
@@ -429,6 +430,18 @@ typedef struct {
 int cep_gate_topk(const cep_gate_desc *desc, const void *logits, const float *bias,
                   int32_t *topk_id, float *topk_w, hipStream_t s);
 
+/* Gradient of cep_gate_topk: from the forward call's logits and topk_id and the
+ * gradient d_topk_w [rows][top_k] (float32) of its coefficients, d_logits
+ * [rows][n_experts] (type and stride of the logits, which it may not overlap;
+ * every element is written).  The choice itself has no gradient: experts outside
+ * topk_id take part only through the softmax's sum without normalize.  Slots with
+ * an id outside [0, n_experts) are empty: their d_topk_w is not used.  Masked
+ * experts (a logit of -inf or NaN) and rows whose coefficients are all 0 get 0.
+ * desc as in the forward call; its groups and a bias shape the choice only and
+ * are not used. */
+int cep_gate_topk_backward(const cep_gate_desc *desc, const void *logits, const int32_t *topk_id,
+                           const float *d_topk_w, void *d_logits, hipStream_t s);
+
 typedef struct {
   int rows;              /* 0..2^21                                           */
   int top_k;             /* 1..16                                             */
@@ -486,6 +499,124 @@ int cep_gated_ffn_backward(const cep_gated_ffn_desc *desc, const void *dy, const
                            const void *w_gate, const void *w_up, const void *w_down,
                            const float *preact, void *dx, void *dw_gate, void *dw_up,
                            void *dw_down, void *workspace, size_t workspace_bytes, hipStream_t s);
+
+/* Sorting by expert, the products between and the way back are the routed experts
+ * in a form that can be trained (moe_block.RoutedExperts runs them together):
+ *   cep_expert_sort     each token's rows to its experts' segments
+ *   cep_linear          a product per segment
+ *   cep_expert_unsort   the experts' rows back, weighted and summed */
+
+typedef struct {
+  int rows;              /* tokens, 0..2^21                                   */
+  int top_k;             /* 1..16                                             */
+  int n_experts;         /* 1..1024                                           */
+  int capacity;          /* sorted rows that pair and out_x hold, >= rows *
+                            top_k                                             */
+  int64_t row_bytes;     /* 1..131072                                         */
+  int64_t ld_x;          /* row stride of x in bytes                          */
+} cep_expert_sort_desc;
+
+/* Sorts routed tokens by expert: a pair (token t, slot j) is flat index t * top_k
+ * + j, and the pairs of expert 0 come first, those of one expert in their order.
+ * topk_id [rows][top_k]: expert of each pair, -1: empty slot (a remote one).
+ * Outputs: plan [n_experts + 2] = segment offsets [n_experts + 1] in sorted rows
+ * (the offsets of cep_linear), then the number of ids outside [-1, n_experts)
+ * (such slots count as empty); pair: the flat index of each sorted row; place
+ * [rows][top_k]: the sorted row of each pair, -1 for an empty slot; out_x: row
+ * x[t] of each sorted row, dense rows of row_bytes bytes.  x and out_x may both be
+ * NULL: the order alone.  pair and out_x past the last segment are left as they
+ * are.  Its gradient, each token's sum over its sorted rows' gradients, is
+ * cep_expert_unsort without weights. */
+size_t cep_expert_sort_workspace(const cep_expert_sort_desc *desc);
+int cep_expert_sort(const cep_expert_sort_desc *desc, const int32_t *topk_id, const void *x,
+                    int32_t *plan, int32_t *pair, int32_t *place, void *out_x, void *workspace,
+                    size_t workspace_bytes, hipStream_t s);
+
+typedef struct {
+  int rows;              /* tokens, 0..2^21                                   */
+  int top_k;             /* 1..16                                             */
+  int d;                 /* 1..32768                                          */
+  int sorted_rows;       /* rows that ys has, >= 0                            */
+  int ys_dtype, res_dtype, y_dtype;  /* CEP_F32 or CEP_BF16                   */
+  int64_t ld_ys;         /* row strides in elements: ys and dys;              */
+  int64_t ld_res;        /*   residual;                                       */
+  int64_t ld_y;          /*   y and dy                                        */
+} cep_expert_unsort_desc;
+
+/* The way back: y[t] = residual[t] + sum over slots j of w[t][j] ys[place[t][j]],
+ * summed in float32 in slot order and rounded once.  ys [sorted_rows][d]; place
+ * [rows][top_k] as cep_expert_sort writes it: a slot with a place outside [0,
+ * sorted_rows) is empty, and its weight not used; w [rows][top_k] float32 (NULL:
+ * ones); residual (NULL: none; may be y itself if types and strides agree).  A
+ * token without a filled slot gets its residual, or 0. */
+int cep_expert_unsort(const cep_expert_unsort_desc *desc, const void *ys, const int32_t *place,
+                      const float *w, const void *residual, void *y, hipStream_t s);
+
+/* Its gradient: from dy (y_dtype) and the forward call's ys, place and w, dys
+ * (ys_dtype): row place[t][j] gets w[t][j] dy[t], rows that are no slot's place are
+ * left as they are; dw [rows][top_k] float32: the product of dy[t] and ys[place], 0
+ * for an empty slot.  dys or dw may be NULL, ys too without dw.  dys may be ys
+ * itself.  The residual's gradient is dy.  A sorted row is the place of at most one
+ * pair. */
+int cep_expert_unsort_backward(const cep_expert_unsort_desc *desc, const void *dy, const void *ys,
+                               const int32_t *place, const float *w, void *dys, float *dw,
+                               hipStream_t s);
+
+enum cep_act {
+  CEP_IDENTITY = 0,
+  CEP_RELU = 1,
+  CEP_SILU = 2,
+  CEP_GELU = 3,          /* z Phi(z), Phi the normal distribution             */
+  CEP_GELU_TANH = 4      /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+};
+
+typedef struct {
+  int rows;              /* 0..2^21                                           */
+  int d_in, d_out;       /* multiples of 8, 8..32768                          */
+  int n_groups;          /* 0: one weight; 1..1024: one per group of rows     */
+  int act;               /* cep_act                                           */
+  int y_dtype, res_dtype, dx_dtype, dw_dtype;  /* CEP_F32 or CEP_BF16         */
+  int64_t ld_x;          /* row strides in elements, multiples of 8, up to    */
+  int64_t ld_y;          /*   2^21: x; y and dy; mul and dmul; residual;      */
+  int64_t ld_mul;        /*   dx and dx_add                                   */
+  int64_t ld_res, ld_dx;
+} cep_linear_desc;
+
+/* Matrix product with an epilogue, bf16 with float32 accumulation:
+ *   z = x W + bias;  y = act(z) * mul + residual       (in float32)
+ * x [rows][d_in] bf16; w [d_in][d_out] bf16 (the math orientation of cep_weights,
+ * read as it is); bias [d_out] float32, mul [rows][d_out] bf16, residual
+ * [rows][d_out] (res_dtype; may be y itself if types and strides agree), each may
+ * be NULL.  y (y_dtype) may not overlap x.  preact (NULL: not kept) gets z, float32
+ * [rows][d_out], for cep_linear_backward.
+ * With groups, w is [n_groups][d_in][d_out] and bias [n_groups][d_out], and offsets,
+ * device int32 [n_groups + 1], ascending within 0..rows, gives the rows
+ * [offsets[g], offsets[g + 1]) of group g, which may be none; rows before the first
+ * and behind the last are neither read nor written.  Offsets outside 0..rows or
+ * descending ones reach no memory outside the arrays, but what rows then hold is
+ * undefined.  Without groups offsets is NULL.
+ * All pointers but offsets are 16-byte aligned.  workspace: cep_linear_workspace(
+ * desc, 0) bytes for this call alone, (desc, 1) bytes for this call and the
+ * backward one (one after the other; nothing in it is kept between them). */
+size_t cep_linear_workspace(const cep_linear_desc *desc, int backward);
+int cep_linear(const cep_linear_desc *desc, const void *x, const void *w, const float *bias,
+               const void *mul, const void *residual, const int32_t *offsets, void *y,
+               float *preact, void *workspace, size_t workspace_bytes, hipStream_t s);
+
+/* Its gradient: from dy (y_dtype) and the forward call's x, w, mul, offsets and
+ * preact (needed with an activation and for dmul),
+ *   dz = dy * mul * act'(z);  dx = dz W^T + dx_add;  dw = x^T dz
+ *   dbias = sum of dz over the (group's) rows;  dmul = dy * act(z)
+ * dx (dx_dtype), dw (dw_dtype, layout of w), dbias (float32, layout of bias) and
+ * dmul (bf16, layout of mul) are written, not added to, and each may be NULL; so may
+ * w without dx and x without dw.  dx_add (dx_dtype, NULL: none, may be dx itself)
+ * joins dx.  A group without rows gets zeros in dw and dbias.  dz is rounded to bf16
+ * once, for the products that follow (dbias sums it before that).  The residual's
+ * gradient is dy. */
+int cep_linear_backward(const cep_linear_desc *desc, const void *dy, const void *x, const void *w,
+                        const void *mul, const int32_t *offsets, const float *preact,
+                        const void *dx_add, void *dx, void *dw, float *dbias, void *dmul,
+                        void *workspace, size_t workspace_bytes, hipStream_t s);
 
 /* ------------------------------------------------------------------------
  * FFN throughput profile (host only; no GPU work).

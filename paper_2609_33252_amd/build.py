@@ -20,7 +20,8 @@ ARCH = "gfx950"
 
 SOURCES = ["route.hip", "gemm.hip", "gemm_bf16.hip", "gemm_fp8.hip", "gemm_mx.hip",
            "gemm_rows.hip", "gemm_rows_bf16.hip", "norm.hip", "gate.hip", "dispatch.hip",
-           "dense.hip", "dense_rows.hip", "runtime.hip", "profile.cpp", "oewf.cpp"]
+           "dense.hip", "dense_rows.hip", "expert_sort.hip", "expert_unsort.hip", "linear.hip",
+           "runtime.hip", "profile.cpp", "oewf.cpp"]
 # Per-source extra flags.  The e4m3 GEMMs promote every MFMA result with
 # VALU arithmetic; taking MFMA results in VGPRs saves one accvgpr read per
 # promoted element.

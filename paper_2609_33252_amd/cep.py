@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libcep.so")
 CEP_OK, CEP_EINVAL, CEP_ENOMEM, CEP_EHIP, CEP_ESTATE, CEP_EBUSY = 0, -1, -2, -3, -4, -5
 CEP_F32, CEP_BF16, CEP_FP8_E4M3_B128, CEP_MXFP4, CEP_MXFP8 = 0, 1, 2, 3, 4
 CEP_SOFTMAX, CEP_SIGMOID = 0, 1
+CEP_IDENTITY, CEP_RELU, CEP_SILU, CEP_GELU, CEP_GELU_TANH = 0, 1, 2, 3, 4
 CEP_WAIT_ALL, CEP_PER_CHUNK, CEP_THRESHOLD = 0, 1, 2
 CEP_FETCH_COPY, CEP_FETCH_IN_PLACE, CEP_FETCH_FAIL_COPY = 0, 1, 2
 STATUS_NAMES = {0: "CEP_OK", -1: "CEP_EINVAL", -2: "CEP_ENOMEM", -3: "CEP_EHIP",
@@ -28,7 +29,9 @@ EXPORTED = ["cep_packed_expert_bytes", "cep_pack_experts", "cep_init_experts", "
             "cep_set_fetch_mode", "cep_ffn_noalloc", "cep_row_bytes",
             "cep_rms_norm", "cep_rms_norm_workspace", "cep_rms_norm_backward", "cep_gate_topk",
             "cep_dispatch_workspace", "cep_dispatch", "cep_gated_ffn_workspace", "cep_gated_ffn",
-            "cep_gated_ffn_backward",
+            "cep_gated_ffn_backward", "cep_gate_topk_backward", "cep_expert_sort_workspace",
+            "cep_expert_sort", "cep_expert_unsort", "cep_expert_unsort_backward",
+            "cep_linear_workspace", "cep_linear", "cep_linear_backward",
             "cep_profile_create",
             "cep_profile_peak", "cep_profile_theta", "cep_profile_eta", "cep_profile_latency",
             "cep_profile_destroy", "cep_oewf_create", "cep_oewf_begin_layer", "cep_oewf_set_rank",
@@ -77,6 +80,28 @@ class cep_dispatch_desc(ctypes.Structure):
 class cep_gated_ffn_desc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int), ("d_model", ctypes.c_int), ("d_ff", ctypes.c_int),
                 ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64), ("ld_dx", ctypes.c_int64)]
+
+
+class cep_expert_sort_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("top_k", ctypes.c_int), ("n_experts", ctypes.c_int),
+                ("capacity", ctypes.c_int), ("row_bytes", ctypes.c_int64),
+                ("ld_x", ctypes.c_int64)]
+
+
+class cep_expert_unsort_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("top_k", ctypes.c_int), ("d", ctypes.c_int),
+                ("sorted_rows", ctypes.c_int), ("ys_dtype", ctypes.c_int),
+                ("res_dtype", ctypes.c_int), ("y_dtype", ctypes.c_int),
+                ("ld_ys", ctypes.c_int64), ("ld_res", ctypes.c_int64), ("ld_y", ctypes.c_int64)]
+
+
+class cep_linear_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int), ("d_in", ctypes.c_int), ("d_out", ctypes.c_int),
+                ("n_groups", ctypes.c_int), ("act", ctypes.c_int), ("y_dtype", ctypes.c_int),
+                ("res_dtype", ctypes.c_int), ("dx_dtype", ctypes.c_int),
+                ("dw_dtype", ctypes.c_int), ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
+                ("ld_mul", ctypes.c_int64), ("ld_res", ctypes.c_int64),
+                ("ld_dx", ctypes.c_int64)]
 
 
 class cep_oewf_fetch(ctypes.Structure):
@@ -143,6 +168,14 @@ def lib():
         L.cep_gated_ffn_workspace.argtypes = [P(cep_gated_ffn_desc), i32]
         L.cep_gated_ffn.argtypes = [P(cep_gated_ffn_desc)] + [vp] * 7 + [sz, vp]
         L.cep_gated_ffn_backward.argtypes = [P(cep_gated_ffn_desc)] + [vp] * 11 + [sz, vp]
+        L.cep_gate_topk_backward.argtypes = [P(cep_gate_desc)] + [vp] * 5
+        L.cep_expert_sort_workspace.argtypes = [P(cep_expert_sort_desc)]
+        L.cep_expert_sort.argtypes = [P(cep_expert_sort_desc)] + [vp] * 7 + [sz, vp]
+        L.cep_expert_unsort.argtypes = [P(cep_expert_unsort_desc)] + [vp] * 6
+        L.cep_expert_unsort_backward.argtypes = [P(cep_expert_unsort_desc)] + [vp] * 7
+        L.cep_linear_workspace.argtypes = [P(cep_linear_desc), i32]
+        L.cep_linear.argtypes = [P(cep_linear_desc)] + [vp] * 9 + [sz, vp]
+        L.cep_linear_backward.argtypes = [P(cep_linear_desc)] + [vp] * 12 + [sz, vp]
         i64, f64 = ctypes.c_int64, ctypes.c_double
         L.cep_profile_create.argtypes = [P(i64), P(f64), i32, P(vp)]
         L.cep_profile_peak.argtypes = [vp]
@@ -361,6 +394,18 @@ def make_gated_ffn(**kw) -> cep_gated_ffn_desc:
     return cep_gated_ffn_desc(**kw)
 
 
+def make_expert_sort(**kw) -> cep_expert_sort_desc:
+    return cep_expert_sort_desc(**kw)
+
+
+def make_expert_unsort(**kw) -> cep_expert_unsort_desc:
+    return cep_expert_unsort_desc(**kw)
+
+
+def make_linear(**kw) -> cep_linear_desc:
+    return cep_linear_desc(**kw)
+
+
 def _room(t):
     return 0 if t is None else t.numel() * t.element_size()
 
@@ -388,6 +433,11 @@ def cep_rms_norm_backward(desc, x, w, dy, dres, dx, dw, workspace, stream=None):
 def cep_gate_topk(desc, logits, bias, topk_id, topk_w, stream=None):
     _check(None, lib().cep_gate_topk(desc, _ptr(logits), _ptr(bias), _ptr(topk_id), _ptr(topk_w),
                                      _stream(stream)))
+
+
+def cep_gate_topk_backward(desc, logits, topk_id, d_topk_w, d_logits, stream=None):
+    _check(None, lib().cep_gate_topk_backward(desc, _ptr(logits), _ptr(topk_id), _ptr(d_topk_w),
+                                              _ptr(d_logits), _stream(stream)))
 
 
 def cep_dispatch_workspace(desc) -> int:
@@ -418,6 +468,45 @@ def cep_gated_ffn_backward(desc, dy, x, w_gate, w_up, w_down, preact, dx, dw_gat
                                               _ptr(dw_gate), _ptr(dw_up), _ptr(dw_down),
                                               _ptr(workspace), _room(workspace),
                                               _stream(stream)))
+
+
+def cep_expert_sort_workspace(desc) -> int:
+    return int(lib().cep_expert_sort_workspace(desc))
+
+
+def cep_expert_sort(desc, topk_id, plan, pair, place, workspace, x=None, out_x=None, stream=None):
+    _check(None, lib().cep_expert_sort(desc, _ptr(topk_id), _ptr(x), _ptr(plan), _ptr(pair),
+                                       _ptr(place), _ptr(out_x), _ptr(workspace),
+                                       _room(workspace), _stream(stream)))
+
+
+def cep_expert_unsort(desc, ys, place, y, w=None, residual=None, stream=None):
+    _check(None, lib().cep_expert_unsort(desc, _ptr(ys), _ptr(place), _ptr(w), _ptr(residual),
+                                         _ptr(y), _stream(stream)))
+
+
+def cep_expert_unsort_backward(desc, dy, ys, place, w, dys, dw, stream=None):
+    _check(None, lib().cep_expert_unsort_backward(desc, _ptr(dy), _ptr(ys), _ptr(place), _ptr(w),
+                                                  _ptr(dys), _ptr(dw), _stream(stream)))
+
+
+def cep_linear_workspace(desc, backward=False) -> int:
+    return int(lib().cep_linear_workspace(desc, 1 if backward else 0))
+
+
+def cep_linear(desc, x, w, y, workspace, bias=None, mul=None, residual=None, offsets=None,
+               preact=None, stream=None):
+    _check(None, lib().cep_linear(desc, _ptr(x), _ptr(w), _ptr(bias), _ptr(mul), _ptr(residual),
+                                  _ptr(offsets), _ptr(y), _ptr(preact), _ptr(workspace),
+                                  _room(workspace), _stream(stream)))
+
+
+def cep_linear_backward(desc, dy, x, w, workspace, dx=None, dw=None, dbias=None, preact=None,
+                        mul=None, dmul=None, dx_add=None, offsets=None, stream=None):
+    _check(None, lib().cep_linear_backward(desc, _ptr(dy), _ptr(x), _ptr(w), _ptr(mul),
+                                           _ptr(offsets), _ptr(preact), _ptr(dx_add), _ptr(dx),
+                                           _ptr(dw), _ptr(dbias), _ptr(dmul), _ptr(workspace),
+                                           _room(workspace), _stream(stream)))
 
 
 # ------------------------------------------------------------ FFN profile

@@ -1,0 +1,195 @@
+// The experts' rows back to their tokens, weighted and summed, and its gradient,
+// for gfx950.
+//
+//   y[t] = r[t] + sum over j of w[t][j] ys[place[t][j]]
+//   dys[place[t][j]] = w[t][j] dy[t];  dw[t][j] = <dy[t], ys[place[t][j]]>
+//
+// Every row is read and written once: bound by HBM.  The sum over the slots and the
+// product over the channels have a fixed order, so results do not depend on timing.
+#include "block_ops.h"
+
+#include <algorithm>
+
+namespace cep {
+namespace {
+
+struct UnsortArgs {
+  const void *ys;
+  const int32_t *place;
+  const float *w;
+  const void *res;
+  void *y;
+  const void *dy;
+  void *dys;
+  float *dw;
+  int64_t ld_ys, ld_res, ld_y;
+  int rows, k, d, sorted, ys_dtype, res_dtype, y_dtype;
+  int waves;  // of a row
+};
+
+// The slot's sorted row, -1: none.
+__device__ inline int place_of(const UnsortArgs &a, int64_t pair) {
+  const int p = a.place[pair];
+  return p < a.sorted ? p : -1;
+}
+
+// A wave a token and 512 channels of it; the rows of all slots on the way at once.
+template <int KM>
+__global__ __launch_bounds__(256) void k_unsort(UnsortArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = item / a.waves;
+  if (t >= a.rows) return;
+  const int c = ((int)(item % a.waves) * 64 + lane) * 8, n = a.d - c;
+  const bool slot = lane < a.k;
+  const int my = slot ? place_of(a, t * a.k + lane) : -1;
+  const float mw = slot && a.w ? a.w[t * a.k + lane] : 1.0f;
+  float s[8] = {}, v[KM][8];
+  if (a.res) load8(a.res, a.res_dtype, t * a.ld_res + c, n, s);
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    const int p = __builtin_amdgcn_readlane(my, j);
+    if (j < a.k && p >= 0) load8(a.ys, a.ys_dtype, p * a.ld_ys + c, n, v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    const int p = __builtin_amdgcn_readlane(my, j);
+    if (j >= a.k || p < 0) continue;
+    const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mw), j));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = fmaf(w, v[j][i], s[i]);
+  }
+  if (n > 0) store8(a.y, a.y_dtype, t * a.ld_y + c, n, s);
+}
+
+// LANES threads a token, 8 channels each at a time.
+template <int LANES, int KM>
+__global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(UnsortArgs a) {
+  __shared__ float part[LANES > 64 ? LANES / 64 : 1][KM];
+  const int lane = threadIdx.x & 63, at = threadIdx.x % LANES;
+  const int64_t t = LANES < 256 ? (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES : blockIdx.x;
+  if (t >= a.rows) return;  // uniform over the token's threads
+  const bool slot = lane < a.k;
+  const int my = slot ? place_of(a, t * a.k + lane) : -1;
+  const float mw = slot && a.w ? a.w[t * a.k + lane] : 1.0f;
+  float dot[KM] = {};
+  for (int c = at * 8; c < (a.d + LANES * 8 - 1) / (LANES * 8) * (LANES * 8); c += LANES * 8) {
+    const int n = a.d - c;
+    float g[8];
+    load8(a.dy, a.y_dtype, t * a.ld_y + c, n, g);
+    float v[KM][8];
+    if (a.dw) {
+#pragma unroll
+      for (int j = 0; j < KM; ++j) {
+        const int p = __builtin_amdgcn_readlane(my, j);
+        if (j < a.k && p >= 0) load8(a.ys, a.ys_dtype, p * a.ld_ys + c, n, v[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < KM; ++j) {
+      const int p = __builtin_amdgcn_readlane(my, j);
+      if (j >= a.k || p < 0) continue;
+      if (a.dw) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot[j] = fmaf(g[i], v[j][i], dot[j]);
+      }
+      if (a.dys && n > 0) {
+        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mw), j));
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = w * g[i];
+        store8(a.dys, a.ys_dtype, p * a.ld_ys + c, n, o);
+      }
+    }
+  }
+  if (!a.dw) return;
+#pragma unroll
+  for (int j = 0; j < KM; ++j) {
+    dot[j] = wave_sum(dot[j]);
+    if (LANES > 64 && lane == 0) part[threadIdx.x >> 6][j] = dot[j];
+  }
+  if (LANES > 64) __syncthreads();
+  if (at >= a.k) return;
+  float sum = 0.f;
+  if (LANES > 64) {
+#pragma unroll
+    for (int i = 0; i < LANES / 64; ++i) sum += part[i][at];
+  } else {
+#pragma unroll
+    for (int j = 0; j < KM; ++j) sum = at == j ? dot[j] : sum;
+  }
+  a.dw[t * a.k + at] = my >= 0 ? sum : 0.f;
+}
+
+template <int KM>
+void launch_grad(const UnsortArgs &a, hipStream_t s) {
+  if (a.d <= 512)
+    hipLaunchKernelGGL((k_unsort_grad<64, KM>), dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_unsort_grad<256, KM>), dim3(a.rows), dim3(256), 0, s, a);
+}
+
+const char *bad_desc(const cep_expert_unsort_desc *d) {
+  if (!d) return "desc is NULL";
+  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^21";
+  if (d->top_k < 1 || d->top_k > kMaxTopK) return "top_k must be in 1..16";
+  if (d->d < 1 || d->d > kMaxDim) return "d must be in 1..32768";
+  if (d->sorted_rows < 0) return "sorted_rows must be >= 0";
+  if (!is_float_dtype(d->ys_dtype) || !is_float_dtype(d->res_dtype) || !is_float_dtype(d->y_dtype))
+    return "types must be CEP_F32 or CEP_BF16";
+  for (int64_t ld : {d->ld_ys, d->ld_res, d->ld_y})
+    if (ld && ld < d->d) return "a row stride is shorter than a row";
+  return nullptr;
+}
+
+UnsortArgs args_of(const cep_expert_unsort_desc *d) {
+  UnsortArgs a{};
+  a.ld_ys = d->ld_ys ? d->ld_ys : d->d;
+  a.ld_res = d->ld_res ? d->ld_res : d->d;
+  a.ld_y = d->ld_y ? d->ld_y : d->d;
+  a.rows = d->rows, a.k = d->top_k, a.d = d->d, a.sorted = d->sorted_rows;
+  a.ys_dtype = d->ys_dtype, a.res_dtype = d->res_dtype, a.y_dtype = d->y_dtype;
+  a.waves = (d->d + 511) / 512;
+  return a;
+}
+
+}  // namespace
+}  // namespace cep
+
+using namespace cep;
+
+CEP_API int cep_expert_unsort(const cep_expert_unsort_desc *d, const void *ys, const int32_t *place,
+                              const float *w, const void *residual, void *y, hipStream_t s) {
+  const char *fn = "cep_expert_unsort";
+  if (const char *why = bad_desc(d)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
+  if (d->rows == 0) return CEP_OK;
+  if (!place || !y || (d->sorted_rows && !ys)) return refuse(CEP_EINVAL, "%s: NULL array", fn);
+  if (!aligned(place, 4) || !aligned(w, 4) || !aligned(ys, dtype_bytes(d->ys_dtype)) ||
+      !aligned(residual, dtype_bytes(d->res_dtype)) || !aligned(y, dtype_bytes(d->y_dtype)))
+    return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  UnsortArgs a = args_of(d);
+  a.ys = ys, a.place = place, a.w = w, a.res = residual, a.y = y;
+  const dim3 grid((unsigned)(((int64_t)a.rows * a.waves + 3) / 4));
+  if (a.k <= 8) hipLaunchKernelGGL(k_unsort<8>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_unsort<16>, grid, dim3(256), 0, s, a);
+  return launched(fn);
+}
+
+CEP_API int cep_expert_unsort_backward(const cep_expert_unsort_desc *d, const void *dy,
+                                       const void *ys, const int32_t *place, const float *w,
+                                       void *dys, float *dw, hipStream_t s) {
+  const char *fn = "cep_expert_unsort_backward";
+  if (const char *why = bad_desc(d)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
+  if (d->rows == 0) return CEP_OK;
+  if (!dy || !place || (!dys && !dw) || (dw && d->sorted_rows && !ys))
+    return refuse(CEP_EINVAL, "%s: NULL array", fn);
+  if (!aligned(place, 4) || !aligned(w, 4) || !aligned(dw, 4) ||
+      !aligned(ys, dtype_bytes(d->ys_dtype)) || !aligned(dys, dtype_bytes(d->ys_dtype)) ||
+      !aligned(dy, dtype_bytes(d->y_dtype)))
+    return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  UnsortArgs a = args_of(d);
+  a.dy = dy, a.ys = ys, a.place = place, a.w = w, a.dys = dys, a.dw = dw;
+  if (a.k <= 8) launch_grad<8>(a, s);
+  else launch_grad<16>(a, s);
+  return launched(fn);
+}

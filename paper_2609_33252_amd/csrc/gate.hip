@@ -351,6 +351,130 @@ void launch_by_experts(const GateArgs &a, hipStream_t s) {
   else launch_gate<64, 16, KM>(a, s);
 }
 
+// Gradient of the choice's coefficients.  With c the chosen experts' scores over
+// their sum, g = scale d_topk_w and sums over the chosen:
+//   softmax, normalised  dl_j = c_j (g_j - sum c g)
+//   sigmoid, normalised  the same times 1 - s_j
+//   sigmoid              dl_j = g_j s_j (1 - s_j)
+//   softmax              dl_e = p_e (g_e - sum p g) for every expert, g 0 outside
+// 1 - s is taken as the sigmoid of -l, which keeps its digits.
+struct GateGradArgs {
+  const void *logits;
+  const int32_t *ids;
+  const float *dw;
+  void *dl;
+  int64_t ld;
+  int rows, E, k, dtype, sigmoid, normalize;
+  float scale;
+};
+
+// A wave a row: lane j holds slot j.
+template <int V>
+__global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  auto logit_of = [&](int e) {
+    return unmasked(a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
+                                        : ((const float *)a.logits)[row * a.ld + e]);
+  };
+  int id = -1;
+  float g = 0.f, l = -INFINITY;
+  if (lane < a.k) {
+    const int i = a.ids[row * a.k + lane];
+    if (i >= 0 && i < a.E) {
+      id = i;
+      g = a.dw[row * a.k + lane] * a.scale;
+      l = logit_of(i);
+      if (l == -INFINITY) id = -1, g = 0.f;
+    }
+  }
+  float d[V] = {};
+  if (a.sigmoid || a.normalize) {
+    float s = 0.f, v = 0.f;
+    if (a.sigmoid) {
+      if (id >= 0) s = sigmoid(l);
+    } else {
+      float top = l;
+#pragma unroll
+      for (int o = 1; o < kMaxTopK; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+      if (id >= 0) s = expf(l - top);
+    }
+    if (a.normalize) {
+      const float sum = row_add<kMaxTopK>(s);
+      const float c = sum > 0.f ? s / sum : 0.f;
+      v = c * (g - row_add<kMaxTopK>(c * g));
+      if (a.sigmoid && id >= 0) v *= sigmoid(-l);
+    } else if (id >= 0) {
+      v = g * s * sigmoid(-l);
+    }
+    for (int j = 0; j < a.k; ++j) {
+      const int e = __builtin_amdgcn_readlane(id, j);
+      const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (e == i * 64 + lane) d[i] += u;
+    }
+  } else {
+    float p[V], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = i * 64 + lane;
+      p[i] = e < a.E ? logit_of(e) : -INFINITY;
+      top = fmaxf(top, p[i]);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      p[i] = p[i] > -INFINITY ? expf(p[i] - top) : 0.f;
+      sum += p[i];
+    }
+    sum = wave_sum(sum);
+    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+    const float dot = row_add<kMaxTopK>(id >= 0 ? expf(l - top) * inv * g : 0.f);
+    const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(dot)));
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] = -all;
+    for (int j = 0; j < a.k; ++j) {
+      const int e = __builtin_amdgcn_readlane(id, j);
+      const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), j));
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (e == i * 64 + lane) d[i] += u;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) d[i] *= p[i] * inv;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = i * 64 + lane;
+    if (e >= a.E) continue;
+    if (a.dtype == CEP_BF16) ((__bf16 *)a.dl)[row * a.ld + e] = (__bf16)d[i];
+    else ((float *)a.dl)[row * a.ld + e] = d[i];
+  }
+}
+
+const char *bad_desc(const cep_gate_desc *g, const float *bias) {
+  if (!g) return "desc is NULL";
+  if (g->rows < 0 || g->rows > kMaxOpRows) return "rows must be in 0..2^21";
+  if (g->n_experts < 1 || g->n_experts > kMaxGateExperts) return "n_experts must be in 1..1024";
+  if (g->top_k < 1 || g->top_k > kMaxTopK || g->top_k > g->n_experts)
+    return "top_k must be in 1..16 and at most n_experts";
+  if (!is_float_dtype(g->logit_dtype)) return "logit_dtype must be CEP_F32 or CEP_BF16";
+  if (g->score != CEP_SOFTMAX && g->score != CEP_SIGMOID)
+    return "score must be CEP_SOFTMAX or CEP_SIGMOID";
+  const int groups = g->n_groups ? g->n_groups : 1;
+  const int topg = g->n_groups ? g->topk_groups : 1;
+  if (groups < 1 || groups > kMaxGroups || g->n_experts % groups || topg < 1 || topg > groups)
+    return "n_groups (up to 64) must divide n_experts, topk_groups be in 1..n_groups";
+  if (g->score == CEP_SOFTMAX && (bias || groups > 1)) return "a bias and groups go with CEP_SIGMOID";
+  if (g->ld && g->ld < g->n_experts) return "ld is shorter than a row";
+  if (!(g->scale == g->scale)) return "scale is NaN";
+  return nullptr;
+}
+
 }  // namespace
 }  // namespace cep
 
@@ -359,34 +483,44 @@ using namespace cep;
 CEP_API int cep_gate_topk(const cep_gate_desc *g, const void *logits, const float *bias,
                           int32_t *topk_id, float *topk_w, hipStream_t s) {
   const char *fn = "cep_gate_topk";
-  if (!g) return refuse(CEP_EINVAL, "%s: desc is NULL", fn);
-  if (g->rows < 0 || g->rows > kMaxOpRows) return refuse(CEP_EINVAL, "%s: rows must be in 0..2^21", fn);
-  if (g->n_experts < 1 || g->n_experts > kMaxGateExperts)
-    return refuse(CEP_EINVAL, "%s: n_experts must be in 1..1024", fn);
-  if (g->top_k < 1 || g->top_k > kMaxTopK || g->top_k > g->n_experts)
-    return refuse(CEP_EINVAL, "%s: top_k must be in 1..16 and at most n_experts", fn);
-  if (!is_float_dtype(g->logit_dtype))
-    return refuse(CEP_EINVAL, "%s: logit_dtype must be CEP_F32 or CEP_BF16", fn);
-  if (g->score != CEP_SOFTMAX && g->score != CEP_SIGMOID)
-    return refuse(CEP_EINVAL, "%s: unknown score %d", fn, g->score);
-  const int groups = g->n_groups ? g->n_groups : 1;
-  const int topg = g->n_groups ? g->topk_groups : 1;
-  if (groups < 1 || groups > kMaxGroups || g->n_experts % groups || topg < 1 || topg > groups)
-    return refuse(CEP_EINVAL, "%s: n_groups (up to 64) must divide n_experts, topk_groups be in "
-                  "1..n_groups", fn);
-  if (g->score == CEP_SOFTMAX && (bias || groups > 1))
-    return refuse(CEP_EINVAL, "%s: a bias and groups go with CEP_SIGMOID", fn);
-  if (g->ld && g->ld < g->n_experts) return refuse(CEP_EINVAL, "%s: ld is shorter than a row", fn);
-  if (!(g->scale == g->scale)) return refuse(CEP_EINVAL, "%s: scale is NaN", fn);
+  if (const char *why = bad_desc(g, bias)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
   if (g->rows == 0) return CEP_OK;
   if (!logits || !topk_id || !topk_w) return refuse(CEP_EINVAL, "%s: NULL array", fn);
   if (!aligned(logits, dtype_bytes(g->logit_dtype)) || !aligned(bias, 4) || !aligned(topk_id, 4) ||
       !aligned(topk_w, 4))
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
   const GateArgs a{logits, bias, topk_id, topk_w, g->ld ? g->ld : g->n_experts, g->rows,
-                   g->n_experts, g->top_k, g->logit_dtype, g->score == CEP_SIGMOID, groups, topg,
+                   g->n_experts, g->top_k, g->logit_dtype, g->score == CEP_SIGMOID,
+                   g->n_groups ? g->n_groups : 1, g->n_groups ? g->topk_groups : 1,
                    g->normalize != 0, g->scale};
   if (g->top_k <= 8) launch_by_experts<8>(a, s);
   else launch_by_experts<16>(a, s);
+  return launched(fn);
+}
+
+CEP_API int cep_gate_topk_backward(const cep_gate_desc *g, const void *logits,
+                                   const int32_t *topk_id, const float *d_topk_w, void *d_logits,
+                                   hipStream_t s) {
+  const char *fn = "cep_gate_topk_backward";
+  if (const char *why = bad_desc(g, nullptr)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
+  if (g->rows == 0) return CEP_OK;
+  if (!logits || !topk_id || !d_topk_w || !d_logits)
+    return refuse(CEP_EINVAL, "%s: NULL array", fn);
+  const size_t el = dtype_bytes(g->logit_dtype);
+  if (!aligned(logits, el) || !aligned(d_logits, el) || !aligned(topk_id, 4) ||
+      !aligned(d_topk_w, 4))
+    return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  if (d_logits == logits) return refuse(CEP_EINVAL, "%s: d_logits overlaps the logits", fn);
+  const GateGradArgs a{logits, topk_id, d_topk_w, d_logits, g->ld ? g->ld : g->n_experts, g->rows,
+                       g->n_experts, g->top_k, g->logit_dtype, g->score == CEP_SIGMOID,
+                       g->normalize != 0, g->scale};
+  const dim3 grid((unsigned)((a.rows + 3) / 4));
+  auto *k = a.E <= 64    ? k_gate_grad<1>
+            : a.E <= 128 ? k_gate_grad<2>
+            : a.E <= 192 ? k_gate_grad<3>
+            : a.E <= 256 ? k_gate_grad<4>
+            : a.E <= 512 ? k_gate_grad<8>
+                         : k_gate_grad<16>;
+  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
   return launched(fn);
 }

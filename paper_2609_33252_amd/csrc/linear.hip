@@ -1,0 +1,649 @@
+// Matrix product with bias, activation, factor and residual in its epilogue, of one
+// weight or of one per group of rows, and its gradient, in bf16 with float32
+// accumulation, for gfx950.
+//
+//   z = x W + b, y = act(z) m + r
+//   dz = dy m act'(z), dm = dy act(z), db = sum of dz, dx = dz W^T + a, dW = x^T dz
+//
+// Few rows a group stream the weights (rows_tile.h), more run the tiled product
+// (dense_tile.h); the tiles of grouped rows are found on the device from the
+// groups' offsets, the grid covers their most.
+#include "dense_tile.h"
+#include "rows_tile.h"
+
+namespace cep {
+namespace {
+
+constexpr int kMaxGroups = 1024;
+
+struct Groups {
+  const int32_t *offsets;  // [n + 1]
+  int n;                   // 0: one weight
+  int rows;
+};
+
+// Rows [lo, lo + n) of group g, inside the arrays whatever the offsets hold.
+struct Span {
+  int lo, n;
+};
+__device__ inline Span span_of(const Groups &gr, int g) {
+  const int lo = min(max(gr.offsets[g], 0), gr.rows);
+  return {lo, min(max(gr.offsets[g + 1], lo), gr.rows) - lo};
+}
+
+// Tiles of TILE rows of the groups g0 + lane and those before it from g0 on.
+template <int TILE>
+__device__ inline int tiles_upto(const Groups &gr, int g0) {
+  const int lane = threadIdx.x & 63;
+  int v = g0 + lane < gr.n ? (span_of(gr, g0 + lane).n + TILE - 1) / TILE : 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+template <int TILE>
+__device__ inline int tiles_of(const Groups &gr) {
+  if (gr.n == 0) return (gr.rows + TILE - 1) / TILE;
+  int all = 0;
+  for (int g0 = 0; g0 < gr.n; g0 += 64)
+    all += __builtin_amdgcn_readlane(tiles_upto<TILE>(gr, g0), 63);
+  return all;
+}
+// Tile mt of them: its group, that group's rows, and the row of it where it starts.
+struct RowTile {
+  int g, m0;
+  Span rows;
+};
+template <int TILE>
+__device__ inline RowTile tile_at(const Groups &gr, int mt) {
+  if (gr.n == 0) return {0, mt * TILE, {0, gr.rows}};
+  for (int g0 = 0;; g0 += 64) {
+    const int upto = tiles_upto<TILE>(gr, g0), all = __builtin_amdgcn_readlane(upto, 63);
+    if (mt < all) {
+      const int i = (int)__popcll(__ballot(upto <= mt));
+      const int first = i ? __builtin_amdgcn_readlane(upto, i - 1) : 0;
+      const Span s = span_of(gr, g0 + i);
+      return {__builtin_amdgcn_readfirstlane(g0 + i),
+              __builtin_amdgcn_readfirstlane((mt - first) * TILE),
+              {__builtin_amdgcn_readfirstlane(s.lo), __builtin_amdgcn_readfirstlane(s.n)}};
+    }
+    mt -= all;
+  }
+}
+// The group of a row, gr.n: none (the first whose end is behind it).
+__device__ inline int group_of(const Groups &gr, int row) {
+  const int lane = threadIdx.x & 63;
+  int g = 0;
+  for (int g0 = 0; g0 < gr.n; g0 += 64) {
+    const bool past = g0 + lane < gr.n && gr.offsets[g0 + lane + 1] <= row;
+    const int n = (int)__popcll(__ballot(past));
+    g += n;
+    if (n < 64) break;
+  }
+  return g;
+}
+
+// ---- epilogue
+
+__device__ inline float normal_cdf(float z) { return 0.5f * erfcf(z * -0.707106781f); }
+// The two operands of the tangent's logistic form: z (1 + tanh(u)) / 2 = z sigma(2 u),
+// where z beyond 30 in magnitude changes nothing any more but could overflow.
+__device__ inline float tanh_arg(float z, float *slope) {
+  constexpr float kA = 1.59576912f, kB = 0.044715f;  // 2 sqrt(2 / pi)
+  const float c = fminf(fmaxf(z, -30.0f), 30.0f), q = c * c;
+  if (slope) *slope = kA * fmaf(3.0f * kB, q, 1.0f);
+  return kA * c * fmaf(kB, q, 1.0f);
+}
+template <int ACT>
+__device__ inline float act_of(float z) {
+  if (ACT == CEP_RELU) return z > 0.f ? z : z != z ? z : 0.f;
+  if (ACT == CEP_SILU) return z * sigma(z);
+  if (ACT == CEP_GELU) return z * normal_cdf(z);
+  if (ACT == CEP_GELU_TANH) return z * sigma(tanh_arg(z, nullptr));
+  return z;
+}
+// act(z), and its slope
+template <int ACT>
+__device__ inline float slope_of(float z, float *value) {
+  if (ACT == CEP_SILU) {
+    const float s = sigma(z);
+    *value = z * s;
+    return s * (1.0f + z * (1.0f - s));
+  }
+  if (ACT == CEP_GELU) {
+    const float phi = normal_cdf(z);
+    *value = z * phi;
+    return fmaf(z, 0.398942280f * __expf(-0.5f * z * z), phi);
+  }
+  if (ACT == CEP_GELU_TANH) {
+    float slope;
+    const float s = sigma(tanh_arg(z, &slope));
+    *value = z * s;
+    const float c = fminf(fmaxf(z, -30.0f), 30.0f);
+    return fmaf(c * s * (1.0f - s), slope, s);
+  }
+  *value = act_of<ACT>(z);
+  return ACT == CEP_RELU ? (z > 0.f ? 1.0f : z != z ? z : 0.f) : 1.0f;
+}
+// f(std::integral_constant) of an activation
+template <class F>
+__device__ inline void with_act(int act, F f) {
+  switch (act) {
+    case CEP_RELU: return f(std::integral_constant<int, CEP_RELU>{});
+    case CEP_SILU: return f(std::integral_constant<int, CEP_SILU>{});
+    case CEP_GELU: return f(std::integral_constant<int, CEP_GELU>{});
+    case CEP_GELU_TANH: return f(std::integral_constant<int, CEP_GELU_TANH>{});
+    default: return f(std::integral_constant<int, CEP_IDENTITY>{});
+  }
+}
+
+struct Finish {
+  const float *bias;   // [groups][N]
+  const __bf16 *mul;
+  const void *res;
+  void *y;
+  float *pre;          // [rows][N]
+  int64_t ld_mul, ld_res, ld_y;
+  int N, act, res_dtype, y_dtype;
+};
+
+__device__ inline f32x4 load4(const void *p, int dtype, int64_t at) {
+  if (dtype == CEP_F32) return *(const f32x4 *)((const float *)p + at);
+  const uint2 u = *(const uint2 *)((const __bf16 *)p + at);
+  return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
+               __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
+}
+__device__ inline void store4(void *p, int dtype, int64_t at, const f32x4 &v) {
+  if (dtype == CEP_F32) *(f32x4 *)((float *)p + at) = v;
+  else store_bf16((__bf16 *)p + at, v);
+}
+
+// Four columns from n of row m, of group g, from their sums.
+template <int ACT>
+__device__ inline void finish(const Finish &f, int64_t m, int n, int g, f32x4 z) {
+  if (f.bias) z += *(const f32x4 *)(f.bias + (int64_t)g * f.N + n);
+  if (f.pre) *(f32x4 *)(f.pre + m * f.N + n) = z;
+  f32x4 v;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) v[r] = act_of<ACT>(z[r]);
+  if (f.mul) v *= load4(f.mul, CEP_BF16, m * f.ld_mul + n);
+  if (f.res) v += load4(f.res, f.res_dtype, m * f.ld_res + n);
+  store4(f.y, f.y_dtype, m * f.ld_y + n, v);
+}
+
+// ---- tiled product
+
+struct LinearArgs : TileArgs {  // M: unused with groups
+  Groups groups;
+  int64_t w_stride;  // elements of a group's weight
+  float *part;       // above one K share their sums: [splits][rows][N]
+  Finish f;
+};
+
+// y (B_K false) or dx (true: N is d_in) in tiles of whole groups' rows.
+template <int HALF, int WM, int WN, bool B_K, int ACT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear(LinearArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  const int x = blockIdx.x & 7, at = blockIdx.x >> 3;
+  const int n_tm = tiles_of<2 * HALF>(a.groups), n_tn = (a.N + 2 * HALF - 1) / (2 * HALF);
+  const int items = n_tm * a.splits * n_tn;
+  if (at >= piece_of(items, x)) return;
+  int mt, nt;
+  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + at, n_tm * a.splits, n_tn, &mt, &nt);
+  const int share = mt / n_tm;
+  const RowTile tile = tile_at<2 * HALF>(a.groups, mt - share * n_tm);
+  TileArgs t = a;
+  t.A += tile.rows.lo * a.lda;
+  t.B0 += tile.g * a.w_stride;
+  t.M = tile.rows.n;
+  dense_tile<HALF, WM, WN, true, B_K, false>(
+      t, tile.m0, nt * 2 * HALF, share, lds,
+      [&](int64_t m, int n, const f32x4 &v, const f32x4 &) {
+        m += tile.rows.lo;
+        if (a.splits == 1) finish<ACT>(a.f, m, n, tile.g, v);
+        else *(f32x4 *)(a.part + ((int64_t)share * a.groups.rows + m) * a.N + n) = v;
+      });
+}
+
+// The shares' sums of a row, added in order, and what becomes of them.
+__global__ __launch_bounds__(256) void k_linear_finish(const float *part, int splits, Groups groups,
+                                                       Finish f) {
+  const int64_t m = blockIdx.x;
+  const int n = ((int)blockIdx.y * 256 + threadIdx.x) * 4;
+  int g = 0;
+  if (groups.n) {
+    g = group_of(groups, (int)m);
+    if (g == groups.n || m < span_of(groups, g).lo) return;  // no group's
+  }
+  if (n >= f.N) return;
+  f32x4 v = {};
+#pragma unroll 4
+  for (int i = 0; i < splits; ++i)
+    v += *(const f32x4 *)(part + ((int64_t)i * groups.rows + m) * f.N + n);
+  with_act(f.act, [&](auto act) { finish<decltype(act)::value>(f, m, n, g, v); });
+}
+
+struct WgradArgs : TileArgs {  // K: unused with groups
+  Groups groups;
+  float *part;  // above one K share (one weight): [splits][M][N]
+  Finish f;     // of one weight's gradient
+};
+
+// dW of each group, its rows as K.
+template <int HALF, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  const int n_tm = (a.M + 2 * HALF - 1) / (2 * HALF), n_tn = (a.N + 2 * HALF - 1) / (2 * HALF);
+  // a group's tiles are dealt to all XCDs
+  const int items = n_tm * a.splits * n_tn, room = (items + 7) / 8 * 8;
+  const int g = blockIdx.x / room, in = blockIdx.x % room, x = in & 7, at = in >> 3;
+  if (at >= piece_of(items, x)) return;
+  int mt, nt;
+  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + at, n_tm * a.splits, n_tn, &mt, &nt);
+  const int share = mt / n_tm;
+  TileArgs t = a;
+  if (a.groups.n) {
+    const Span s = span_of(a.groups, g);
+    const int lo = __builtin_amdgcn_readfirstlane(s.lo);
+    t.A += lo * a.lda;
+    t.B0 += lo * a.ldb;
+    t.K = __builtin_amdgcn_readfirstlane(s.n);
+  }
+  const int64_t w0 = (int64_t)g * a.M;
+  dense_tile<HALF, WM, WN, false, false, false>(
+      t, (mt - share * n_tm) * 2 * HALF, nt * 2 * HALF, share, lds,
+      [&](int64_t m, int n, const f32x4 &v, const f32x4 &) {
+        if (a.splits == 1) finish<CEP_IDENTITY>(a.f, w0 + m, n, 0, v);
+        else *(f32x4 *)(a.part + ((int64_t)share * a.M + m) * a.N + n) = v;
+      });
+}
+
+// ---- few rows: the weights are streamed
+
+struct LinearRowsArgs : RowsArgs {
+  Groups groups;
+  int64_t w_stride;
+  float *part;
+  Finish f;
+};
+
+template <int MF>
+__global__ __launch_bounds__(256) void k_linear_rows(LinearRowsArgs a) {
+  __shared__ RowsLds<MF, kRows> lds;
+  const int cb = blockIdx.x % a.col_blocks, sp = blockIdx.x / a.col_blocks % a.splits;
+  const int mt = blockIdx.x / (a.col_blocks * a.splits);
+  if (mt >= tiles_of<MF * 16>(a.groups)) return;
+  const RowTile tile = tile_at<MF * 16>(a.groups, mt);
+  const int64_t row0 = tile.rows.lo + tile.m0;
+  RowsArgs t = a;
+  t.A[0] += row0 * a.lda;
+  t.B0 += tile.g * a.w_stride;
+  t.M = min(tile.rows.n - tile.m0, MF * 16);
+  rows_tile<MF, kRows, false>(t, cb, sp, lds, [&](int row, int col, const f32x4 &v) {
+    const int64_t m = row0 + row;
+    if (a.splits == 1)
+      with_act(a.f.act, [&](auto act) { finish<decltype(act)::value>(a.f, m, col, tile.g, v); });
+    else *(f32x4 *)(a.part + ((int64_t)sp * a.groups.rows + m) * a.N + col) = v;
+  });
+}
+
+// ---- the gradient of the epilogue
+
+constexpr int kDzRows = 32;   // rows of a k_linear_dz block
+constexpr int kDzCols = 256;  // and columns: 32 lanes of eight, eight rows at a time
+
+struct DzArgs {
+  const void *dy;
+  const float *pre;
+  const __bf16 *mul;
+  __bf16 *dz, *dmul;  // dz [rows][N]
+  float *part;        // column sums of a block's rows of a group: [blocks + groups][N]
+  int64_t ld_y, ld_mul;
+  int N, act, y_dtype;
+  Groups groups;
+};
+
+// Row r0's chunk of kDzRows rows, group by group.  The sums of group g's rows go to
+// line chunk + g of `part`: from one pair of chunk and group to the next, one of the
+// two grows, so no line is written twice.
+template <int ACT>
+__global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
+  __shared__ f32x4 sums[8][kDzCols / 4];
+  const int lane = threadIdx.x & 31, rl = threadIdx.x >> 5;
+  const int n = (int)blockIdx.y * kDzCols + lane * 8;
+  const int chunk = blockIdx.x, end = min((chunk + 1) * kDzRows, a.groups.rows);
+  int row = chunk * kDzRows;
+  int g = 0, groups = 1;
+  if (a.groups.n) {
+    groups = a.groups.n;
+    g = group_of(a.groups, row);
+  }
+  for (; g < groups && row < end; ++g) {
+    int to = end;
+    if (a.groups.n) {
+      const Span s = span_of(a.groups, g);
+      row = __builtin_amdgcn_readfirstlane(max(row, s.lo));
+      to = __builtin_amdgcn_readfirstlane(min(s.lo + s.n, end));
+      if (row >= to) continue;
+    }
+    f32x4 sum[2] = {};
+    if (n < a.N) {
+      for (int m = row + rl; m < to; m += 8) {
+        float dy[8], z[8], f[8], out[8], dm[8];
+        load8(a.dy, a.y_dtype, m * a.ld_y + n, 8, dy);
+        if (a.pre) load8(a.pre, CEP_F32, (int64_t)m * a.N + n, 8, z);
+        if (a.mul) load8(a.mul, CEP_BF16, m * a.ld_mul + n, 8, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float value = 0.f, slope = 1.0f;
+          if (a.pre) slope = slope_of<ACT>(z[i], &value);
+          out[i] = (a.mul ? dy[i] * f[i] : dy[i]) * slope;
+          dm[i] = dy[i] * value;
+          sum[i / 4][i % 4] += out[i];
+        }
+        if (a.dz) store8(a.dz, CEP_BF16, (int64_t)m * a.N + n, 8, out);
+        if (a.dmul) store8(a.dmul, CEP_BF16, m * a.ld_mul + n, 8, dm);
+      }
+    }
+    if (a.part) {
+      sums[rl][lane * 2] = sum[0];
+      sums[rl][lane * 2 + 1] = sum[1];
+      __syncthreads();
+      const int c = threadIdx.x;
+      if (c < kDzCols / 4 && (int)blockIdx.y * kDzCols + c * 4 < a.N) {
+        f32x4 v = sums[0][c];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) v += sums[i][c];
+        *(f32x4 *)(a.part + (int64_t)(chunk + g) * a.N + blockIdx.y * kDzCols + c * 4) = v;
+      }
+      __syncthreads();
+    }
+    row = to;
+  }
+}
+
+// db of a group: its lines of `part`, added in order by 16 lanes of columns' fours.
+__global__ __launch_bounds__(256) void k_linear_dbias(const float *part, int N, Groups groups,
+                                                      float *db) {
+  __shared__ f32x4 sums[16][16];
+  const int lane = threadIdx.x & 15, sl = threadIdx.x >> 4, g = blockIdx.y;
+  const int n = ((int)blockIdx.x * 16 + lane) * 4;
+  const Span s = groups.n ? span_of(groups, g) : Span{0, groups.rows};
+  f32x4 v = {};
+  if (s.n && n < N) {
+    const int last = (s.lo + s.n - 1) / kDzRows;
+#pragma unroll 4
+    for (int c = s.lo / kDzRows + sl; c <= last; c += 16)
+      v += *(const f32x4 *)(part + (int64_t)(c + g) * N + n);
+  }
+  sums[sl][lane] = v;
+  __syncthreads();
+  if (sl || n >= N) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) v += sums[i][lane];
+  *(f32x4 *)(db + (int64_t)g * N + n) = v;
+}
+
+// ---- host
+
+constexpr int64_t kMaxStride = 1 << 21;  // a tile's offsets stay below 2^31 bytes
+
+const char *bad_desc(const cep_linear_desc *d) {
+  if (!d) return "desc is NULL";
+  if (d->rows < 0 || d->rows > kMaxOpRows) return "rows must be in 0..2^21";
+  for (int w : {d->d_in, d->d_out})
+    if (w < 8 || w > kMaxDim || w % 8) return "d_in and d_out must be multiples of 8, up to 32768";
+  if (d->n_groups < 0 || d->n_groups > kMaxGroups) return "n_groups must be in 0..1024";
+  if (d->act < CEP_IDENTITY || d->act > CEP_GELU_TANH) return "unknown act";
+  for (int t : {d->y_dtype, d->res_dtype, d->dx_dtype, d->dw_dtype})
+    if (!is_float_dtype(t)) return "types must be CEP_F32 or CEP_BF16";
+  for (int64_t ld : {d->ld_x, d->ld_dx})
+    if (ld && (ld < d->d_in || ld % 8 || ld > kMaxStride))
+      return "row strides must be multiples of 8, at least a row, at most 2^21";
+  for (int64_t ld : {d->ld_y, d->ld_mul, d->ld_res})
+    if (ld && (ld < d->d_out || ld % 8 || ld > kMaxStride))
+      return "row strides must be multiples of 8, at least a row, at most 2^21";
+  return nullptr;
+}
+
+// How a product of `rows` rows (in groups) runs.
+struct Plan {
+  bool stream;  // in row blocks of 16 or 32 (MF fragments)
+  int mf;
+  int tile, splits;
+};
+
+// Rows of a group, on average, up to which the weights are streamed.
+constexpr int kStreamRows = 32;
+
+Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
+  Plan p{};
+  const int g = std::max(groups, 1);
+  if (may_stream && rows <= (int64_t)kStreamRows * g) {
+    p.stream = true;
+    p.mf = rows <= 16 * g ? 1 : 2;
+    // one workgroup a compute unit (a ring takes most of its LDS), at least a unit
+    // for each wave
+    const int cols = (N + kCols - 1) / kCols, blocks = cols * std::min(g, std::max(rows, 1));
+    p.splits = std::max(1, std::min(256 / blocks, K / kUnit / 4));
+    return p;
+  }
+  int64_t tiles[2];
+  for (int t = 0; t < 2; ++t) {
+    // a group's last tile is half full on average
+    const int64_t n_tm = groups ? rows / kTile[t] + (groups + 1) / 2 : (rows + kTile[t] - 1) / kTile[t];
+    tiles[t] = std::max<int64_t>(n_tm, 1) * ((N + kTile[t] - 1) / kTile[t]);
+  }
+  const DensePlan d = plan_tiles(tiles, K / 64, (double)rows * N, 16);
+  p.tile = d.tile;
+  p.splits = d.splits;
+  return p;
+}
+
+Plan wgrad_plan(const cep_linear_desc *d) {
+  Plan p{};
+  const int g = std::max(d->n_groups, 1);
+  const int64_t tiles[2] = {g * dense_tiles(0, d->d_in, d->d_out),
+                            g * dense_tiles(1, d->d_in, d->d_out)};
+  const DensePlan w = plan_tiles(tiles, d->rows / g / 64, (double)d->d_in * d->d_out,
+                                 d->n_groups ? 1 : 16);
+  p.tile = w.tile;
+  p.splits = w.splits;
+  return p;
+}
+
+size_t part_bytes(const Plan &p, int rows, int N) {
+  return p.splits > 1 ? (size_t)p.splits * rows * N * 4 : 0;
+}
+
+int dz_chunks(const cep_linear_desc *d) { return (d->rows + kDzRows - 1) / kDzRows; }
+
+// Scratch of the backward pass: dz, the parts of db, the K shares of a product.
+struct Space {
+  size_t bias, part, bytes;
+};
+Space space_of(const cep_linear_desc *d, int backward) {
+  Space s{};
+  size_t most = part_bytes(plan_of(d->rows, d->d_out, d->d_in, d->n_groups, true), d->rows, d->d_out);
+  if (backward) {
+    s.bias = align_up((size_t)d->rows * d->d_out * 2, 256);
+    s.part = s.bias + align_up((size_t)(dz_chunks(d) + d->n_groups) * d->d_out * 4, 256);
+    most = std::max({most,
+                     s.part + part_bytes(plan_of(d->rows, d->d_in, d->d_out, d->n_groups, false),
+                                         d->rows, d->d_in),
+                     s.part + part_bytes(wgrad_plan(d), d->d_in, d->d_out)});
+  }
+  s.bytes = std::max<size_t>(most, 256);
+  return s;
+}
+
+void launch_finish(const float *part, int splits, const Groups &g, const Finish &f, int rows,
+                   hipStream_t s) {
+  hipLaunchKernelGGL(k_linear_finish, dim3(rows, (f.N + 1023) / 1024), dim3(256), 0, s, part, splits,
+                     g, f);
+}
+
+template <int HALF, int WM, int WN, bool B_K>
+void launch_tiles(const LinearArgs &a, dim3 grid, hipStream_t s) {
+  auto *k = k_linear<HALF, WM, WN, B_K, CEP_IDENTITY>;
+  if constexpr (!B_K) {
+    if (a.f.act == CEP_RELU) k = k_linear<HALF, WM, WN, B_K, CEP_RELU>;
+    if (a.f.act == CEP_SILU) k = k_linear<HALF, WM, WN, B_K, CEP_SILU>;
+    if (a.f.act == CEP_GELU) k = k_linear<HALF, WM, WN, B_K, CEP_GELU>;
+    if (a.f.act == CEP_GELU_TANH) k = k_linear<HALF, WM, WN, B_K, CEP_GELU_TANH>;
+  }
+  hipLaunchKernelGGL(k, grid, dim3(WM * WN * 64), 0, s, a);
+}
+
+// A product over the groups' rows: A [rows][K], W as B, the epilogue's output [rows][N].
+template <bool B_K>
+void launch_linear(const Plan &p, const Groups &g, const __bf16 *A, int64_t lda, const __bf16 *W,
+                   int64_t ldb, int N, int K, const Finish &f, float *part, hipStream_t s) {
+  // the most tiles that the groups' rows can be in
+  auto most = [&](int tile) {
+    return g.n ? std::min<int64_t>(g.rows, g.rows / tile + g.n) : (g.rows + tile - 1) / tile;
+  };
+  const int64_t w_stride = g.n ? (int64_t)N * K : 0;
+  if (p.stream) {
+    LinearRowsArgs a{};
+    a.A[0] = A, a.lda = lda;
+    a.B0 = W, a.ldb = ldb;
+    a.N = N, a.K = K;
+    a.splits = p.splits, a.col_blocks = (N + kCols - 1) / kCols;
+    a.groups = g, a.w_stride = w_stride, a.part = part, a.f = f;
+    const dim3 grid((unsigned)(most(p.mf * 16) * a.col_blocks * a.splits));
+    if (p.mf == 1) hipLaunchKernelGGL(k_linear_rows<1>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(k_linear_rows<2>, grid, dim3(256), 0, s, a);
+  } else {
+    LinearArgs a{};
+    a.A = A, a.lda = lda;
+    a.B0 = W, a.ldb = ldb;
+    a.N = N, a.K = K, a.segs = 1, a.splits = p.splits;
+    a.groups = g, a.w_stride = w_stride, a.part = part, a.f = f;
+    const int64_t items = most(kTile[p.tile]) * p.splits * ((N + kTile[p.tile] - 1) / kTile[p.tile]);
+    const dim3 grid((unsigned)((items + 7) / 8 * 8));
+    if (p.tile == 0) launch_tiles<128, 2, 4, B_K>(a, grid, s);
+    else launch_tiles<64, 2, 2, B_K>(a, grid, s);
+  }
+  if (p.splits > 1) launch_finish(part, p.splits, g, f, g.rows, s);
+}
+
+int check_shared(const char *fn, const cep_linear_desc *d, const int32_t *offsets) {
+  if (const char *why = bad_desc(d)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
+  if (!offsets != !d->n_groups)
+    return refuse(CEP_EINVAL, "%s: offsets go with n_groups", fn);
+  if (!aligned(offsets, 4)) return refuse(CEP_EINVAL, "%s: offsets are not aligned to their type", fn);
+  return CEP_OK;
+}
+
+}  // namespace
+}  // namespace cep
+
+using namespace cep;
+
+CEP_API size_t cep_linear_workspace(const cep_linear_desc *d, int backward) {
+  return bad_desc(d) ? 0 : space_of(d, backward).bytes;
+}
+
+CEP_API int cep_linear(const cep_linear_desc *d, const void *x, const void *w, const float *bias,
+                       const void *mul, const void *residual, const int32_t *offsets, void *y,
+                       float *preact, void *workspace, size_t workspace_bytes, hipStream_t s) {
+  const char *fn = "cep_linear";
+  if (const int rc = check_shared(fn, d, offsets)) return rc;
+  if (d->rows == 0) return CEP_OK;
+  if (!x || !w || !y) return refuse(CEP_EINVAL, "%s: NULL array", fn);
+  for (const void *p : {x, w, (const void *)bias, mul, residual, (const void *)y,
+                        (const void *)preact, (const void *)workspace})
+    if (!aligned(p, 16)) return refuse(CEP_EINVAL, "%s: pointers must be 16-byte aligned", fn);
+  if (!workspace || workspace_bytes < cep_linear_workspace(d, 0))
+    return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
+                  cep_linear_workspace(d, 0));
+  const int D = d->d_in, N = d->d_out;
+  Finish f{};
+  f.bias = bias, f.mul = (const __bf16 *)mul, f.res = residual, f.y = y, f.pre = preact;
+  f.ld_mul = d->ld_mul ? d->ld_mul : N;
+  f.ld_res = d->ld_res ? d->ld_res : N;
+  f.ld_y = d->ld_y ? d->ld_y : N;
+  f.N = N, f.act = d->act, f.res_dtype = d->res_dtype, f.y_dtype = d->y_dtype;
+  const Groups g{offsets, d->n_groups, d->rows};
+  launch_linear<false>(plan_of(d->rows, N, D, d->n_groups, true), g, (const __bf16 *)x,
+                       d->ld_x ? d->ld_x : D, (const __bf16 *)w, N, N, D, f, (float *)workspace, s);
+  return launched(fn);
+}
+
+CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const void *x,
+                                const void *w, const void *mul, const int32_t *offsets,
+                                const float *preact, const void *dx_add, void *dx, void *dw,
+                                float *dbias, void *dmul, void *workspace, size_t workspace_bytes,
+                                hipStream_t s) {
+  const char *fn = "cep_linear_backward";
+  if (const int rc = check_shared(fn, d, offsets)) return rc;
+  if (!dx && !dw && !dbias && !dmul) return refuse(CEP_EINVAL, "%s: no output", fn);
+  if (dx_add && !dx) return refuse(CEP_EINVAL, "%s: dx_add goes with dx", fn);
+  if (dmul && !mul) return refuse(CEP_EINVAL, "%s: dmul goes with mul", fn);
+  const bool curved = d->act != CEP_IDENTITY || dmul;
+  if (d->rows && (!dy || (dx && !w) || (dw && !x) || (curved && !preact)))
+    return refuse(CEP_EINVAL, "%s: NULL array", fn);
+  for (const void *p : {dy, x, w, mul, (const void *)preact, dx_add, (const void *)dx,
+                        (const void *)dw, (const void *)dbias, (const void *)dmul,
+                        (const void *)workspace})
+    if (!aligned(p, 16)) return refuse(CEP_EINVAL, "%s: pointers must be 16-byte aligned", fn);
+  if (!workspace || workspace_bytes < cep_linear_workspace(d, 1))
+    return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
+                  cep_linear_workspace(d, 1));
+  const int D = d->d_in, N = d->d_out, T = d->rows, n_groups = std::max(d->n_groups, 1);
+  const Space space = space_of(d, 1);
+  const Groups g{offsets, d->n_groups, T};
+  uint8_t *ws = (uint8_t *)workspace;
+  float *part = (float *)(ws + space.part), *sums = (float *)(ws + space.bias);
+  // dy is dz already where nothing lies between them but a bias
+  const __bf16 *dz = (const __bf16 *)dy;
+  int64_t ld_z = d->ld_y ? d->ld_y : N;
+  const bool same = d->act == CEP_IDENTITY && !mul && d->y_dtype == CEP_BF16;
+  if (T && (dbias || dmul || (!same && (dx || dw)))) {
+    DzArgs a{};
+    a.dy = dy, a.ld_y = ld_z, a.y_dtype = d->y_dtype;
+    a.pre = curved ? preact : nullptr;
+    a.mul = (const __bf16 *)mul, a.ld_mul = d->ld_mul ? d->ld_mul : N;
+    a.dz = !same && (dx || dw) ? (__bf16 *)ws : nullptr;
+    a.dmul = (__bf16 *)dmul;
+    a.part = dbias ? sums : nullptr;
+    a.N = N, a.act = d->act, a.groups = g;
+    const dim3 grid(dz_chunks(d), (N + kDzCols - 1) / kDzCols);
+    auto *k = d->act == CEP_RELU        ? k_linear_dz<CEP_RELU>
+              : d->act == CEP_SILU      ? k_linear_dz<CEP_SILU>
+              : d->act == CEP_GELU      ? k_linear_dz<CEP_GELU>
+              : d->act == CEP_GELU_TANH ? k_linear_dz<CEP_GELU_TANH>
+                                        : k_linear_dz<CEP_IDENTITY>;
+    hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
+  }
+  if (!same) dz = (const __bf16 *)ws, ld_z = N;
+  if (dbias)
+    hipLaunchKernelGGL(k_linear_dbias, dim3((N + 63) / 64, n_groups), dim3(256), 0, s, sums, N, g,
+                       dbias);
+  if (dx && T) {
+    Finish f{};
+    f.res = dx_add, f.y = dx, f.N = D, f.res_dtype = f.y_dtype = d->dx_dtype;
+    f.ld_res = f.ld_y = d->ld_dx ? d->ld_dx : D;
+    launch_linear<true>(plan_of(T, D, N, d->n_groups, false), g, dz, ld_z, (const __bf16 *)w, N, D, N,
+                        f, part, s);
+  }
+  if (dw) {
+    const Plan p = wgrad_plan(d);
+    WgradArgs a{};
+    a.A = (const __bf16 *)x, a.lda = d->ld_x ? d->ld_x : D;
+    a.B0 = dz, a.ldb = ld_z;
+    a.M = D, a.N = N, a.K = T, a.segs = 1, a.splits = p.splits;
+    a.groups = g, a.part = part;
+    a.f.y = dw, a.f.N = N, a.f.y_dtype = d->dw_dtype, a.f.ld_y = N;
+    const int64_t items = dense_tiles(p.tile, D, N) * p.splits;
+    const dim3 grid((unsigned)((items + 7) / 8 * 8 * n_groups));
+    if (p.tile == 0)
+      hipLaunchKernelGGL((k_linear_wgrad<128, 2, 4>), grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((k_linear_wgrad<64, 2, 2>), grid, dim3(256), 0, s, a);
+    if (p.splits > 1) launch_finish(part, p.splits, Groups{nullptr, 0, D}, a.f, D, s);
+  }
+  return launched(fn);
+}

@@ -13,9 +13,13 @@ ranks' segments of the send buffer to them; here they are only packed.  The
 gate's projection is a plain product and goes to the library.
 
 ``backward`` gives the gradients of the shared expert's weights, the norm's weight
-and the block's input.  The routed experts and the gate have no gradients of
-their own here, but y reaches the output through them too: a program that trains
-the norm, or anything before the block, passes that part of the gradient of y in.
+and the block's input.  The streamed experts have no gradient, but y reaches the
+output through them and the gate too: a program that trains the norm, or anything
+before the block, passes that part of the gradient of y in.  Where one rank holds
+every expert in bf16, it comes from
+
+    RoutedExperts.forward, .backward      cep_expert_sort, cep_linear, cep_expert_unsort
+    MoEBlock.gate_backward                cep_gate_topk_backward
 
 Run ``python -m paper_2609_33252_amd.moe_block`` for a small block on cuda:0.
 """
@@ -133,7 +137,7 @@ class MoEBlock:
         pre = torch.empty(T, 2, self.d_shared, device=y.device) if train else None
         cep.cep_gated_ffn(ffn, y, *self.shared, self.shared_y, self._ffn_space(ffn, train),
                           preact=pre, stream=s)
-        self.saved = (residual.clone(), y.clone(), pre) if train else None
+        self.saved = (residual.clone(), y.clone(), pre, logits) if train else None
         routed = self.routed[0, :T]
         routed.zero_()
         plan = self.plan.cpu()
@@ -163,7 +167,7 @@ class MoEBlock:
         they leave those paths out, as one addend of the gradients."""
         if self.saved is None:
             raise ValueError("backward without a forward(train=True) before it")
-        residual, y, pre = self.saved
+        residual, y, pre, _ = self.saved
         T, d, s = y.shape[0], self.d, torch.cuda.current_stream()
         BF16 = (torch.bfloat16,)
         _expect("d_out", d_out, y.device, BF16, (T, d))
@@ -187,10 +191,124 @@ class MoEBlock:
                                   stream=s)
         return dx, d_norm, dw
 
+    def gate_backward(self, d_topk_w):
+        """Gradients through the gate of a forward(train=True), from that of its
+        coefficients, float32 [T][top_k]: of y (float32 [T][d], an addend of
+        ``backward``'s d_y) and of the gate's weight (float32 [d][n_experts])."""
+        if self.saved is None:
+            raise ValueError("gate_backward without a forward(train=True) before it")
+        _, y, _, logits = self.saved
+        T = y.shape[0]
+        _expect("d_topk_w", d_topk_w, y.device, (torch.float32,), (T, self.top_k))
+        d_logits = torch.empty_like(logits)
+        cep.cep_gate_topk_backward(cep.make_gate(rows=T, **self.gate_args), logits, self.ids,
+                                   d_topk_w, d_logits, stream=torch.cuda.current_stream())
+        return d_logits @ self.gate.T, y.float().T @ d_logits
+
     def close(self):
         if self.ctx:
             cep.cep_destroy(self.ctx)
             self.ctx = None
+
+
+class RoutedExperts:
+    """Gated experts of one rank with gradients: w_gate, w_up [n_experts][d][d_ff] and
+    w_down [n_experts][d_ff][d], bf16, for up to max_tokens tokens a call.
+
+        sorted rows x of each expert       cep_expert_sort
+        u = x W_up, h = silu(x W_gate) u   cep_linear
+        h W_down, weighted and summed      cep_linear, cep_expert_unsort
+    """
+
+    def __init__(self, *, top_k, max_tokens, w_gate, w_up, w_down):
+        BF16 = (torch.bfloat16,)
+        if w_gate.dim() != 3:
+            raise ValueError("w_gate must be of shape [n_experts, d, d_ff]")
+        E, d, d_ff = w_gate.shape
+        _expect("w_gate", w_gate, w_gate.device, BF16, (E, d, d_ff))
+        _expect("w_up", w_up, w_gate.device, BF16, (E, d, d_ff))
+        _expect("w_down", w_down, w_gate.device, BF16, (E, d_ff, d))
+        self.E, self.d, self.d_ff, self.top_k, self.max_tokens = E, d, d_ff, top_k, max_tokens
+        self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
+        self.ws = self._buf(0, dtype=torch.uint8)
+        self.saved = None  # of the last forward pass, if that was a training one
+
+    def _buf(self, *shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device=self.w_gate.device)
+
+    def _space(self, need):
+        if self.ws.numel() < need:  # grows to the largest call's
+            self.ws = self._buf(need, dtype=torch.uint8)
+        return self.ws
+
+    def _linear(self, rows, d_in, d_out, act=cep.CEP_IDENTITY):
+        return cep.make_linear(rows=rows, d_in=d_in, d_out=d_out, n_groups=self.E, act=act,
+                               y_dtype=cep.CEP_BF16, dx_dtype=cep.CEP_BF16,
+                               dw_dtype=cep.CEP_BF16)
+
+    def _unsort(self, T, ys_dtype, y_dtype):
+        return cep.make_expert_unsort(rows=T, top_k=self.top_k, d=self.d,
+                                      sorted_rows=T * self.top_k, ys_dtype=ys_dtype,
+                                      y_dtype=y_dtype)
+
+    def forward(self, y, ids, w, train=False):
+        """y [T][d] bf16; ids int32 and w float32 [T][top_k] as cep_gate_topk leaves
+        them (-1: empty slot).  Returns float32 [T][d], each token's weighted sum."""
+        T, k, d, I, s = y.shape[0], self.top_k, self.d, self.d_ff, torch.cuda.current_stream()
+        if T > self.max_tokens:
+            raise ValueError(f"{T} tokens, the experts hold {self.max_tokens}")
+        dev, P = self.w_gate.device, T * k
+        _expect("y", y, dev, (torch.bfloat16,), (T, d))
+        _expect("ids", ids, dev, (torch.int32,), (T, k))
+        _expect("w", w, dev, (torch.float32,), (T, k))
+        sort = cep.make_expert_sort(rows=T, top_k=k, n_experts=self.E, capacity=P, row_bytes=2 * d)
+        plan, pair = self._buf(self.E + 2, dtype=torch.int32), self._buf(P, dtype=torch.int32)
+        place, x = self._buf(T, k, dtype=torch.int32), self._buf(P, d)
+        cep.cep_expert_sort(sort, ids, plan, pair, place,
+                            self._space(cep.cep_expert_sort_workspace(sort)), x=y, out_x=x,
+                            stream=s)
+        up, gate = self._linear(P, d, I), self._linear(P, d, I, cep.CEP_SILU)
+        down = self._linear(P, I, d)
+        ws = self._space(max(cep.cep_linear_workspace(q) for q in (up, gate, down)))
+        u, h, out = self._buf(P, I), self._buf(P, I), self._buf(P, d)
+        pre = self._buf(P, I, dtype=torch.float32) if train else None
+        cep.cep_linear(up, x, self.w_up, u, ws, offsets=plan, stream=s)
+        cep.cep_linear(gate, x, self.w_gate, h, ws, mul=u, offsets=plan, preact=pre, stream=s)
+        cep.cep_linear(down, h, self.w_down, out, ws, offsets=plan, stream=s)
+        total = self._buf(T, d, dtype=torch.float32)
+        cep.cep_expert_unsort(self._unsort(T, cep.CEP_BF16, cep.CEP_F32), out, place, total, w=w,
+                              stream=s)
+        self.saved = (plan, place, w.clone(), x, u, h, pre, out) if train else None
+        return total
+
+    def backward(self, d_total):
+        """Gradients of a forward(train=True) from that of its output (float32 or bf16
+        [T][d]): of y (float32 [T][d]), of the coefficients (float32 [T][top_k]) and
+        of w_gate, w_up and w_down (bf16)."""
+        if self.saved is None:
+            raise ValueError("backward without a forward(train=True) before it")
+        plan, place, w, x, u, h, pre, out = self.saved
+        T, P, d, I = place.shape[0], x.shape[0], self.d, self.d_ff
+        s, dev = torch.cuda.current_stream(), x.device
+        _expect("d_total", d_total, dev, (torch.float32, torch.bfloat16), (T, d))
+        kind = cep.CEP_F32 if d_total.dtype == torch.float32 else cep.CEP_BF16
+        d_out, d_w = torch.empty_like(out), torch.empty_like(w)
+        cep.cep_expert_unsort_backward(self._unsort(T, cep.CEP_BF16, kind), d_total, out, place, w,
+                                       d_out, d_w, stream=s)
+        up, gate = self._linear(P, d, I), self._linear(P, d, I, cep.CEP_SILU)
+        down = self._linear(P, I, d)
+        ws = self._space(max(cep.cep_linear_workspace(q, True) for q in (up, gate, down)))
+        dh, du, dx = torch.empty_like(h), torch.empty_like(u), torch.empty_like(x)
+        dw = [torch.empty_like(t) for t in (self.w_gate, self.w_up, self.w_down)]
+        cep.cep_linear_backward(down, d_out, h, self.w_down, ws, dx=dh, dw=dw[2], offsets=plan,
+                                stream=s)
+        cep.cep_linear_backward(gate, dh, x, self.w_gate, ws, dx=dx, dw=dw[0], preact=pre, mul=u,
+                                dmul=du, offsets=plan, stream=s)
+        cep.cep_linear_backward(up, du, x, self.w_up, ws, dx=dx, dw=dw[1], dx_add=dx, offsets=plan,
+                                stream=s)
+        d_y = self._buf(T, d, dtype=torch.float32)
+        cep.cep_expert_unsort(self._unsort(T, cep.CEP_BF16, cep.CEP_F32), dx, place, d_y, stream=s)
+        return d_y, d_w, dw
 
 
 def main():
@@ -206,14 +324,21 @@ def main():
                      gate=normal(d, E).float(),
                      shared=(normal(d, d_shared), normal(d, d_shared), normal(d_shared, d)),
                      experts=cep.make_weights(*experts), w_dtype=cep.CEP_BF16)
+    routed = RoutedExperts(top_k=k, max_tokens=2048, w_gate=experts[0], w_up=experts[1],
+                           w_down=experts[2])
     for T in (1, 100, 2048):
-        x, residual = normal(T, d, std=1.0), normal(T, d, std=1.0)
+        x, residual, d_out = normal(T, d, std=1.0), normal(T, d, std=1.0), normal(T, d)
         out = block.forward(x, residual, train=True)
-        dx, d_norm, _ = block.backward(normal(T, d))
+        # the gradient through the routed experts and the gate, then all of it
+        routed.forward(block.y[:T], block.ids[:T], block.w[:T], train=True)
+        d_y, d_w, _ = routed.backward(d_out)
+        d_gate_y, d_gate = block.gate_backward(d_w)
+        dx, d_norm, _ = block.backward(d_out, d_y=d_y + d_gate_y)
         torch.cuda.synchronize()
         print(f"{T} tokens: output rms {float(out.square().mean().sqrt()):.4f}, "
-              f"{int(block.plan[1])} rows sent, gradient rms of x through the shared expert "
-              f"{float(dx.float().square().mean().sqrt()):.6f}")
+              f"{int(block.plan[1])} rows sent, gradient rms of x "
+              f"{float(dx.float().square().mean().sqrt()):.6f}, of the gate "
+              f"{float(d_gate.square().mean().sqrt()):.6f}")
     block.close()
 
 

@@ -594,3 +594,126 @@ def test_replay_in_a_graph_beside_eager_work():
         torch.cuda.synchronize()
         for name in eager:
             assert torch.equal(eager[name], captured[name]), (i, name)
+
+
+def _whole_block(b, experts, x, res, k):
+    """The block in float64 as a function that autograd differentiates, with the
+    choice of experts held fixed; its leaves by name."""
+    leaf = lambda t: t.detach().double().requires_grad_()
+    p = dict(x=leaf(x), norm=leaf(b.norm), gate=leaf(b.gate),
+             **{n: leaf(t) for n, t in zip(("wg", "wu", "wd"), experts)})
+    s = p["x"] + res.double()
+    y = s / torch.sqrt((s * s).mean(-1, keepdim=True) + 1e-6) * p["norm"]
+    logits = y @ p["gate"]
+    w = torch.softmax(logits.gather(1, b.ids[:len(x)].long()), -1)
+    ffn = lambda a, wg, wu, wd: (torch.nn.functional.silu(a @ wg) * (a @ wu)) @ wd
+    out = ffn(y, *(t.double() for t in b.shared))
+    for e in range(len(experts[0])):
+        coef = torch.where(b.ids[:len(x)] == e, w, 0.0).sum(1, keepdim=True)
+        out = out + coef * ffn(y, p["wg"][e], p["wu"][e], p["wd"][e])
+    return out, p
+
+
+@pytest.mark.parametrize("T", [1, 9, 300])
+def test_block_gradients_through_the_routed_experts(T):
+    """MoEBlock and RoutedExperts together against the whole block differentiated in
+    float64: sums of terms with at most four bf16 roundings of random signs each on
+    their way (y, h, the gradients of z and of a sorted row): 2^-8 / 3^.5 each, and
+    a margin of two.  The gate's gradient has no such averaging: a coefficient's is
+    one product, <d_out, expert's row>, whose error is up to |d_out| times that of the
+    row (Cauchy-Schwarz), and c_j (g_j - sum c g) at most doubles the largest."""
+    from paper_2609_33252_amd import moe_block
+    d, I, E, k = 256, 128, 8, 3
+    g = _gen(T)
+    n = lambda *s, std=0.08: _randn(g, *s, std=std)
+    experts = [n(E, d, I), n(E, d, I), n(E, I, d)]
+    b = moe_block.MoEBlock(d=d, d_ff=I, d_shared=200, n_experts=E, top_k=k, n_ranks=1, rank=0,
+                           max_tokens=300, norm=1 + n(d).float(), gate=n(d, E).float(),
+                           shared=(n(d, 200), n(d, 200), n(200, d)),
+                           experts=cep.make_weights(*experts), w_dtype=cep.CEP_BF16)
+    routed = moe_block.RoutedExperts(top_k=k, max_tokens=300, w_gate=experts[0], w_up=experts[1],
+                                     w_down=experts[2])
+    # the sum x + residual is exact in bf16: it is saved without a rounding of its own
+    x = (torch.randint(-32, 33, (T, d), device="cuda", generator=g) / 16).bfloat16()
+    res, dout = torch.zeros_like(x), n(T, d, std=1.0)
+    out = b.forward(x, res, train=True)
+    total = routed.forward(b.y[:T], b.ids[:T], b.w[:T], train=True)
+    d_y, d_w, dw = routed.backward(dout)
+    again = routed.backward(dout.float())
+    d_gate_y, d_gate = b.gate_backward(d_w)
+    dx, d_norm, _ = b.backward(dout, d_y=d_y + d_gate_y)
+    ref, p = _whole_block(b, experts, x, torch.zeros_like(x), k)
+    ref.backward(dout.double())
+    lim = 2 * (4 / 3) ** 0.5 * 2.0 ** -8
+    rel = lambda got, want: float((got.double() - want).norm() / want.norm().clamp_min(1e-30))
+    assert rel(total + b.shared_y[:T], ref.detach()) < lim
+    assert rel(out, ref.detach()) < lim
+    place, rows = routed.saved[1], routed.saved[-1]
+    worst = rows[place.long().flatten()].double().norm(dim=1).view(T, k).amax(1)
+    most = (b.y[:T].double().norm(dim=1) * 2 * lim * worst * dout.double().norm(dim=1)).sum()
+    want = p["gate"].grad
+    assert (d_gate.double() - want).norm() < lim * want.norm() + most
+    for name, got in (("x", dx), ("norm", d_norm), ("wg", dw[0]), ("wu", dw[1]), ("wd", dw[2])):
+        assert rel(got, p[name].grad) < lim, name
+    assert torch.equal(again[1], d_w) and all(torch.equal(a, c) for a, c in zip(again[2], dw))
+    b.close()
+
+
+def test_routed_experts_refuse_what_their_operators_would_misread():
+    from paper_2609_33252_amd import moe_block
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    w = [torch.zeros(4, 64, 32, **bf), torch.zeros(4, 64, 32, **bf), torch.zeros(4, 32, 64, **bf)]
+    make = lambda a, b, c: moe_block.RoutedExperts(top_k=2, max_tokens=8, w_gate=a, w_up=b, w_down=c)
+    for i in range(3):
+        for wrong in (w[i].float(), w[i][:3], w[i].cpu(), w[i].transpose(1, 2)):
+            with pytest.raises(ValueError):
+                make(*[wrong if j == i else w[j] for j in range(3)])
+    r = make(*w)
+    y, ids = torch.zeros(8, 64, **bf), torch.zeros(8, 2, dtype=torch.int32, device="cuda")
+    c = torch.ones(8, 2, device="cuda")
+    with pytest.raises(ValueError):
+        r.backward(y)
+    for bad in ((y.float(), ids, c), (y[:, :32], ids, c), (y, ids.long(), c), (y, ids, c.double()),
+                (y, ids[:7], c), (torch.zeros(9, 64, **bf), ids, c)):
+        with pytest.raises(ValueError):
+            r.forward(*bad)
+    r.forward(y, ids, c)
+    with pytest.raises(ValueError):
+        r.backward(y)  # that pass kept nothing
+    r.forward(y, ids, c, train=True)
+    with pytest.raises(ValueError):
+        r.backward(y[:7])
+
+
+@pytest.mark.parametrize("seed", [0, 1])
+def test_routed_experts_match_differences(seed):
+    """Directional derivatives of the float64 form beside the gradients' product with
+    the direction, at the same tolerance as against the formula."""
+    from paper_2609_33252_amd import moe_block
+    T, d, I, E, k = 40, 64, 40, 5, 2
+    g = _gen(seed + 50)
+    w = [_randn(g, E, d, I, std=0.2), _randn(g, E, d, I, std=0.2), _randn(g, E, I, d, std=0.2)]
+    r = moe_block.RoutedExperts(top_k=k, max_tokens=T, w_gate=w[0], w_up=w[1], w_down=w[2])
+    y, dt = _randn(g, T, d), _randn(g, T, d)
+    ids = torch.randint(-1, E, (T, k), device="cuda", generator=g).int()
+    c = torch.rand(T, k, device="cuda", generator=g)
+    r.forward(y, ids, c, train=True)
+    d_y, d_c, dw = r.backward(dt)
+
+    def f(y, c, wg, wu, wd):
+        out = torch.zeros(T, d, dtype=torch.float64, device="cuda")
+        for e in range(E):
+            coef = torch.where(ids == e, c, 0.0).sum(1, keepdim=True)
+            out += coef * B.gated_ffn(y, wg[e], wu[e], wd[e])[3]
+        return (out * dt.double()).sum()
+
+    at = [t.double() for t in (y, c, *w)]
+    for i, grad in enumerate((d_y, d_c, *dw)):
+        # along the gradient itself: the product is its square's sum, and the bf16
+        # roundings on the way (2^-8 each, four) carry over as they are
+        v = grad.double() / grad.double().norm()
+        h = 1e-4
+        up, down = list(at), list(at)
+        up[i], down[i] = at[i] + h * v, at[i] - h * v
+        slope = float(f(*up) - f(*down)) / (2 * h)
+        assert abs(slope / float(grad.double().norm()) - 1) < 4 * U16, i

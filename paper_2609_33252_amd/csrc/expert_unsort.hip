@@ -33,8 +33,39 @@ __device__ inline int place_of(const UnsortArgs &a, int64_t pair) {
   return p < a.sorted ? p : -1;
 }
 
+// Eight consecutive values of a row as they are in memory, so that a row on the way
+// takes no more registers than bytes (n: those inside the row, the others zero).
+template <bool F32>
+struct Eight {
+  Vec16 v[F32 ? 2 : 1];
+  __device__ inline void load(const void *row, int64_t at, int n) {
+    if (n >= 8) {
+#pragma unroll
+      for (int h = 0; h < (F32 ? 2 : 1); ++h)
+        v[h] = *(const Any16 *)((const char *)row + at * (F32 ? 4 : 2) + 16 * h);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < (F32 ? 8 : 4); ++i) {
+      uint32_t u = 0;
+      if (F32) {
+        if (i < n) u = ((const uint32_t *)row)[at + i];
+      } else {
+        if (2 * i < n) u = ((const uint16_t *)row)[at + 2 * i];
+        if (2 * i + 1 < n) u |= (uint32_t)((const uint16_t *)row)[at + 2 * i + 1] << 16;
+      }
+      v[i / 4][i % 4] = u;
+    }
+  }
+  __device__ inline float operator[](int i) const {
+    if (F32) return __uint_as_float(v[i / 4][i % 4]);
+    const uint32_t u = v[0][i / 2];
+    return __uint_as_float(i % 2 ? u & 0xffff0000u : u << 16);
+  }
+};
+
 // A wave a token and 512 channels of it; the rows of all slots on the way at once.
-template <int KM>
+template <int KM, bool YS32>
 __global__ __launch_bounds__(256) void k_unsort(UnsortArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -44,12 +75,13 @@ __global__ __launch_bounds__(256) void k_unsort(UnsortArgs a) {
   const bool slot = lane < a.k;
   const int my = slot ? place_of(a, t * a.k + lane) : -1;
   const float mw = slot && a.w ? a.w[t * a.k + lane] : 1.0f;
-  float s[8] = {}, v[KM][8];
+  float s[8] = {};
+  Eight<YS32> v[KM];
   if (a.res) load8(a.res, a.res_dtype, t * a.ld_res + c, n, s);
 #pragma unroll
   for (int j = 0; j < KM; ++j) {
     const int p = __builtin_amdgcn_readlane(my, j);
-    if (j < a.k && p >= 0) load8(a.ys, a.ys_dtype, p * a.ld_ys + c, n, v[j]);
+    if (j < a.k && p >= 0) v[j].load(a.ys, p * a.ld_ys + c, n);
   }
 #pragma unroll
   for (int j = 0; j < KM; ++j) {
@@ -63,7 +95,7 @@ __global__ __launch_bounds__(256) void k_unsort(UnsortArgs a) {
 }
 
 // LANES threads a token, 8 channels each at a time.
-template <int LANES, int KM>
+template <int LANES, int KM, bool YS32>
 __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(UnsortArgs a) {
   __shared__ float part[LANES > 64 ? LANES / 64 : 1][KM];
   const int lane = threadIdx.x & 63, at = threadIdx.x % LANES;
@@ -77,12 +109,12 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(Unsor
     const int n = a.d - c;
     float g[8];
     load8(a.dy, a.y_dtype, t * a.ld_y + c, n, g);
-    float v[KM][8];
+    Eight<YS32> v[KM];
     if (a.dw) {
 #pragma unroll
       for (int j = 0; j < KM; ++j) {
         const int p = __builtin_amdgcn_readlane(my, j);
-        if (j < a.k && p >= 0) load8(a.ys, a.ys_dtype, p * a.ld_ys + c, n, v[j]);
+        if (j < a.k && p >= 0) v[j].load(a.ys, p * a.ld_ys + c, n);
       }
     }
 #pragma unroll
@@ -98,7 +130,7 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(Unsor
         float o[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = w * g[i];
-        store8(a.dys, a.ys_dtype, p * a.ld_ys + c, n, o);
+        store8(a.dys, YS32 ? CEP_F32 : CEP_BF16, p * a.ld_ys + c, n, o);
       }
     }
   }
@@ -121,12 +153,17 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(Unsor
   a.dw[t * a.k + at] = my >= 0 ? sum : 0.f;
 }
 
-template <int KM>
+template <int KM, bool YS32>
+void launch_unsort(const UnsortArgs &a, hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)a.rows * a.waves + 3) / 4));
+  hipLaunchKernelGGL((k_unsort<KM, YS32>), grid, dim3(256), 0, s, a);
+}
+template <int KM, bool YS32>
 void launch_grad(const UnsortArgs &a, hipStream_t s) {
   if (a.d <= 512)
-    hipLaunchKernelGGL((k_unsort_grad<64, KM>), dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_unsort_grad<64, KM, YS32>), dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_unsort_grad<256, KM>), dim3(a.rows), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_unsort_grad<256, KM, YS32>), dim3(a.rows), dim3(256), 0, s, a);
 }
 
 const char *bad_desc(const cep_expert_unsort_desc *d) {
@@ -169,9 +206,9 @@ CEP_API int cep_expert_unsort(const cep_expert_unsort_desc *d, const void *ys, c
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
   UnsortArgs a = args_of(d);
   a.ys = ys, a.place = place, a.w = w, a.res = residual, a.y = y;
-  const dim3 grid((unsigned)(((int64_t)a.rows * a.waves + 3) / 4));
-  if (a.k <= 8) hipLaunchKernelGGL(k_unsort<8>, grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_unsort<16>, grid, dim3(256), 0, s, a);
+  auto *launch = a.k <= 8 ? launch_unsort<8, false> : launch_unsort<16, false>;
+  if (a.ys_dtype == CEP_F32) launch = a.k <= 8 ? launch_unsort<8, true> : launch_unsort<16, true>;
+  launch(a, s);
   return launched(fn);
 }
 
@@ -189,7 +226,8 @@ CEP_API int cep_expert_unsort_backward(const cep_expert_unsort_desc *d, const vo
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
   UnsortArgs a = args_of(d);
   a.dy = dy, a.ys = ys, a.place = place, a.w = w, a.dys = dys, a.dw = dw;
-  if (a.k <= 8) launch_grad<8>(a, s);
-  else launch_grad<16>(a, s);
+  auto *launch = a.k <= 8 ? launch_grad<8, false> : launch_grad<16, false>;
+  if (a.ys_dtype == CEP_F32) launch = a.k <= 8 ? launch_grad<8, true> : launch_grad<16, true>;
+  launch(a, s);
   return launched(fn);
 }

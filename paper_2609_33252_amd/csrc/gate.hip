@@ -368,30 +368,55 @@ struct GateGradArgs {
   float scale;
 };
 
-// A wave a row: lane j holds slot j.
-template <int V>
+__device__ inline float grad_logit(const GateGradArgs &a, int64_t row, int e) {
+  return unmasked(a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
+                                      : ((const float *)a.logits)[row * a.ld + e]);
+}
+
+// LPR lanes a row, V experts a lane (chunk c of a lane is the four experts from (c *
+// LPR + lane) * 4); lane j holds slot j.  The slots' values meet their experts in
+// LDS, from which a row is written whole.
+template <int LPR, int V>
 __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (row >= a.rows) return;
-  auto logit_of = [&](int e) {
-    return unmasked(a.dtype == CEP_BF16 ? (float)((const __bf16 *)a.logits)[row * a.ld + e]
-                                        : ((const float *)a.logits)[row * a.ld + e]);
-  };
+  constexpr int ROWS = 256 / LPR;
+  __shared__ __attribute__((aligned(16))) float at[ROWS][LPR * V];
+  const int lane = threadIdx.x % LPR, sub = threadIdx.x / LPR;
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS + sub;
+  const bool live = row0 < a.rows;
+  const int64_t row = live ? row0 : a.rows - 1;
+  const bool all = !a.sigmoid && !a.normalize;  // every expert has a gradient
   int id = -1;
   float g = 0.f, l = -INFINITY;
   if (lane < a.k) {
-    const int i = a.ids[row * a.k + lane];
-    if (i >= 0 && i < a.E) {
-      id = i;
-      g = a.dw[row * a.k + lane] * a.scale;
-      l = logit_of(i);
-      if (l == -INFINITY) id = -1, g = 0.f;
+    id = a.ids[row * a.k + lane];
+    g = a.dw[row * a.k + lane] * a.scale;
+  }
+  float p[V];
+  if (all) {
+#pragma unroll
+    for (int c = 0; c < V / 4; ++c) {
+      const int e0 = (c * LPR + lane) * 4;
+      if (e0 + 4 <= a.E && a.dtype == CEP_F32) {
+        const Vec16 v = *(const Any16 *)((const float *)a.logits + row * a.ld + e0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[4 * c + i] = unmasked(__uint_as_float(v[i]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          p[4 * c + i] = e0 + i < a.E ? grad_logit(a, row, e0 + i) : -INFINITY;
+      }
     }
   }
-  float d[V] = {};
-  if (a.sigmoid || a.normalize) {
-    float s = 0.f, v = 0.f;
+#pragma unroll
+  for (int c = 0; c < V / 4; ++c)
+    *(float4 *)&at[sub][(c * LPR + lane) * 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (id < 0 || id >= a.E) id = -1;
+  if (id >= 0) l = grad_logit(a, row, id);
+  if (l == -INFINITY) id = -1;
+  if (id < 0) g = 0.f;
+  float v = g;  // of the slot
+  if (!all) {
+    float s = 0.f;
     if (a.sigmoid) {
       if (id >= 0) s = sigmoid(l);
     } else {
@@ -404,56 +429,73 @@ __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a) {
       const float sum = row_add<kMaxTopK>(s);
       const float c = sum > 0.f ? s / sum : 0.f;
       v = c * (g - row_add<kMaxTopK>(c * g));
-      if (a.sigmoid && id >= 0) v *= sigmoid(-l);
-    } else if (id >= 0) {
-      v = g * s * sigmoid(-l);
+    } else {
+      v = g * s;
     }
-    for (int j = 0; j < a.k; ++j) {
-      const int e = __builtin_amdgcn_readlane(id, j);
-      const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (e == i * 64 + lane) d[i] += u;
+    if (a.sigmoid && id >= 0) v *= sigmoid(-l);
+  }
+  // an expert that fills several slots: its first slot takes the sum, in their order
+  bool first = id >= 0;
+  float sum = 0.f;
+  for (int j = 0; j < a.k; ++j) {
+    const int e = __shfl(id, j, kMaxTopK);
+    const float u = __shfl(v, j, kMaxTopK);
+    if (e == id) {
+      first = first && j >= lane;
+      sum += u;
     }
-  } else {
-    float p[V], top = -INFINITY;
+  }
+  __syncthreads();
+  if (first && lane < a.k) at[sub][id] = sum;
+  __syncthreads();
+  float d[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * 64 + lane;
-      p[i] = e < a.E ? logit_of(e) : -INFINITY;
-      top = fmaxf(top, p[i]);
-    }
+  for (int c = 0; c < V / 4; ++c) {
+    const float4 q = *(const float4 *)&at[sub][(c * LPR + lane) * 4];
+    d[4 * c] = q.x, d[4 * c + 1] = q.y, d[4 * c + 2] = q.z, d[4 * c + 3] = q.w;
+  }
+  if (all) {
+    float top = -INFINITY, total = 0.f, dot = 0.f;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float sum = 0.f;
+    for (int i = 0; i < V; ++i) top = fmaxf(top, p[i]);
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       p[i] = p[i] > -INFINITY ? expf(p[i] - top) : 0.f;
-      sum += p[i];
+      total += p[i];
+      dot = fmaf(p[i], d[i], dot);
     }
-    sum = wave_sum(sum);
-    const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-    const float dot = row_add<kMaxTopK>(id >= 0 ? expf(l - top) * inv * g : 0.f);
-    const float all = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(dot)));
+    total = row_add<LPR>(total);
+    const float inv = total > 0.f ? 1.0f / total : 0.f;
+    dot = row_add<LPR>(dot) * inv;
 #pragma unroll
-    for (int i = 0; i < V; ++i) d[i] = -all;
-    for (int j = 0; j < a.k; ++j) {
-      const int e = __builtin_amdgcn_readlane(id, j);
-      const float u = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), j));
+    for (int i = 0; i < V; ++i) d[i] = (d[i] - dot) * (p[i] * inv);
+  }
+  if (!live) return;
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (e == i * 64 + lane) d[i] += u;
+  for (int c = 0; c < V / 4; ++c) {
+    const int e0 = (c * LPR + lane) * 4;
+    if (e0 + 4 <= a.E && a.dtype == CEP_F32) {
+      Vec16 u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(d[4 * c + i]);
+      *(Any16 *)((float *)a.dl + row * a.ld + e0) = u;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (e0 + i >= a.E) continue;
+        if (a.dtype == CEP_BF16) ((__bf16 *)a.dl)[row * a.ld + e0 + i] = (__bf16)d[4 * c + i];
+        else ((float *)a.dl)[row * a.ld + e0 + i] = d[4 * c + i];
+      }
     }
-#pragma unroll
-    for (int i = 0; i < V; ++i) d[i] *= p[i] * inv;
   }
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = i * 64 + lane;
-    if (e >= a.E) continue;
-    if (a.dtype == CEP_BF16) ((__bf16 *)a.dl)[row * a.ld + e] = (__bf16)d[i];
-    else ((float *)a.dl)[row * a.ld + e] = d[i];
-  }
+}
+
+template <int LPR, int V>
+void launch_gate_grad(const GateGradArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((k_gate_grad<LPR, V>), dim3((unsigned)(((int64_t)a.rows * LPR + 255) / 256)),
+                     dim3(256), 0, s, a);
 }
 
 const char *bad_desc(const cep_gate_desc *g, const float *bias) {
@@ -514,13 +556,11 @@ CEP_API int cep_gate_topk_backward(const cep_gate_desc *g, const void *logits,
   const GateGradArgs a{logits, topk_id, d_topk_w, d_logits, g->ld ? g->ld : g->n_experts, g->rows,
                        g->n_experts, g->top_k, g->logit_dtype, g->score == CEP_SIGMOID,
                        g->normalize != 0, g->scale};
-  const dim3 grid((unsigned)((a.rows + 3) / 4));
-  auto *k = a.E <= 64    ? k_gate_grad<1>
-            : a.E <= 128 ? k_gate_grad<2>
-            : a.E <= 192 ? k_gate_grad<3>
-            : a.E <= 256 ? k_gate_grad<4>
-            : a.E <= 512 ? k_gate_grad<8>
-                         : k_gate_grad<16>;
-  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
+  if (a.E <= 64) launch_gate_grad<16, 4>(a, s);
+  else if (a.E <= 128) launch_gate_grad<16, 8>(a, s);
+  else if (a.E <= 192) launch_gate_grad<16, 12>(a, s);
+  else if (a.E <= 256) launch_gate_grad<16, 16>(a, s);
+  else if (a.E <= 512) launch_gate_grad<64, 8>(a, s);
+  else launch_gate_grad<64, 16>(a, s);
   return launched(fn);
 }

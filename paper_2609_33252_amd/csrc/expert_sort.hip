@@ -18,8 +18,10 @@ namespace {
 
 constexpr int kMaxSortExperts = 1024;
 constexpr int kFewPairs = 4096;     // placed by one launch
-constexpr int kSortPairs = 2048;    // pairs of a k_sort_count block, a quarter a wave
+constexpr int kSortPairs = 1024;    // pairs of a k_sort_count block, a quarter a wave
 constexpr int kSortTokens = 4;      // tokens of a k_sort_rows block, one a wave
+// Counts (blocks times buckets) up to which k_sort_rows sums them itself, and buckets.
+constexpr int kFusedSums = 8192, kFusedCounts = 512;
 
 struct SortArgs {
   const int32_t *ids;  // [rows][k]
@@ -44,6 +46,22 @@ __device__ inline int wave_upto(int v) {
     if (lane >= o) v += u;
   }
   return v;
+}
+
+// Sum over the wave, by adds that read neighbouring lanes: within rows of 16, then a
+// row's last lane into the next rows.
+template <int CTRL, int ROWS>
+__device__ inline int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ inline int wave_total(int v) {
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  v = dpp_add<0x143, 0xc>(v);
+  return __builtin_amdgcn_readlane(v, 63);
 }
 
 // A wave walks its quarter of the block's pairs 64 at a time, lanes with the same
@@ -168,8 +186,14 @@ __device__ inline void copy_tail(const SortArgs &a, const char *src, int place) 
   }
 }
 
+// SCANNED: k_sort_scan ran.  Otherwise the workgroup sums the blocks' counts itself,
+// while its rows are on the way.
+template <bool SCANNED>
 __global__ __launch_bounds__(64 * kSortTokens) void k_sort_rows(SortArgs a) {
   __shared__ int32_t off[kMaxSortExperts + 1];
+  __shared__ int32_t sums[SCANNED ? 1 : 3][SCANNED ? 1 : kFusedCounts];  // all, before the
+                                                                         // first pair's block
+                                                                         // and the one after
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = (int64_t)blockIdx.x * kSortTokens + wave;
   const bool live = t < a.rows, copies = live && a.x;
@@ -182,14 +206,32 @@ __global__ __launch_bounds__(64 * kSortTokens) void k_sort_rows(SortArgs a) {
     at = a.place[p];
     if (at >= 0) {
       id = a.ids[p];
-      before = a.counts[p / kSortPairs * (a.E + 1) + id];
+      if (SCANNED) before = a.counts[p / kSortPairs * (a.E + 1) + id];
     }
   }
-  if (wave == 0) scan_totals(a.total, a.E, off);
+  // (the workgroup's pairs are fewer than a block's, so they lie in two at most)
+  const int b0 = (int)((int64_t)blockIdx.x * kSortTokens * a.k / kSortPairs);
+  if (!SCANNED) {
+    for (int e = tid; e <= a.E; e += 64 * kSortTokens) {
+      int run = 0, before0 = 0, before1 = 0;
+#pragma unroll 8
+      for (int b = 0; b < a.blocks; ++b) {
+        const int n = a.counts[b * (a.E + 1) + e];
+        run += n;
+        before0 += b < b0 ? n : 0;
+        before1 += b <= b0 ? n : 0;
+      }
+      sums[0][e] = run, sums[1][e] = before0, sums[2][e] = before1;
+    }
+    __syncthreads();
+    if (at >= 0) before = sums[p / kSortPairs > b0 ? 2 : 1][id];
+  }
+  const int32_t *total = SCANNED ? a.total : sums[0];
+  if (wave == 0) scan_totals(total, a.E, off);
   __syncthreads();
   if (blockIdx.x == 0) {
     for (int e = tid; e <= a.E; e += 64 * kSortTokens) a.plan[e] = off[e];
-    if (tid == 0) a.plan[a.E + 1] = a.total[a.E];
+    if (tid == 0) a.plan[a.E + 1] = total[a.E];
   }
   if (!live) return;
   int place = -1;
@@ -218,9 +260,17 @@ __global__ __launch_bounds__(256) void k_sort_few(SortArgs a) {
   if (token == a.rows) {  // uniform over the workgroup
     for (int e = tid; e <= a.E; e += 256) total[e] = 0;
     __syncthreads();
-    for (int p = tid; p < pairs; p += 256) {
-      const int b = bucket_of(a.ids[p], a.E);
-      if (b >= 0) atomicAdd(&total[b], 1);
+    constexpr int kOnTheWay = 8;  // loads
+    for (int p0 = tid; p0 < pairs; p0 += 256 * kOnTheWay) {
+      int b[kOnTheWay];
+#pragma unroll
+      for (int u = 0; u < kOnTheWay; ++u)
+        b[u] = p0 + u * 256 < pairs ? a.ids[p0 + u * 256] : -1;
+#pragma unroll
+      for (int u = 0; u < kOnTheWay; ++u) {
+        const int e = bucket_of(b[u], a.E);
+        if (e >= 0) atomicAdd(&total[e], 1);
+      }
     }
     __syncthreads();
     if (wave == 0) scan_totals(total, a.E, off);
@@ -234,21 +284,31 @@ __global__ __launch_bounds__(256) void k_sort_few(SortArgs a) {
   Vec16 v[kChunks] = {};
   if (a.x) load_row<256>(a, src, wave * 64, v);
   const int own = lane < a.k ? a.ids[token * a.k + lane] : -1;
-  int first[kMaxTopK] = {};  // the wave's pairs that come before slot j's
-  for (int p0 = wave * 64; p0 < pairs; p0 += 256) {
-    const int p = p0 + lane;
-    const int id = p < pairs ? a.ids[p] : -1;
-    const bool valid = id >= 0 && id < a.E;
+  // (id, index) as one number, below 2^22
+  const int mine = own >= 0 && own < a.E ? own * pairs + token * a.k + lane : 0;
+  int first[kMaxTopK] = {};  // of the lane's pairs, those that come before slot j's
+  constexpr int kAhead = 4;  // loads on the way
+  for (int p0 = tid; p0 < pairs; p0 += 256 * kAhead) {
+    int key[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int p = p0 + u * 256, id = p < pairs ? a.ids[p] : -1;
+      key[u] = id >= 0 && id < a.E ? id * pairs + p : INT32_MAX;
+    }
 #pragma unroll
     for (int j = 0; j < kMaxTopK; ++j) {
-      const int e = __builtin_amdgcn_readlane(own, j);
-      if (j < a.k)
-        first[j] += (int)__popcll(__ballot(valid && (id < e || (id == e && p < token * a.k + j))));
+      if (j >= a.k) continue;
+      const int at = __builtin_amdgcn_readlane(mine, j);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) first[j] += key[u] < at;
     }
   }
 #pragma unroll
-  for (int j = 0; j < kMaxTopK; ++j)
-    if (lane == 0) sum[wave][j] = first[j];
+  for (int j = 0; j < kMaxTopK; ++j) {
+    if (j >= a.k) continue;
+    const int n = wave_total(first[j]);
+    if (lane == 0) sum[wave][j] = n;
+  }
   __syncthreads();
   int place = -1;
   if (lane < a.k && own >= 0 && own < a.E)
@@ -318,9 +378,13 @@ CEP_API int cep_expert_sort(const cep_expert_sort_desc *d, const int32_t *topk_i
     hipLaunchKernelGGL(k_sort_few, dim3(d->rows + 1), dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(k_sort_scan, dim3(E / 4 + 1), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(k_sort_rows, dim3((d->rows + kSortTokens - 1) / kSortTokens),
-                       dim3(64 * kSortTokens), 0, s, a);
+    const dim3 grid((d->rows + kSortTokens - 1) / kSortTokens), threads(64 * kSortTokens);
+    if (E < kFusedCounts && (int64_t)blocks * (E + 1) <= kFusedSums) {
+      hipLaunchKernelGGL(k_sort_rows<false>, grid, threads, 0, s, a);
+    } else {
+      hipLaunchKernelGGL(k_sort_scan, dim3(E / 4 + 1), dim3(256), 0, s, a);
+      hipLaunchKernelGGL(k_sort_rows<true>, grid, threads, 0, s, a);
+    }
   }
   return launched(fn);
 }

@@ -68,7 +68,7 @@ def test_sort_refuses_arguments():
     _refused(cep.CEP_ENOMEM, f, _sort(), PTR, PTR, PTR, PTR, BIG[:16])
     _refused(cep.CEP_EINVAL, f, _sort(rows=0), None, None, None, None, BIG)
     assert cep.cep_expert_sort_workspace(_sort(rows=1 << 21, top_k=16, n_experts=1024)) \
-        == 4 * ((1 << 25) // 2048 + 1) * 1025
+        == 4 * ((1 << 25) // 1024 + 1) * 1025
 
 
 # ----------------------------------------------------------------- unsort

@@ -75,6 +75,9 @@ SORTS = [
     (600, 8, 64, 131072, 0, "few"), (20000, 16, 1023, 8, 0, "any"),
     (4096, 8, 1, 48, 0, "any"), (4097, 8, 64, 48, 0, "one"), (4097, 2, 64, 48, 0, "none"),
     (1 << 17, 16, 300, 1, 0, "any"),
+    # the counts summed by the rows' workgroups, up to both limits, and past them
+    (600, 15, 511, 40, 0, "any"), (600, 15, 512, 40, 0, "any"), (1024, 16, 510, 24, 0, "few"),
+    (1025, 16, 511, 24, 0, "any"), (9000, 11, 80, 33, 0, "any"), (9400, 11, 80, 33, 0, "any"),
 ]
 
 

@@ -43,6 +43,10 @@ __device__ inline int piece_of(int items, int x) { return items / 8 + (x < items
 // out(m, n, v, w) takes the sums of four columns from n of row m, w those of the
 // second product.  A has k or m contiguous (A_K), B k or n (B_K).
 //
+// STAGED: the sums go through LDS first, and out.load(m, n) and out.store(m, n, v, w,
+// loaded) take eight columns of a row, four rows' loads on the way at once: for an
+// epilogue that reads a matrix of its own.
+//
 // Each operand's 64-wide step is two halves of HALF rows (columns), loaded
 // straight to LDS; the operands' halves meet in four quadrants, one phase
 // each, in which a wave multiplies HALF/WM x HALF/WN outputs (16 matrix
@@ -68,7 +72,7 @@ __device__ inline int piece_of(int items, int x) { return items / 8 + (x < items
 // the time at 2.1 GHz.  Bound inside the CU: without the loads the pass is 15 %
 // shorter, without the LDS reads 18 %, with neither 31 %, with every load an L2
 // hit 4 %.
-template <int HALF, int WM, int WN, bool A_K, bool B_K, bool DUAL, class Out>
+template <int HALF, int WM, int WN, bool A_K, bool B_K, bool DUAL, bool STAGED = false, class Out>
 __device__ inline void dense_tile(const TileArgs &a, int m0, int n0, int share, uint8_t *lds,
                                   Out out) {
   constexpr int MF = HALF / 16 / WM, NF = HALF / 16 / WN;  // fragments of a wave in a half
@@ -301,22 +305,63 @@ __device__ inline void dense_tile(const TileArgs &a, int m0, int n0, int share, 
     }
   }
 
-  // lane: row lane % 16 of a fragment, four columns from 4 (lane / 16)
+  if constexpr (STAGED) {
+    static_assert(!DUAL, "one product");
+    // half of the rows at a time: [HALF][2 HALF] float32, 16-byte chunk c of row r at c ^
+    // (r % 16)
+    constexpr int TN = 2 * HALF, PER = TN / 8, ROWS = WM * WN * 64 / PER, AT_ONCE = 4;
+    auto at = [&](int r, int chunk) { return (f32x4 *)(lds + r * TN * 4 + ((chunk ^ (r & 15)) << 4)); };
+    auto meet = [] {
+      wait_lgkm0();
+      asm volatile("s_barrier" ::: "memory");
+    };
 #pragma unroll
-  for (int mh = 0; mh < 2; ++mh)
+    for (int mh = 0; mh < 2; ++mh) {
+      if (mh) meet();
 #pragma unroll
-    for (int i = 0; i < MF; ++i) {
-      const int64_t m = m0 + mh * HALF + (wm * MF + i) * 16 + l15;
-      if (m >= a.M) continue;
+      for (int i = 0; i < MF; ++i)
 #pragma unroll
-      for (int nh = 0; nh < (DUAL ? 1 : 2); ++nh)
+        for (int nh = 0; nh < 2; ++nh)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) {
-          const int n = n0 + nh * HALF + (wn * NF + j) * 16 + g4 * 4;
-          if (n >= a.N) continue;
-          out(m, n, acc[mh][nh][i][j], acc[mh][1][i][j]);
+          for (int j = 0; j < NF; ++j)
+            *at((wm * MF + i) * 16 + l15, (nh * HALF + (wn * NF + j) * 16) / 4 + g4) = acc[mh][nh][i][j];
+      meet();
+      const int c8 = tid % PER, n = n0 + c8 * 8;
+      if (n < a.N) {
+        for (int r0 = tid / PER; r0 < HALF; r0 += AT_ONCE * ROWS) {
+          decltype(out.load(0, 0)) in[AT_ONCE];
+#pragma unroll
+          for (int u = 0; u < AT_ONCE; ++u) {
+            const int64_t m = m0 + mh * HALF + r0 + u * ROWS;
+            if (m < a.M) in[u] = out.load(m, n);
+          }
+#pragma unroll
+          for (int u = 0; u < AT_ONCE; ++u) {
+            const int r = r0 + u * ROWS;
+            const int64_t m = m0 + mh * HALF + r;
+            if (m < a.M) out.store(m, n, *at(r, 2 * c8), *at(r, 2 * c8 + 1), in[u]);
+          }
         }
+      }
     }
+  } else {
+    // lane: row lane % 16 of a fragment, four columns from 4 (lane / 16)
+#pragma unroll
+    for (int mh = 0; mh < 2; ++mh)
+#pragma unroll
+      for (int i = 0; i < MF; ++i) {
+        const int64_t m = m0 + mh * HALF + (wm * MF + i) * 16 + l15;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int nh = 0; nh < (DUAL ? 1 : 2); ++nh)
+#pragma unroll
+          for (int j = 0; j < NF; ++j) {
+            const int n = n0 + nh * HALF + (wn * NF + j) * 16 + g4 * 4;
+            if (n >= a.N) continue;
+            out(m, n, acc[mh][nh][i][j], acc[mh][1][i][j]);
+          }
+      }
+  }
 }
 
 // Tile and K shares of a product.

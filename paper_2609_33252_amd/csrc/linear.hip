@@ -173,6 +173,74 @@ __device__ inline void finish(const Finish &f, int64_t m, int n, int g, f32x4 z)
   store4(f.y, f.y_dtype, m * f.ld_y + n, v);
 }
 
+// The same for eight columns, in two steps.
+struct Loaded {
+  Vec16 mul, res[2];
+};
+__device__ inline Loaded load_eight(const Finish &f, int64_t m, int n) {
+  Loaded in;
+  if (f.mul) in.mul = *(const Vec16 *)(f.mul + m * f.ld_mul + n);
+  if (f.res) {
+    const char *p = (const char *)f.res + (m * f.ld_res + n) * (f.res_dtype == CEP_F32 ? 4 : 2);
+    in.res[0] = *(const Vec16 *)p;
+    if (f.res_dtype == CEP_F32) in.res[1] = *(const Vec16 *)(p + 16);
+  }
+  return in;
+}
+__device__ inline f32x4 half_of(const Vec16 &v, int h) {  // four of eight bf16 values
+  return f32x4{__uint_as_float(v[2 * h] << 16), __uint_as_float(v[2 * h] & 0xffff0000u),
+               __uint_as_float(v[2 * h + 1] << 16), __uint_as_float(v[2 * h + 1] & 0xffff0000u)};
+}
+template <int ACT>
+__device__ inline void finish_eight(const Finish &f, int64_t m, int n, int g, const f32x4 &lo,
+                                    const f32x4 &hi, const Loaded &in) {
+  f32x4 v[2] = {lo, hi};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (f.bias) v[h] += *(const f32x4 *)(f.bias + (int64_t)g * f.N + n + 4 * h);
+    if (f.pre) *(f32x4 *)(f.pre + m * f.N + n + 4 * h) = v[h];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[h][r] = act_of<ACT>(v[h][r]);
+    if (f.mul) v[h] *= half_of(in.mul, h);
+    if (f.res) v[h] += f.res_dtype == CEP_F32 ? __builtin_bit_cast(f32x4, in.res[h]) : half_of(in.res[0], h);
+  }
+  if (f.y_dtype == CEP_F32) {
+    *(f32x4 *)((float *)f.y + m * f.ld_y + n) = v[0];
+    *(f32x4 *)((float *)f.y + m * f.ld_y + n + 4) = v[1];
+  } else {
+    *(Vec16 *)((__bf16 *)f.y + m * f.ld_y + n) =
+        Vec16{bf16_pair(v[0][0], v[0][1]), bf16_pair(v[0][2], v[0][3]), bf16_pair(v[1][0], v[1][1]),
+              bf16_pair(v[1][2], v[1][3])};
+  }
+}
+
+// Where a tile's sums go, row 0 of the tile's matrix being row `row0` of the
+// epilogue's: the epilogue, or with K shares their lines of part.
+template <int ACT>
+struct TileOut {
+  const Finish &f;
+  int64_t row0;
+  int g;
+  float *part;  // of this share, null: one share
+  __device__ inline Loaded load(int64_t m, int n) const {
+    return part ? Loaded{} : load_eight(f, row0 + m, n);
+  }
+  __device__ inline void store(int64_t m, int n, const f32x4 &lo, const f32x4 &hi,
+                               const Loaded &in) const {
+    if (part) {
+      float *p = part + (row0 + m) * f.N + n;
+      *(f32x4 *)p = lo;
+      *(f32x4 *)(p + 4) = hi;
+    } else {
+      finish_eight<ACT>(f, row0 + m, n, g, lo, hi, in);
+    }
+  }
+  __device__ inline void operator()(int64_t m, int n, const f32x4 &v, const f32x4 &) const {
+    if (part) *(f32x4 *)(part + (row0 + m) * f.N + n) = v;
+    else finish<ACT>(f, row0 + m, n, g, v);
+  }
+};
+
 // ---- tiled product
 
 struct LinearArgs : TileArgs {  // M: unused with groups
@@ -183,7 +251,7 @@ struct LinearArgs : TileArgs {  // M: unused with groups
 };
 
 // y (B_K false) or dx (true: N is d_in) in tiles of whole groups' rows.
-template <int HALF, int WM, int WN, bool B_K, int ACT>
+template <int HALF, int WM, int WN, bool B_K, bool STAGED, int ACT>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear(LinearArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
   const int x = blockIdx.x & 7, at = blockIdx.x >> 3;
@@ -198,13 +266,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear(LinearArgs a) {
   t.A += tile.rows.lo * a.lda;
   t.B0 += tile.g * a.w_stride;
   t.M = tile.rows.n;
-  dense_tile<HALF, WM, WN, true, B_K, false>(
-      t, tile.m0, nt * 2 * HALF, share, lds,
-      [&](int64_t m, int n, const f32x4 &v, const f32x4 &) {
-        m += tile.rows.lo;
-        if (a.splits == 1) finish<ACT>(a.f, m, n, tile.g, v);
-        else *(f32x4 *)(a.part + ((int64_t)share * a.groups.rows + m) * a.N + n) = v;
-      });
+  const TileOut<ACT> out{a.f, tile.rows.lo, tile.g,
+                         a.splits > 1 ? a.part + (int64_t)share * a.groups.rows * a.N : nullptr};
+  dense_tile<HALF, WM, WN, true, B_K, false, STAGED>(t, tile.m0, nt * 2 * HALF, share, lds, out);
 }
 
 // The shares' sums of a row, added in order, and what becomes of them.
@@ -251,13 +315,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
     t.B0 += lo * a.ldb;
     t.K = __builtin_amdgcn_readfirstlane(s.n);
   }
-  const int64_t w0 = (int64_t)g * a.M;
-  dense_tile<HALF, WM, WN, false, false, false>(
-      t, (mt - share * n_tm) * 2 * HALF, nt * 2 * HALF, share, lds,
-      [&](int64_t m, int n, const f32x4 &v, const f32x4 &) {
-        if (a.splits == 1) finish<CEP_IDENTITY>(a.f, w0 + m, n, 0, v);
-        else *(f32x4 *)(a.part + ((int64_t)share * a.M + m) * a.N + n) = v;
-      });
+  const TileOut<CEP_IDENTITY> out{a.f, (int64_t)g * a.M, 0,
+                                  a.splits > 1 ? a.part + (int64_t)share * a.M * a.N : nullptr};
+  dense_tile<HALF, WM, WN, false, false, false>(t, (mt - share * n_tm) * 2 * HALF, nt * 2 * HALF,
+                                                share, lds, out);
 }
 
 // ---- few rows: the weights are streamed
@@ -485,14 +546,19 @@ void launch_finish(const float *part, int splits, const Groups &g, const Finish 
                      g, f);
 }
 
+// The epilogue is staged except where it is a plain store (us, staged and not: 777 x
+// 6144 x 2560 with bias and residual 42, 47; 8192 x 2048 x 4096 in eight groups with
+// a factor 212, 229; plain 4095 x 4096 x 2048 68, 64).
 template <int HALF, int WM, int WN, bool B_K>
 void launch_tiles(const LinearArgs &a, dim3 grid, hipStream_t s) {
-  auto *k = k_linear<HALF, WM, WN, B_K, CEP_IDENTITY>;
-  if constexpr (!B_K) {
-    if (a.f.act == CEP_RELU) k = k_linear<HALF, WM, WN, B_K, CEP_RELU>;
-    if (a.f.act == CEP_SILU) k = k_linear<HALF, WM, WN, B_K, CEP_SILU>;
-    if (a.f.act == CEP_GELU) k = k_linear<HALF, WM, WN, B_K, CEP_GELU>;
-    if (a.f.act == CEP_GELU_TANH) k = k_linear<HALF, WM, WN, B_K, CEP_GELU_TANH>;
+  auto *k = k_linear<HALF, WM, WN, B_K, true, CEP_IDENTITY>;
+  if constexpr (B_K) {
+    if (!a.f.res) k = k_linear<HALF, WM, WN, B_K, false, CEP_IDENTITY>;
+  } else {
+    if (a.f.act == CEP_RELU) k = k_linear<HALF, WM, WN, B_K, true, CEP_RELU>;
+    if (a.f.act == CEP_SILU) k = k_linear<HALF, WM, WN, B_K, true, CEP_SILU>;
+    if (a.f.act == CEP_GELU) k = k_linear<HALF, WM, WN, B_K, true, CEP_GELU>;
+    if (a.f.act == CEP_GELU_TANH) k = k_linear<HALF, WM, WN, B_K, true, CEP_GELU_TANH>;
   }
   hipLaunchKernelGGL(k, grid, dim3(WM * WN * 64), 0, s, a);
 }

@@ -309,7 +309,8 @@ __device__ inline void dense_tile(const TileArgs &a, int m0, int n0, int share, 
     static_assert(!DUAL, "one product");
     // half of the rows at a time: [HALF][2 HALF] float32, 16-byte chunk c of row r at c ^
     // (r % 16)
-    constexpr int TN = 2 * HALF, PER = TN / 8, ROWS = WM * WN * 64 / PER, AT_ONCE = 4;
+    constexpr int TN = 2 * HALF, PER = TN / 8, ROWS = WM * WN * 64 / PER;
+    constexpr int AT_ONCE = HALF / ROWS < 4 ? HALF / ROWS : 4;
     auto at = [&](int r, int chunk) { return (f32x4 *)(lds + r * TN * 4 + ((chunk ^ (r & 15)) << 4)); };
     auto meet = [] {
       wait_lgkm0();

@@ -250,25 +250,64 @@ struct LinearArgs : TileArgs {  // M: unused with groups
   Finish f;
 };
 
-// y (B_K false) or dx (true: N is d_in) in tiles of whole groups' rows.
-template <int HALF, int WM, int WN, bool B_K, bool STAGED, int ACT>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear(LinearArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+// Tile L of an order of tiles: its rows, columns and share.
+template <int SIZE, bool B_K, bool STAGED, int ACT>
+struct TileWork {
+  const LinearArgs &a;
+  int n_tm, n_tn;
+  uint8_t *lds;
+  // PART of the tile's height and width from row m0 + SIZE / PART * row, ...
+  template <int HALF, int WM, int WN>
+  __device__ inline void run(int L, int row, int col) const {
+    int mt, nt;
+    tile_of<kGroupM>(L, n_tm * a.splits, n_tn, &mt, &nt);
+    const int share = mt / n_tm;
+    const RowTile tile = tile_at<SIZE>(a.groups, mt - share * n_tm);
+    TileArgs t = a;
+    t.A += tile.rows.lo * a.lda;
+    t.B0 += tile.g * a.w_stride;
+    t.M = tile.rows.n;
+    const int m0 = tile.m0 + row * 2 * HALF, n0 = nt * SIZE + col * 2 * HALF;
+    if (m0 >= t.M || n0 >= t.N) return;
+    const TileOut<ACT> out{a.f, tile.rows.lo, tile.g,
+                           a.splits > 1 ? a.part + (int64_t)share * a.groups.rows * a.N : nullptr};
+    dense_tile<HALF, WM, WN, true, B_K, false, STAGED>(t, m0, n0, share, lds, out);
+  }
+};
+
+// y (B_K false) or dx (true: N is d_in) in 128-wide tiles of whole groups' rows.
+template <bool B_K, bool STAGED, int ACT>
+__global__ __launch_bounds__(256, 2) void k_linear_128(LinearArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[65536];
   const int x = blockIdx.x & 7, at = blockIdx.x >> 3;
-  const int n_tm = tiles_of<2 * HALF>(a.groups), n_tn = (a.N + 2 * HALF - 1) / (2 * HALF);
-  const int items = n_tm * a.splits * n_tn;
+  const TileWork<128, B_K, STAGED, ACT> work{a, tiles_of<128>(a.groups), (a.N + 127) / 128, lds};
+  const int items = work.n_tm * a.splits * work.n_tn;
   if (at >= piece_of(items, x)) return;
-  int mt, nt;
-  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + at, n_tm * a.splits, n_tn, &mt, &nt);
-  const int share = mt / n_tm;
-  const RowTile tile = tile_at<2 * HALF>(a.groups, mt - share * n_tm);
-  TileArgs t = a;
-  t.A += tile.rows.lo * a.lda;
-  t.B0 += tile.g * a.w_stride;
-  t.M = tile.rows.n;
-  const TileOut<ACT> out{a.f, tile.rows.lo, tile.g,
-                         a.splits > 1 ? a.part + (int64_t)share * a.groups.rows * a.N : nullptr};
-  dense_tile<HALF, WM, WN, true, B_K, false, STAGED>(t, tile.m0, nt * 2 * HALF, share, lds, out);
+  work.template run<64, 2, 2>(x * (items / 8) + min(x, items % 8) + at, 0, 0);
+}
+
+// ... in 256-wide ones, one a compute unit.  Where a few are left after the last full
+// round, those are cut into quarters: up to two rounds of them (of 64 steps 38 us each)
+// cost less than one of whole tiles (101 us).
+constexpr int kUnits = 256;
+__host__ __device__ inline int whole_tiles(int items) {
+  const int full = items / kUnits * kUnits;
+  return full && (items - full) * 4 <= 2 * kUnits ? full : items;
+}
+template <bool B_K, bool STAGED, int ACT>
+__global__ __launch_bounds__(512, 2) void k_linear_256(LinearArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[131072];
+  const TileWork<256, B_K, STAGED, ACT> work{a, tiles_of<256>(a.groups), (a.N + 255) / 256, lds};
+  const int items = work.n_tm * a.splits * work.n_tn, whole = whole_tiles(items);
+  const int x = blockIdx.x & 7, at = blockIdx.x >> 3;
+  if (at < piece_of(whole, x)) {
+    work.template run<128, 2, 4>(x * (whole / 8) + min(x, whole % 8) + at, 0, 0);
+  } else if (whole < items) {  // `whole` is then a multiple of 8
+    const int quarters = (items - whole) * 4, q = at - whole / 8;
+    if (q >= piece_of(quarters, x)) return;
+    const int i = x * (quarters / 8) + min(x, quarters % 8) + q;
+    work.template run<64, 2, 4>(whole + i / 4, i & 1, i >> 1 & 1);
+  }
 }
 
 // The shares' sums of a row, added in order, and what becomes of them.
@@ -500,6 +539,11 @@ Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
   const DensePlan d = plan_tiles(tiles, K / 64, (double)rows * N, 16);
   p.tile = d.tile;
   p.splits = d.splits;
+  // 256-wide tiles with quarters, which that estimate does not know
+  const int whole = whole_tiles((int)tiles[0]), quarters = ((int)tiles[0] - whole) * 4;
+  const double us = (double)((whole + kUnits - 1) / kUnits) * (12 + 1.4 * (K / 64)) +
+                    (double)((quarters + kUnits - 1) / kUnits) * (3 + 0.55 * (K / 64));
+  if (us < d.us) p.tile = 0, p.splits = 1;
   return p;
 }
 
@@ -549,18 +593,26 @@ void launch_finish(const float *part, int splits, const Groups &g, const Finish 
 // The epilogue is staged except where it is a plain store (us, staged and not: 777 x
 // 6144 x 2560 with bias and residual 42, 47; 8192 x 2048 x 4096 in eight groups with
 // a factor 212, 229; plain 4095 x 4096 x 2048 68, 64).
-template <int HALF, int WM, int WN, bool B_K>
-void launch_tiles(const LinearArgs &a, dim3 grid, hipStream_t s) {
-  auto *k = k_linear<HALF, WM, WN, B_K, true, CEP_IDENTITY>;
+template <int TILE, bool B_K, bool STAGED, int ACT>
+void launch_kind(const LinearArgs &a, int64_t items, hipStream_t s) {
+  // with groups fewer tiles may be live, and then quarters
+  const int64_t blocks = TILE == 0 && items > kUnits ? items + 2 * kUnits : items;
+  const dim3 grid((unsigned)((blocks + 7) / 8 * 8));
+  if constexpr (TILE == 0) hipLaunchKernelGGL((k_linear_256<B_K, STAGED, ACT>), grid, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((k_linear_128<B_K, STAGED, ACT>), grid, dim3(256), 0, s, a);
+}
+template <int TILE, bool B_K>
+void launch_tiles(const LinearArgs &a, int64_t items, hipStream_t s) {
+  auto *launch = launch_kind<TILE, B_K, true, CEP_IDENTITY>;
   if constexpr (B_K) {
-    if (!a.f.res) k = k_linear<HALF, WM, WN, B_K, false, CEP_IDENTITY>;
+    if (!a.f.res) launch = launch_kind<TILE, B_K, false, CEP_IDENTITY>;
   } else {
-    if (a.f.act == CEP_RELU) k = k_linear<HALF, WM, WN, B_K, true, CEP_RELU>;
-    if (a.f.act == CEP_SILU) k = k_linear<HALF, WM, WN, B_K, true, CEP_SILU>;
-    if (a.f.act == CEP_GELU) k = k_linear<HALF, WM, WN, B_K, true, CEP_GELU>;
-    if (a.f.act == CEP_GELU_TANH) k = k_linear<HALF, WM, WN, B_K, true, CEP_GELU_TANH>;
+    if (a.f.act == CEP_RELU) launch = launch_kind<TILE, B_K, true, CEP_RELU>;
+    if (a.f.act == CEP_SILU) launch = launch_kind<TILE, B_K, true, CEP_SILU>;
+    if (a.f.act == CEP_GELU) launch = launch_kind<TILE, B_K, true, CEP_GELU>;
+    if (a.f.act == CEP_GELU_TANH) launch = launch_kind<TILE, B_K, true, CEP_GELU_TANH>;
   }
-  hipLaunchKernelGGL(k, grid, dim3(WM * WN * 64), 0, s, a);
+  launch(a, items, s);
 }
 
 // A product over the groups' rows: A [rows][K], W as B, the epilogue's output [rows][N].
@@ -589,9 +641,8 @@ void launch_linear(const Plan &p, const Groups &g, const __bf16 *A, int64_t lda,
     a.N = N, a.K = K, a.segs = 1, a.splits = p.splits;
     a.groups = g, a.w_stride = w_stride, a.part = part, a.f = f;
     const int64_t items = most(kTile[p.tile]) * p.splits * ((N + kTile[p.tile] - 1) / kTile[p.tile]);
-    const dim3 grid((unsigned)((items + 7) / 8 * 8));
-    if (p.tile == 0) launch_tiles<128, 2, 4, B_K>(a, grid, s);
-    else launch_tiles<64, 2, 2, B_K>(a, grid, s);
+    if (p.tile == 0) launch_tiles<0, B_K>(a, items, s);
+    else launch_tiles<1, B_K>(a, items, s);
   }
   if (p.splits > 1) launch_finish(part, p.splits, g, f, g.rows, s);
 }

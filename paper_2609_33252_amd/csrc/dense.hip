@@ -221,54 +221,6 @@ void launch_dense(DenseArgs a, float *part, hipStream_t s) {
                        dim3((unsigned)(((int64_t)a.M * (a.N / 4) + 255) / 256)), dim3(256), 0, s, a);
 }
 
-// Estimated time, in us, of the tiles of n products in one launch, the longest
-// first; steps: of 64 of K, with 2 for a tile's start and end and 3 for each
-// ragged end of K.
-double tiles_us(int t, int n, const int64_t *tiles, const double *steps) {
-  if (t == 0) {  // one a compute unit, on the one that is free first
-    int order[3] = {0, 1, 2};
-    std::sort(order, order + n, [&](int i, int j) { return steps[i] > steps[j]; });
-    // units that are free at a time: a product splits one group at most
-    struct { double at; int64_t units; } group[4] = {{0.0, 256}};
-    int groups = 1;
-    double whole = 0, end = 0;
-    for (int o = 0; o < n; ++o) {
-      const int i = order[o];
-      const double us = 10 + 1.4 * steps[i];
-      const int64_t rounds = std::max<int64_t>(tiles[i] / 256 - 64, 0);
-      whole += (double)rounds * us;
-      for (int64_t left = tiles[i] - rounds * 256; left > 0;) {
-        auto *first = &group[0];
-        for (int g = 1; g < groups; ++g)
-          if (group[g].at < first->at) first = &group[g];
-        if (left < first->units) {
-          first->units -= left;
-          group[groups++] = {first->at + us, left};
-          end = std::max(end, first->at + us);
-          left = 0;
-        } else {
-          left -= first->units;
-          first->at += us;
-          end = std::max(end, first->at);
-        }
-      }
-    }
-    return whole + end;
-  }
-  // two a unit share it, so that its work counts, and the last round's gaps
-  int64_t all = 0;
-  double work = 0, longest = 0, shortest = steps[0];
-  for (int i = 0; i < n; ++i) {
-    all += tiles[i];
-    work += (double)tiles[i] * steps[i] / 512;
-    longest = std::max(longest, steps[i]);
-    shortest = std::min(shortest, steps[i]);
-  }
-  const double part = (double)(all % 512) / 512;
-  const double last = part == 0 ? 0 : part <= 0.5 ? 0.5 : 0.85 + 0.3 * (part - 0.5);
-  return 4 + std::max(0.55 * longest, work + shortest * (last - part) * (all < 512 ? 1.0 : 0.5));
-}
-
 // The tile with which dx, dWg and dWu, and dWd run in one launch, -1: a launch
 // each.  One launch saves the others' starts and joins their last rounds;
 // launches of their own can share K and take different tiles.  Kernels' us, one

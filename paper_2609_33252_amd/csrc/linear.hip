@@ -87,7 +87,26 @@ __device__ inline int group_of(const Groups &gr, int row) {
 
 // ---- epilogue
 
-__device__ inline float normal_cdf(float z) { return 0.5f * erfcf(z * -0.707106781f); }
+// Phi(z), the normal distribution, and *density, its slope.  Phi(-x) = exp(-x^2 / 2) t
+// P(t) for x >= 0 with t = 1 / (1 + 0.31 x): P, of degree 7, fits erfcx(x / sqrt 2) / (2
+// t) within 1.6e-7 of its value for x up to 14, where float32 has no smaller result
+// (weighted least squares, the weights raised where the error is largest).  About 20
+// instructions; with the library's erfc the gradient of 4095 x 2048 GELUs took 24 us,
+// bound by them.
+__device__ inline float normal_cdf(float z, float *density = nullptr) {
+  const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.31f, x, 1.0f));
+  const float e = __builtin_amdgcn_exp2f(x * x * -0.721347520f);  // log2(e) / 2
+  float p = fmaf(t, 0.0358419456f, -0.141605452f);
+  p = fmaf(t, p, 0.155069277f);
+  p = fmaf(t, p, -0.0149046248f);
+  p = fmaf(t, p, 0.110110752f);
+  p = fmaf(t, p, 0.10777092f);
+  p = fmaf(t, p, 0.12406037f);
+  p = fmaf(t, p, 0.123656906f);
+  const float below = e * t * p;
+  if (density) *density = 0.398942280f * e;
+  return z > 0.f ? 1.0f - below : below;
+}
 // The two operands of the tangent's logistic form: z (1 + tanh(u)) / 2 = z sigma(2 u),
 // where z beyond 30 in magnitude changes nothing any more but could overflow.
 __device__ inline float tanh_arg(float z, float *slope) {
@@ -113,9 +132,10 @@ __device__ inline float slope_of(float z, float *value) {
     return s * (1.0f + z * (1.0f - s));
   }
   if (ACT == CEP_GELU) {
-    const float phi = normal_cdf(z);
+    float density;
+    const float phi = normal_cdf(z, &density);
     *value = z * phi;
-    return fmaf(z, 0.398942280f * __expf(-0.5f * z * z), phi);
+    return fmaf(z, density, phi);
   }
   if (ACT == CEP_GELU_TANH) {
     float slope;
@@ -149,11 +169,14 @@ struct Finish {
   int N, act, res_dtype, y_dtype;
 };
 
+__device__ inline f32x4 from_bf16(uint32_t a, uint32_t b) {
+  return f32x4{__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u),
+               __uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)};
+}
 __device__ inline f32x4 load4(const void *p, int dtype, int64_t at) {
   if (dtype == CEP_F32) return *(const f32x4 *)((const float *)p + at);
   const uint2 u = *(const uint2 *)((const __bf16 *)p + at);
-  return f32x4{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u),
-               __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u)};
+  return from_bf16(u.x, u.y);
 }
 __device__ inline void store4(void *p, int dtype, int64_t at, const f32x4 &v) {
   if (dtype == CEP_F32) *(f32x4 *)((float *)p + at) = v;
@@ -188,8 +211,7 @@ __device__ inline Loaded load_eight(const Finish &f, int64_t m, int n) {
   return in;
 }
 __device__ inline f32x4 half_of(const Vec16 &v, int h) {  // four of eight bf16 values
-  return f32x4{__uint_as_float(v[2 * h] << 16), __uint_as_float(v[2 * h] & 0xffff0000u),
-               __uint_as_float(v[2 * h + 1] << 16), __uint_as_float(v[2 * h + 1] & 0xffff0000u)};
+  return from_bf16(v[2 * h], v[2 * h + 1]);
 }
 template <int ACT>
 __device__ inline void finish_eight(const Finish &f, int64_t m, int n, int g, const f32x4 &lo,
@@ -310,21 +332,30 @@ __global__ __launch_bounds__(512, 2) void k_linear_256(LinearArgs a) {
   }
 }
 
-// The shares' sums of a row, added in order, and what becomes of them.
-__global__ __launch_bounds__(256) void k_linear_finish(const float *part, int splits, Groups groups,
-                                                       Finish f) {
+// The shares' sums of a row, added in order, eight on the way at once, and what becomes
+// of them.
+constexpr int kFinishThreads = 128;
+__global__ __launch_bounds__(kFinishThreads) void k_linear_finish(const float *part, int splits,
+                                                                  Groups groups, Finish f) {
   const int64_t m = blockIdx.x;
-  const int n = ((int)blockIdx.y * 256 + threadIdx.x) * 4;
+  const int n = ((int)blockIdx.y * kFinishThreads + threadIdx.x) * 4;
   int g = 0;
   if (groups.n) {
     g = group_of(groups, (int)m);
     if (g == groups.n || m < span_of(groups, g).lo) return;  // no group's
   }
   if (n >= f.N) return;
+  const float *p = part + m * f.N + n;
+  const int64_t share = (int64_t)groups.rows * f.N;
   f32x4 v = {};
-#pragma unroll 4
-  for (int i = 0; i < splits; ++i)
-    v += *(const f32x4 *)(part + ((int64_t)i * groups.rows + m) * f.N + n);
+  for (int i0 = 0; i0 < splits; i0 += 8) {
+    f32x4 w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *(const f32x4 *)(p + min(i0 + i, splits - 1) * share);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += i0 + i < splits ? w[i] : f32x4{};
+  }
   with_act(f.act, [&](auto act) { finish<decltype(act)::value>(f, m, n, g, v); });
 }
 
@@ -334,30 +365,94 @@ struct WgradArgs : TileArgs {  // K: unused with groups
   Finish f;     // of one weight's gradient
 };
 
-// dW of each group, its rows as K.
-template <int HALF, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
-  const int n_tm = (a.M + 2 * HALF - 1) / (2 * HALF), n_tn = (a.N + 2 * HALF - 1) / (2 * HALF);
-  // a group's tiles are dealt to all XCDs
-  const int items = n_tm * a.splits * n_tn, room = (items + 7) / 8 * 8;
-  const int g = blockIdx.x / room, in = blockIdx.x % room, x = in & 7, at = in >> 3;
-  if (at >= piece_of(items, x)) return;
+// The r-th largest group, the lower of equals first (up to 64 groups, past which they
+// come in their own order): a launch's longest tiles go first.
+constexpr int kOrderedGroups = 64;
+__device__ inline int ranked_group(const Groups &gr, int r) {
+  if (gr.n > kOrderedGroups) return r;
+  const int lane = threadIdx.x & 63, n = lane < gr.n ? span_of(gr, lane).n : -1;
+  int rank = 0;
+  for (int h = 0; h < gr.n; ++h) {
+    const int o = __builtin_amdgcn_readlane(n, h);
+    rank += o > n || (o == n && h < lane);
+  }
+  return (int)__builtin_ctzll(__ballot(lane < gr.n && rank == r));
+}
+
+// A group's tiles are dealt to all XCDs: those of XCD x, and item `at` of its order,
+// groups by size.  False: none.
+struct WgradTile {
+  int g, m0, n0, share;
+};
+template <int SIZE>
+__device__ inline int wgrad_room(const WgradArgs &a) {  // of an XCD, a group
+  return ((a.M + SIZE - 1) / SIZE * ((a.N + SIZE - 1) / SIZE) * a.splits + 7) / 8;
+}
+// (ordered only where tiles are long: of 128-wide ones, a few steps each, finding the
+// order costs more than it gives, 16 groups of 3000 rows 77 us with it, 69 without)
+template <int SIZE>
+__device__ inline bool wgrad_item(const WgradArgs &a, int x, int at, WgradTile *t) {
+  const int n_tm = (a.M + SIZE - 1) / SIZE, n_tn = (a.N + SIZE - 1) / SIZE;
+  const int items = n_tm * a.splits * n_tn, room = wgrad_room<SIZE>(a);
+  const int r = at / room, in = at - r * room;
+  if (in >= piece_of(items, x)) return false;
   int mt, nt;
-  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + at, n_tm * a.splits, n_tn, &mt, &nt);
-  const int share = mt / n_tm;
+  tile_of<kGroupM>(x * (items / 8) + min(x, items % 8) + in, n_tm * a.splits, n_tn, &mt, &nt);
+  t->share = mt / n_tm;
+  t->m0 = (mt - t->share * n_tm) * SIZE;
+  t->n0 = nt * SIZE;
+  t->g = a.groups.n && SIZE == 256 ? __builtin_amdgcn_readfirstlane(ranked_group(a.groups, r)) : r;
+  return true;
+}
+template <int HALF, int WM, int WN>
+__device__ inline void wgrad_run(const WgradArgs &a, const WgradTile &w, uint8_t *lds) {
   TileArgs t = a;
   if (a.groups.n) {
-    const Span s = span_of(a.groups, g);
+    const Span s = span_of(a.groups, w.g);
     const int lo = __builtin_amdgcn_readfirstlane(s.lo);
     t.A += lo * a.lda;
     t.B0 += lo * a.ldb;
     t.K = __builtin_amdgcn_readfirstlane(s.n);
   }
-  const TileOut<CEP_IDENTITY> out{a.f, (int64_t)g * a.M, 0,
-                                  a.splits > 1 ? a.part + (int64_t)share * a.M * a.N : nullptr};
-  dense_tile<HALF, WM, WN, false, false, false>(t, (mt - share * n_tm) * 2 * HALF, nt * 2 * HALF,
-                                                share, lds, out);
+  const TileOut<CEP_IDENTITY> out{a.f, (int64_t)w.g * a.M, 0,
+                                  a.splits > 1 ? a.part + (int64_t)w.share * a.M * a.N : nullptr};
+  dense_tile<HALF, WM, WN, false, false, false>(t, w.m0, w.n0, w.share, lds, out);
+}
+
+// dW of each group, its rows as K.
+template <int HALF, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  WgradTile t;
+  if (wgrad_item<2 * HALF>(a, blockIdx.x & 7, blockIdx.x >> 3, &t)) wgrad_run<HALF, WM, WN>(a, t, lds);
+}
+
+// dW and dx in one launch: the weights of groups with more rows than dx has columns to
+// sum over, dx, the other weights, so that the longest tiles come first and the tiles of
+// one fill the compute units that the others' last round leaves.
+template <int HALF, int WM, int WN, bool STAGED>
+__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_grads(LinearArgs dx, WgradArgs dw) {
+  constexpr int SIZE = 2 * HALF;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
+  const int x = blockIdx.x & 7, room = wgrad_room<SIZE>(dw);
+  int at = blockIdx.x >> 3, first = dw.K > dx.K;  // of one weight
+  if (dw.groups.n > kOrderedGroups) {
+    first = dw.K / dw.groups.n > dx.K ? dw.groups.n : 0;
+  } else if (dw.groups.n) {
+    const int lane = threadIdx.x & 63;
+    first = (int)__popcll(__ballot(lane < dw.groups.n && span_of(dw.groups, min(lane, dw.groups.n - 1)).n > dx.K));
+  }
+  const TileWork<SIZE, true, STAGED, CEP_IDENTITY> work{dx, tiles_of<SIZE>(dx.groups),
+                                                        (dx.N + SIZE - 1) / SIZE, lds};
+  const int items = work.n_tm * work.n_tn, mine = piece_of(items, x);
+  if (at >= first * room && at < first * room + mine) {
+    work.template run<HALF, WM, WN>(x * (items / 8) + min(x, items % 8) + at - first * room, 0, 0);
+    return;
+  }
+  if (at >= first * room) at -= mine;
+  WgradTile t;
+  if (at < room * max(dw.groups.n, 1) && wgrad_item<SIZE>(dw, x, at, &t))
+    wgrad_run<HALF, WM, WN>(dw, t, lds);
 }
 
 // ---- few rows: the weights are streamed
@@ -401,7 +496,7 @@ struct DzArgs {
   __bf16 *dz, *dmul;  // dz [rows][N]
   float *part;        // column sums of a block's rows of a group: [blocks + groups][N]
   int64_t ld_y, ld_mul;
-  int N, act, y_dtype;
+  int N, y_dtype;
   Groups groups;
 };
 
@@ -513,6 +608,7 @@ struct Plan {
   bool stream;  // in row blocks of 16 or 32 (MF fragments)
   int mf;
   int tile, splits;
+  double us;  // estimated
 };
 
 // Rows of a group, on average, up to which the weights are streamed.
@@ -537,13 +633,12 @@ Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
     tiles[t] = std::max<int64_t>(n_tm, 1) * ((N + kTile[t] - 1) / kTile[t]);
   }
   const DensePlan d = plan_tiles(tiles, K / 64, (double)rows * N, 16);
-  p.tile = d.tile;
-  p.splits = d.splits;
+  p.tile = d.tile, p.splits = d.splits, p.us = d.us;
   // 256-wide tiles with quarters, which that estimate does not know
   const int whole = whole_tiles((int)tiles[0]), quarters = ((int)tiles[0] - whole) * 4;
   const double us = (double)((whole + kUnits - 1) / kUnits) * (12 + 1.4 * (K / 64)) +
                     (double)((quarters + kUnits - 1) / kUnits) * (3 + 0.55 * (K / 64));
-  if (us < d.us) p.tile = 0, p.splits = 1;
+  if (us < d.us) p.tile = 0, p.splits = 1, p.us = us;
   return p;
 }
 
@@ -554,9 +649,36 @@ Plan wgrad_plan(const cep_linear_desc *d) {
                             g * dense_tiles(1, d->d_in, d->d_out)};
   const DensePlan w = plan_tiles(tiles, d->rows / g / 64, (double)d->d_in * d->d_out,
                                  d->n_groups ? 1 : 16);
-  p.tile = w.tile;
-  p.splits = w.splits;
+  p.tile = w.tile, p.splits = w.splits, p.us = w.us;
   return p;
+}
+
+// Tiles that the groups' rows are in, on average (a group's last is half full).
+int64_t row_tiles(const cep_linear_desc *d, int size) {
+  if (!d->n_groups) return (d->rows + size - 1) / size;
+  return std::max<int64_t>(d->rows / size + (d->n_groups + 1) / 2, 1);
+}
+
+// The tile with which dx and dW run in one launch, -1: a launch each.
+int grads_tile(const cep_linear_desc *d) {
+  if (d->rows == 0) return -1;
+  const int g = std::max(d->n_groups, 1);
+  // Launches of their own for groups take longer than estimated, with the tiles of unlike
+  // sizes that they wait for (us, one launch and two: 8192 rows of 4096 x 2048 in eight
+  // groups 284, 288, and with some popular 292, 306; 2048 x 1408 in 32 groups 216, 226;
+  // 2048 x 4096 in four 246, 260; one weight, 4095 x 4096 x 2048, 125, 140)
+  double least = plan_of(d->rows, d->d_in, d->d_out, d->n_groups, false).us +
+                 wgrad_plan(d).us * (d->n_groups ? 1.3 : 1.0);
+  int best = -1;
+  auto steps = [](int K) { return 2 + K / 64 + (K % 64 ? 3.0 : 0.0); };
+  const double st[2] = {steps(d->d_out), steps(d->rows / g)};
+  for (int t = 0; t < 2; ++t) {
+    const int64_t tiles[2] = {row_tiles(d, kTile[t]) * ((d->d_in + kTile[t] - 1) / kTile[t]),
+                              g * dense_tiles(t, d->d_in, d->d_out)};
+    const double us = tiles_us(t, 2, tiles, st);
+    if (us < least) best = t, least = us;
+  }
+  return best;
 }
 
 size_t part_bytes(const Plan &p, int rows, int N) {
@@ -586,8 +708,8 @@ Space space_of(const cep_linear_desc *d, int backward) {
 
 void launch_finish(const float *part, int splits, const Groups &g, const Finish &f, int rows,
                    hipStream_t s) {
-  hipLaunchKernelGGL(k_linear_finish, dim3(rows, (f.N + 1023) / 1024), dim3(256), 0, s, part, splits,
-                     g, f);
+  hipLaunchKernelGGL(k_linear_finish, dim3(rows, (f.N / 4 + kFinishThreads - 1) / kFinishThreads),
+                     dim3(kFinishThreads), 0, s, part, splits, g, f);
 }
 
 // The epilogue is staged except where it is a plain store (us, staged and not: 777 x
@@ -615,32 +737,51 @@ void launch_tiles(const LinearArgs &a, int64_t items, hipStream_t s) {
   launch(a, items, s);
 }
 
+// The most tiles that the groups' rows can be in.
+int64_t most_tiles(const Groups &g, int tile) {
+  return g.n ? std::min<int64_t>(g.rows, g.rows / tile + g.n) : (g.rows + tile - 1) / tile;
+}
+
+LinearArgs linear_args(const Groups &g, const __bf16 *A, int64_t lda, const __bf16 *W, int64_t ldb,
+                       int N, int K, const Finish &f) {
+  LinearArgs a{};
+  a.A = A, a.lda = lda;
+  a.B0 = W, a.ldb = ldb;
+  a.N = N, a.K = K, a.segs = 1, a.splits = 1;
+  a.groups = g, a.f = f;
+  a.w_stride = g.n ? (int64_t)N * K : 0;
+  return a;
+}
+
+void launch_grads(int tile, const LinearArgs &dx, WgradArgs dw, hipStream_t s) {
+  dw.splits = 1;
+  const int64_t items = most_tiles(dx.groups, kTile[tile]) * ((dx.N + kTile[tile] - 1) / kTile[tile]);
+  const int64_t room = (dense_tiles(tile, dw.M, dw.N) + 7) / 8 * std::max(dw.groups.n, 1);
+  const dim3 grid((unsigned)(((items + 7) / 8 + room) * 8));
+  auto *k = tile == 0 ? k_linear_grads<128, 2, 4, false> : k_linear_grads<64, 2, 2, false>;
+  if (dx.f.res) k = tile == 0 ? k_linear_grads<128, 2, 4, true> : k_linear_grads<64, 2, 2, true>;
+  hipLaunchKernelGGL(k, grid, dim3(tile == 0 ? 512 : 256), 0, s, dx, dw);
+}
+
 // A product over the groups' rows: A [rows][K], W as B, the epilogue's output [rows][N].
 template <bool B_K>
 void launch_linear(const Plan &p, const Groups &g, const __bf16 *A, int64_t lda, const __bf16 *W,
                    int64_t ldb, int N, int K, const Finish &f, float *part, hipStream_t s) {
-  // the most tiles that the groups' rows can be in
-  auto most = [&](int tile) {
-    return g.n ? std::min<int64_t>(g.rows, g.rows / tile + g.n) : (g.rows + tile - 1) / tile;
-  };
-  const int64_t w_stride = g.n ? (int64_t)N * K : 0;
   if (p.stream) {
     LinearRowsArgs a{};
     a.A[0] = A, a.lda = lda;
     a.B0 = W, a.ldb = ldb;
     a.N = N, a.K = K;
     a.splits = p.splits, a.col_blocks = (N + kCols - 1) / kCols;
-    a.groups = g, a.w_stride = w_stride, a.part = part, a.f = f;
-    const dim3 grid((unsigned)(most(p.mf * 16) * a.col_blocks * a.splits));
+    a.groups = g, a.w_stride = g.n ? (int64_t)N * K : 0, a.part = part, a.f = f;
+    const dim3 grid((unsigned)(most_tiles(g, p.mf * 16) * a.col_blocks * a.splits));
     if (p.mf == 1) hipLaunchKernelGGL(k_linear_rows<1>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(k_linear_rows<2>, grid, dim3(256), 0, s, a);
   } else {
-    LinearArgs a{};
-    a.A = A, a.lda = lda;
-    a.B0 = W, a.ldb = ldb;
-    a.N = N, a.K = K, a.segs = 1, a.splits = p.splits;
-    a.groups = g, a.w_stride = w_stride, a.part = part, a.f = f;
-    const int64_t items = most(kTile[p.tile]) * p.splits * ((N + kTile[p.tile] - 1) / kTile[p.tile]);
+    LinearArgs a = linear_args(g, A, lda, W, ldb, N, K, f);
+    a.splits = p.splits, a.part = part;
+    const int64_t items =
+        most_tiles(g, kTile[p.tile]) * p.splits * ((N + kTile[p.tile] - 1) / kTile[p.tile]);
     if (p.tile == 0) launch_tiles<0, B_K>(a, items, s);
     else launch_tiles<1, B_K>(a, items, s);
   }
@@ -727,7 +868,7 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
     a.dz = !same && (dx || dw) ? (__bf16 *)ws : nullptr;
     a.dmul = (__bf16 *)dmul;
     a.part = dbias ? sums : nullptr;
-    a.N = N, a.act = d->act, a.groups = g;
+    a.N = N, a.groups = g;
     const dim3 grid(dz_chunks(d), (N + kDzCols - 1) / kDzCols);
     auto *k = d->act == CEP_RELU        ? k_linear_dz<CEP_RELU>
               : d->act == CEP_SILU      ? k_linear_dz<CEP_SILU>
@@ -740,21 +881,24 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
   if (dbias)
     hipLaunchKernelGGL(k_linear_dbias, dim3((N + 63) / 64, n_groups), dim3(256), 0, s, sums, N, g,
                        dbias);
-  if (dx && T) {
-    Finish f{};
-    f.res = dx_add, f.y = dx, f.N = D, f.res_dtype = f.y_dtype = d->dx_dtype;
-    f.ld_res = f.ld_y = d->ld_dx ? d->ld_dx : D;
+  Finish f{};
+  f.res = dx_add, f.y = dx, f.N = D, f.res_dtype = f.y_dtype = d->dx_dtype;
+  f.ld_res = f.ld_y = d->ld_dx ? d->ld_dx : D;
+  const Plan p = wgrad_plan(d);
+  WgradArgs a{};
+  a.A = (const __bf16 *)x, a.lda = d->ld_x ? d->ld_x : D;
+  a.B0 = dz, a.ldb = ld_z;
+  a.M = D, a.N = N, a.K = T, a.segs = 1, a.splits = p.splits;
+  a.groups = g, a.part = part;
+  a.f.y = dw, a.f.N = N, a.f.y_dtype = d->dw_dtype, a.f.ld_y = N;
+  if (const int tile = dx && dw ? grads_tile(d) : -1; tile >= 0) {
+    launch_grads(tile, linear_args(g, dz, ld_z, (const __bf16 *)w, N, D, N, f), a, s);
+    return launched(fn);
+  }
+  if (dx && T)
     launch_linear<true>(plan_of(T, D, N, d->n_groups, false), g, dz, ld_z, (const __bf16 *)w, N, D, N,
                         f, part, s);
-  }
   if (dw) {
-    const Plan p = wgrad_plan(d);
-    WgradArgs a{};
-    a.A = (const __bf16 *)x, a.lda = d->ld_x ? d->ld_x : D;
-    a.B0 = dz, a.ldb = ld_z;
-    a.M = D, a.N = N, a.K = T, a.segs = 1, a.splits = p.splits;
-    a.groups = g, a.part = part;
-    a.f.y = dw, a.f.N = N, a.f.y_dtype = d->dw_dtype, a.f.ld_y = N;
     const int64_t items = dense_tiles(p.tile, D, N) * p.splits;
     const dim3 grid((unsigned)((items + 7) / 8 * 8 * n_groups));
     if (p.tile == 0)

@@ -427,6 +427,99 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
   if (wgrad_item<2 * HALF>(a, blockIdx.x & 7, blockIdx.x >> 3, &t)) wgrad_run<HALF, WM, WN>(a, t, lds);
 }
 
+// dW of groups of few rows, in 128-wide tiles by 2 x 2 waves: a tile is mostly its start
+// and its store, so that several share a compute unit (32 KB of LDS) instead of one
+// running ahead of itself.  64 rows at a time, [64 rows][128 columns] of each operand,
+// 16-byte chunk pair p of line k at p ^ f(k); lines past the group's rows are zeros.
+// Measured: FEW_US.
+__global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
+  constexpr int F = 4;  // fragments of a wave in each operand
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2][16384];
+  WgradTile w;
+  if (!wgrad_item<128>(a, blockIdx.x & 7, blockIdx.x >> 3, &w)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l15 = lane & 15, g4 = lane >> 4, wm = wave & 1, wn = wave >> 1;
+  int lo = 0, K = a.K;
+  if (a.groups.n) {
+    const Span s = span_of(a.groups, w.g);
+    lo = __builtin_amdgcn_readfirstlane(s.lo);
+    K = __builtin_amdgcn_readfirstlane(s.n);
+  }
+  auto f_of = [](int k) { return (k & 3) | ((k >> 3) & 1) << 2; };
+  // a thread's 16 bytes of lines k0 + tid / 16, and every 16th from there
+  const int chunk = tid & 15;
+  const __bf16 *srcA = a.A + lo * a.lda + min(w.m0 + chunk * 8, a.M - 8);
+  const __bf16 *srcB = a.B0 + lo * a.ldb + min(w.n0 + chunk * 8, a.N - 8);
+  f32x4 acc[F][F] = {};
+  for (int k0 = 0; k0 < K; k0 += 64) {
+    uint4 v[2][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t k = k0 + e * 16 + (tid >> 4);
+      v[0][e] = v[1][e] = make_uint4(0u, 0u, 0u, 0u);
+      if (k < K) {
+        v[0][e] = *(const uint4 *)(srcA + k * a.lda);
+        v[1][e] = *(const uint4 *)(srcB + k * a.ldb);
+      }
+    }
+    if (k0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = e * 16 + (tid >> 4);
+      const int to = k * 256 + (((chunk >> 1) ^ f_of(k)) << 5) + (chunk & 1) * 16;
+      *(uint4 *)(lds[0] + to) = v[0][e];
+      *(uint4 *)(lds[1] + to) = v[1][e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const int k = ks * 32 + g4 * 8 + (l15 >> 2);
+      auto read = [&](const uint8_t *at, int row0, int i) {
+        union { bf16x8 v; bf16x4 h[2]; } o;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          o.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+              (__attribute__((address_space(3))) bf16x4 *)(at + (k + h * 4) * 256 +
+                                                            (((row0 >> 4) + i) ^ f_of(k)) * 32 +
+                                                            (l15 & 3) * 8));
+        return o.v;
+      };
+      bf16x8 fa[F], fb[F];
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        fa[i] = read(lds[0], wm * 64, i);
+        fb[i] = read(lds[1], wn * 64, i);
+      }
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    }
+  }
+  // a row fragment of both halves at a time through LDS, [32 rows][128] float32, 16-byte
+  // chunk c of row r at c ^ (r % 16), so that whole cache lines are written
+  auto at = [&](int i, int r, int c) {
+    return (f32x4 *)(lds[i & 1] + r * 512 + ((c ^ (r & 15)) << 4));
+  };
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < F; ++i) {
+#pragma unroll
+    for (int j = 0; j < F; ++j) *at(i, wm * 16 + l15, wn * 16 + j * 4 + g4) = acc[i][j];
+    wait_lgkm0();
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = u * 16 + (tid >> 4), n = w.n0 + chunk * 8;
+      const int64_t m = w.m0 + (r >> 4) * 64 + i * 16 + (r & 15);
+      if (m < a.M && n < a.N)
+        finish_eight<CEP_IDENTITY>(a.f, (int64_t)w.g * a.M + m, n, 0, *at(i, r, 2 * chunk),
+                                   *at(i, r, 2 * chunk + 1), Loaded{});
+    }
+  }
+}
+
 // dW and dx in one launch: the weights of groups with more rows than dx has columns to
 // sum over, dx, the other weights, so that the longest tiles come first and the tiles of
 // one fill the compute units that the others' last round leaves.
@@ -642,14 +735,28 @@ Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
   return p;
 }
 
+// dW: 256- or 128-wide tiles (0, 1), or k_linear_wgrad_few (2), by estimates of the time
+// for K in steps of 64 (us; measured, 4096 x 2048 a group):
+//   256-wide: 12 + 1.4 a step, a round of 256; groups of unlike sizes a tenth more
+//   128-wide, more than a round: 6 + 1.3 a step, a round of 512 (32 groups of 34 rows 262,
+//     16 of 128 rows 175)
+//   few: 5 + 2 a step, a round of 768, three a compute unit (the same two 154 and 110, 16
+//     of 256 rows 147, eight of 512 109, eight of 1024 198); two of them 1.5 a step, one 1
+constexpr int kFewTile = 2;
 Plan wgrad_plan(const cep_linear_desc *d) {
-  Plan p{};
   const int g = std::max(d->n_groups, 1);
   const int64_t tiles[2] = {g * dense_tiles(0, d->d_in, d->d_out),
                             g * dense_tiles(1, d->d_in, d->d_out)};
-  const DensePlan w = plan_tiles(tiles, d->rows / g / 64, (double)d->d_in * d->d_out,
-                                 d->n_groups ? 1 : 16);
+  const double steps = std::max(1.0, (double)d->rows / g / 64);
+  DensePlan w = plan_tiles(tiles, d->rows / g / 64, (double)d->d_in * d->d_out, d->n_groups ? 1 : 16);
+  if (w.tile == 1 && tiles[1] > 512) w.us = (double)tiles[1] / 512 * (6 + 1.3 * steps);
+  Plan p{};
   p.tile = w.tile, p.splits = w.splits, p.us = w.us;
+  const double wide = (double)((tiles[0] + 255) / 256) * (12 + 1.4 * steps) * (d->n_groups ? 1.1 : 1.0);
+  if (wide < p.us) p.tile = 0, p.splits = 1, p.us = wide;
+  const double few = tiles[1] > 768 ? (double)tiles[1] / 768 * (5 + 2 * steps)
+                                    : 5 + steps * (0.5 + 0.5 * (double)((tiles[1] + 255) / 256));
+  if (few < p.us) p.tile = kFewTile, p.splits = 1, p.us = few;
   return p;
 }
 
@@ -665,17 +772,20 @@ int grads_tile(const cep_linear_desc *d) {
   const int g = std::max(d->n_groups, 1);
   // Launches of their own for groups take longer than estimated, with the tiles of unlike
   // sizes that they wait for (us, one launch and two: 8192 rows of 4096 x 2048 in eight
-  // groups 284, 288, and with some popular 292, 306; 2048 x 1408 in 32 groups 216, 226;
-  // 2048 x 4096 in four 246, 260; one weight, 4095 x 4096 x 2048, 125, 140)
+  // groups 284, 288, and with some popular 292, 306; 2048 x 4096 in four 246, 260; one
+  // weight, 4095 x 4096 x 2048, 125, 140)
+  const Plan own = wgrad_plan(d);
   double least = plan_of(d->rows, d->d_in, d->d_out, d->n_groups, false).us +
-                 wgrad_plan(d).us * (d->n_groups ? 1.3 : 1.0);
+                 own.us * (d->n_groups && own.tile == 0 ? 1.2 : 1.0);
   int best = -1;
   auto steps = [](int K) { return 2 + K / 64 + (K % 64 ? 3.0 : 0.0); };
   const double st[2] = {steps(d->d_out), steps(d->rows / g)};
   for (int t = 0; t < 2; ++t) {
     const int64_t tiles[2] = {row_tiles(d, kTile[t]) * ((d->d_in + kTile[t] - 1) / kTile[t]),
                               g * dense_tiles(t, d->d_in, d->d_out)};
-    const double us = tiles_us(t, 2, tiles, st);
+    double us = tiles_us(t, 2, tiles, st);
+    if (t == 1 && tiles[0] + tiles[1] > 512)
+      us = std::max(us, ((double)tiles[0] * (6 + 1.3 * st[0]) + (double)tiles[1] * (6 + 1.3 * st[1])) / 512);
     if (us < least) best = t, least = us;
   }
   return best;
@@ -898,7 +1008,11 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
   if (dx && T)
     launch_linear<true>(plan_of(T, D, N, d->n_groups, false), g, dz, ld_z, (const __bf16 *)w, N, D, N,
                         f, part, s);
-  if (dw) {
+  if (dw && p.tile == kFewTile) {
+    const int64_t items = dense_tiles(1, D, N);
+    hipLaunchKernelGGL(k_linear_wgrad_few, dim3((unsigned)((items + 7) / 8 * 8 * n_groups)), dim3(256),
+                       0, s, a);
+  } else if (dw) {
     const int64_t items = dense_tiles(p.tile, D, N) * p.splits;
     const dim3 grid((unsigned)((items + 7) / 8 * 8 * n_groups));
     if (p.tile == 0)

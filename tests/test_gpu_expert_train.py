@@ -387,6 +387,29 @@ def test_linear_backward(rows, d, N, groups, act, bias, mul, y, dxt, dwt, add, p
             assert torch.equal(alone, t)
 
 
+LARGE = [
+    # 256-wide tiles, the last of them in quarters
+    (8700, 1032, 2056, 0), (8730, 1032, 2056, [3000, 20, 0, 2500, 1300, 1900]),
+    # gradients: long tiles of more groups than are ordered by size, then of fewer
+    (71685, 1032, 1032, [1024] * 70), (9000, 2056, 1544, [400, 5000, 70, 0, 3500]),
+    # many short tiles of dW, and dx's before and behind them in one launch
+    (2000, 1544, 1032, [60] * 31 + [100]), (4096, 520, 4104, [1500, 2500]),
+    (5000, 4104, 520, [3000, 2000]),
+]
+
+
+@pytest.mark.parametrize("rows,d,N,groups", LARGE)
+@pytest.mark.parametrize("case", [3, 5])
+def test_linear_of_many_tiles(rows, d, N, groups, case):
+    test_linear(rows, d, N, groups, *EXTRAS[case])
+
+
+@pytest.mark.parametrize("rows,d,N,groups", LARGE)
+@pytest.mark.parametrize("case", [1, 4])
+def test_linear_backward_of_many_tiles(rows, d, N, groups, case):
+    test_linear_backward(rows, d, N, groups, *GRADS[case])
+
+
 def test_linear_of_no_rows_has_zero_weight_gradients():
     for groups in (0, 3):
         desc = cep.make_linear(rows=0, d_in=64, d_out=32, n_groups=groups)

@@ -523,8 +523,8 @@ typedef struct {
  * (the offsets of cep_linear), then the number of ids outside [-1, n_experts)
  * (such slots count as empty); pair: the flat index of each sorted row; place
  * [rows][top_k]: the sorted row of each pair, -1 for an empty slot; out_x: row
- * x[t] of each sorted row, dense rows of row_bytes bytes.  x and out_x may both be
- * NULL: the order alone.  pair and out_x past the last segment are left as they
+ * x[t] of each sorted row, dense rows of row_bytes bytes, no part of x.  x and out_x may
+ * both be NULL: the order alone.  pair and out_x past the last segment are left as they
  * are.  Its gradient, each token's sum over its sorted rows' gradients, is
  * cep_expert_unsort without weights. */
 size_t cep_expert_sort_workspace(const cep_expert_sort_desc *desc);

@@ -70,7 +70,8 @@ struct Eight {
 template <int KM, bool YS32>
 __global__ __launch_bounds__(256) void k_unsort(UnsortArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int64_t item = block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t t = item / a.waves;
   if (t >= a.rows) return;
   const int c = ((int)(item % a.waves) * 64 + lane) * 8, n = a.d - c;
@@ -157,7 +158,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void k_unsort_grad(Unsor
 
 template <int KM, bool YS32>
 void launch_unsort(const UnsortArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)a.rows * a.waves + 3) / 4));
+  // (a launch holds fewer than 2^32 threads in x)
+  constexpr int64_t kMost = 1 << 22;
+  const int64_t blocks = ((int64_t)a.rows * a.waves + 3) / 4;
+  const dim3 grid((unsigned)std::min(blocks, kMost), (unsigned)((blocks + kMost - 1) / kMost));
   hipLaunchKernelGGL((k_unsort<KM, YS32>), grid, dim3(256), 0, s, a);
 }
 template <int KM, bool YS32>

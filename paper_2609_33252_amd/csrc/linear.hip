@@ -111,7 +111,7 @@ __device__ inline float normal_cdf(float z, float *density = nullptr) {
 // where z beyond 30 in magnitude changes nothing any more but could overflow.
 __device__ inline float tanh_arg(float z, float *slope) {
   constexpr float kA = 1.59576912f, kB = 0.044715f;  // 2 sqrt(2 / pi)
-  const float c = fminf(fmaxf(z, -30.0f), 30.0f), q = c * c;
+  const float c = z != z ? z : fminf(fmaxf(z, -30.0f), 30.0f), q = c * c;
   if (slope) *slope = kA * fmaf(3.0f * kB, q, 1.0f);
   return kA * c * fmaf(kB, q, 1.0f);
 }
@@ -141,7 +141,7 @@ __device__ inline float slope_of(float z, float *value) {
     float slope;
     const float s = sigma(tanh_arg(z, &slope));
     *value = z * s;
-    const float c = fminf(fmaxf(z, -30.0f), 30.0f);
+    const float c = fminf(fmaxf(z, -30.0f), 30.0f);  // (s is NaN where z is)
     return fmaf(c * s * (1.0f - s), slope, s);
   }
   *value = act_of<ACT>(z);

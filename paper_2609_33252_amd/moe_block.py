@@ -213,14 +213,14 @@ class MoEBlock:
 
 class RoutedExperts:
     """Gated experts of one rank with gradients: w_gate, w_up [n_experts][d][d_ff] and
-    w_down [n_experts][d_ff][d], bf16, for up to max_tokens tokens a call.
+    w_down [n_experts][d_ff][d], bf16.
 
         sorted rows x of each expert       cep_expert_sort
         u = x W_up, h = silu(x W_gate) u   cep_linear
         h W_down, weighted and summed      cep_linear, cep_expert_unsort
     """
 
-    def __init__(self, *, top_k, max_tokens, w_gate, w_up, w_down):
+    def __init__(self, *, top_k, w_gate, w_up, w_down):
         BF16 = (torch.bfloat16,)
         if w_gate.dim() != 3:
             raise ValueError("w_gate must be of shape [n_experts, d, d_ff]")
@@ -228,18 +228,15 @@ class RoutedExperts:
         _expect("w_gate", w_gate, w_gate.device, BF16, (E, d, d_ff))
         _expect("w_up", w_up, w_gate.device, BF16, (E, d, d_ff))
         _expect("w_down", w_down, w_gate.device, BF16, (E, d_ff, d))
-        self.E, self.d, self.d_ff, self.top_k, self.max_tokens = E, d, d_ff, top_k, max_tokens
+        self.E, self.d, self.d_ff, self.top_k = E, d, d_ff, top_k
         self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
-        self.ws = self._buf(0, dtype=torch.uint8)
         self.saved = None  # of the last forward pass, if that was a training one
 
     def _buf(self, *shape, dtype=torch.bfloat16):
         return torch.empty(*shape, dtype=dtype, device=self.w_gate.device)
 
-    def _space(self, need):
-        if self.ws.numel() < need:  # grows to the largest call's
-            self.ws = self._buf(need, dtype=torch.uint8)
-        return self.ws
+    def _space(self, need):  # the allocator's, so that calls on two streams have one each
+        return self._buf(need, dtype=torch.uint8)
 
     def _linear(self, rows, d_in, d_out, act=cep.CEP_IDENTITY):
         return cep.make_linear(rows=rows, d_in=d_in, d_out=d_out, n_groups=self.E, act=act,
@@ -254,13 +251,16 @@ class RoutedExperts:
     def forward(self, y, ids, w, train=False):
         """y [T][d] bf16; ids int32 and w float32 [T][top_k] as cep_gate_topk leaves
         them (-1: empty slot).  Returns float32 [T][d], each token's weighted sum."""
-        T, k, d, I, s = y.shape[0], self.top_k, self.d, self.d_ff, torch.cuda.current_stream()
-        if T > self.max_tokens:
-            raise ValueError(f"{T} tokens, the experts hold {self.max_tokens}")
-        dev, P = self.w_gate.device, T * k
+        T, k, d, dev = y.shape[0], self.top_k, self.d, self.w_gate.device
         _expect("y", y, dev, (torch.bfloat16,), (T, d))
         _expect("ids", ids, dev, (torch.int32,), (T, k))
         _expect("w", w, dev, (torch.float32,), (T, k))
+        with torch.cuda.device(dev):
+            return self._forward(y, ids, w, train)
+
+    def _forward(self, y, ids, w, train):
+        T, k, d, I = y.shape[0], self.top_k, self.d, self.d_ff
+        s, P = torch.cuda.current_stream(), T * k
         sort = cep.make_expert_sort(rows=T, top_k=k, n_experts=self.E, capacity=P, row_bytes=2 * d)
         plan, pair = self._buf(self.E + 2, dtype=torch.int32), self._buf(P, dtype=torch.int32)
         place, x = self._buf(T, k, dtype=torch.int32), self._buf(P, d)
@@ -287,10 +287,16 @@ class RoutedExperts:
         of w_gate, w_up and w_down (bf16)."""
         if self.saved is None:
             raise ValueError("backward without a forward(train=True) before it")
+        _expect("d_total", d_total, self.w_gate.device, (torch.float32, torch.bfloat16),
+                (self.saved[1].shape[0], self.d))
+        with torch.cuda.device(self.w_gate.device):
+            return self._backward(d_total)
+
+    def _backward(self, d_total):
         plan, place, w, x, u, h, pre, out = self.saved
-        T, P, d, I = place.shape[0], x.shape[0], self.d, self.d_ff
-        s, dev = torch.cuda.current_stream(), x.device
-        _expect("d_total", d_total, dev, (torch.float32, torch.bfloat16), (T, d))
+        T, P, d, I, s = place.shape[0], x.shape[0], self.d, self.d_ff, torch.cuda.current_stream()
+        for t in self.saved:
+            t.record_stream(s)  # it may be another one than the forward pass's
         kind = cep.CEP_F32 if d_total.dtype == torch.float32 else cep.CEP_BF16
         d_out, d_w = torch.empty_like(out), torch.empty_like(w)
         cep.cep_expert_unsort_backward(self._unsort(T, cep.CEP_BF16, kind), d_total, out, place, w,
@@ -324,8 +330,7 @@ def main():
                      gate=normal(d, E).float(),
                      shared=(normal(d, d_shared), normal(d, d_shared), normal(d_shared, d)),
                      experts=cep.make_weights(*experts), w_dtype=cep.CEP_BF16)
-    routed = RoutedExperts(top_k=k, max_tokens=2048, w_gate=experts[0], w_up=experts[1],
-                           w_down=experts[2])
+    routed = RoutedExperts(top_k=k, w_gate=experts[0], w_up=experts[1], w_down=experts[2])
     for T in (1, 100, 2048):
         x, residual, d_out = normal(T, d, std=1.0), normal(T, d, std=1.0), normal(T, d)
         out = block.forward(x, residual, train=True)

@@ -462,6 +462,26 @@ def test_linear_of_large_arguments(act):
     assert torch.equal(dx, (want > 0).float().expand(4, d))
 
 
+@pytest.mark.parametrize("act", range(5))
+def test_linear_gradient_of_a_row_that_is_no_number(act):
+    """Its gradients, and the weights' where it counts, are none either."""
+    T, d, N = 40, 64, 72
+    g = _gen(act)
+    x, w, mul = _randn(g, T, d), _randn(g, d, N, std=0.1), _randn(g, T, N)
+    x[5] = NAN
+    desc = cep.make_linear(rows=T, d_in=d, d_out=N, act=act)
+    ws = _space(cep.cep_linear_workspace(desc, True))
+    y, pre, dx = (torch.empty(T, n, device="cuda") for n in (N, N, d))
+    dw, dm = torch.empty(d, N, device="cuda"), torch.empty_like(mul)
+    cep.cep_linear(desc, x, w, y, ws, preact=pre, mul=mul)
+    cep.cep_linear_backward(desc, torch.ones_like(y), x, w, ws, dx=dx, dw=dw, preact=pre, mul=mul,
+                            dmul=dm)
+    assert torch.isnan(y[5]).all() and torch.isnan(dm[5]).all() and torch.isnan(dw).all()
+    assert act == 0 or torch.isnan(dx[5]).all()  # without an activation it hangs on dy alone
+    for t in (y, dx, dm):
+        assert torch.isfinite(t[torch.arange(T, device="cuda") != 5]).all()
+
+
 @pytest.mark.parametrize("off", [[9, 5, 1, 0], [-7, 20, 1 << 30, -(1 << 30)], [0, 40, 0, 40],
                                  [50, 60, 70, 80], [0, 0, 0, 1 << 31 - 1]])
 def test_linear_with_broken_offsets_stays_inside_its_arrays(off):
@@ -550,6 +570,66 @@ def test_gate_gradient_of_far_scores():
     want = torch.sigmoid(x) * torch.sigmoid(-x)
     # subnormal scores have steps of 2^-149
     assert ((out - want).abs() <= 2.0 ** -20 * want + 2.0 ** -149).all()
+
+
+# ----------------------------------------------- arrays past 2^31 elements
+
+def test_sort_and_way_back_past_32_bits():
+    T, k, d = 36000, 8, 8192  # 2.4e9 sorted values
+    g = _gen(4)
+    ids = torch.randint(-1, 12, (T, k), device="cuda", generator=g).int()
+    x = _randn(g, T, d)
+    sd = cep.make_expert_sort(rows=T, top_k=k, n_experts=12, capacity=T * k, row_bytes=2 * d)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    plan, pair, place = i32(14), i32(T * k), i32(T, k)
+    xs = torch.empty(T * k, d, dtype=torch.bfloat16, device="cuda")
+    cep.cep_expert_sort(sd, ids, plan, pair, place, _space(cep.cep_expert_sort_workspace(sd)), x=x,
+                        out_x=xs)
+    n = int(plan[12])
+    assert n * d > 1 << 31
+    for at in range(0, n, 20000):
+        some = slice(at, min(at + 20000, n))
+        assert torch.equal(xs[some], x[pair[some].long() // k])
+    ud = cep.make_expert_unsort(rows=T, top_k=k, d=d, sorted_rows=n, ys_dtype=BF16, y_dtype=F32)
+    y = torch.empty(T, d, device="cuda")
+    cep.cep_expert_unsort(ud, xs, place, y)
+    count = (place >= 0).sum(1, keepdim=True)
+    # a token's own row, as often as it has experts: up to eight equal bf16 values, exact
+    assert torch.equal(y, x.float() * count)
+    dw = torch.empty(T, k, device="cuda")
+    cep.cep_expert_unsort_backward(ud, y, xs, place, None, xs, dw)
+    last = slice(n - 1000, n)
+    want = y[pair[last].long() // k]
+    _close(xs[last], want.double(), U16 * 1.01 * want.double().abs(), "dys")
+    ref = (y[-500:].double() * x[-500:].double()).sum(1, keepdim=True)
+    mag = (y[-500:].double() * x[-500:].double()).abs().sum(1, keepdim=True)
+    _close(dw[-500:], torch.where(place[-500:] >= 0, ref, 0.0), SUM32 * mag.expand(-1, k), "dw")
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+def test_linear_past_32_bits(grouped):
+    rows, d, N = (1 << 20) + 77, 64, 2056  # 2.2e9 outputs
+    g = _gen(6)
+    off = [0, 5, (1 << 19) + 3, rows - 2] if grouped else None
+    lead = (3,) if grouped else ()
+    x, w = _randn(g, rows, d), _randn(g, *lead, d, N, std=0.1)
+    dev = None if off is None else torch.tensor(off, dtype=torch.int32, device="cuda")
+    desc = cep.make_linear(rows=rows, d_in=d, d_out=N, n_groups=3 if grouped else 0,
+                           act=cep.CEP_SILU, y_dtype=BF16, dx_dtype=F32)
+    ws = torch.empty(cep.cep_linear_workspace(desc, True), dtype=torch.uint8, device="cuda")
+    y = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    pre, dx = torch.empty(rows, N, device="cuda"), torch.full((rows, d), 7.0, device="cuda")
+    cep.cep_linear(desc, x, w, y, ws, offsets=dev, preact=pre)
+    cep.cep_linear_backward(desc, y, x, w, ws, dx=dx, preact=pre, offsets=dev)  # dy: y itself
+    for r, e in ((slice(0, 5), 0), (slice(5, 2000), 1), (slice(rows - 3000, rows - 2), 2)):
+        we = w[e] if grouped else w
+        z, ref, mag = R.linear(x[r], we, None, None, None, cep.CEP_SILU, None)
+        _close(y[r], ref, 1.1 * SUM32 * mag + SUM32 * ref.abs() + U16 * 1.01 * ref.abs() + 1e-37, "y")
+        grad = R.linear_grad(y[r], x[r], we, pre[r], None, cep.CEP_SILU, None)
+        edz = 2.0 ** -16 * (1 + z.abs()) * y[r].double().abs() + (1.02 * U16 + SUM32) * grad["dz"].abs()
+        _close(dx[r], grad["dx"], edz @ we.double().abs().T.contiguous() + 1e-37, "dx")
+    if grouped:
+        assert (y[-2:] == 7.0).all() and (dx[-2:] == 7.0).all()
 
 
 # --------------------------------------------------------------- together
@@ -660,7 +740,7 @@ def test_block_gradients_through_the_routed_experts(T):
                            max_tokens=300, norm=1 + n(d).float(), gate=n(d, E).float(),
                            shared=(n(d, 200), n(d, 200), n(200, d)),
                            experts=cep.make_weights(*experts), w_dtype=cep.CEP_BF16)
-    routed = moe_block.RoutedExperts(top_k=k, max_tokens=300, w_gate=experts[0], w_up=experts[1],
+    routed = moe_block.RoutedExperts(top_k=k, w_gate=experts[0], w_up=experts[1],
                                      w_down=experts[2])
     # the sum x + residual is exact in bf16: it is saved without a rounding of its own
     x = (torch.randint(-32, 33, (T, d), device="cuda", generator=g) / 16).bfloat16()
@@ -688,11 +768,47 @@ def test_block_gradients_through_the_routed_experts(T):
     b.close()
 
 
+def test_routed_experts_on_two_streams():
+    """Two sets of experts at work at once, each on a stream of its own, the backward
+    pass on another one than the forward pass."""
+    from paper_2609_33252_amd import moe_block
+    T, d, I, E, k = 500, 256, 264, 6, 3
+    g = _gen(8)
+    n = lambda *s: _randn(g, *s, std=0.1)
+    sets = []
+    for _ in range(2):
+        r = moe_block.RoutedExperts(top_k=k, w_gate=n(E, d, I), w_up=n(E, d, I), w_down=n(E, I, d))
+        ids = torch.randint(-1, E, (T, k), device="cuda", generator=g).int()
+        sets.append((r, _randn(g, T, d), ids, torch.rand(T, k, device="cuda", generator=g), n(T, d)))
+
+    def alone(r, y, ids, c, dt):
+        out = r.forward(y, ids, c, train=True)
+        return [out, *(lambda a, b, e: [a, b, *e])(*r.backward(dt))]
+
+    want = [alone(*s) for s in sets]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for (r, y, ids, c, dt), s in zip(sets, streams):
+            with torch.cuda.stream(s):
+                got.append([r.forward(y, ids, c, train=True)])
+        for s in streams[:2]:
+            streams[2].wait_stream(s)
+        for (r, *_, dt), o in zip(sets, got):
+            with torch.cuda.stream(streams[2]):
+                d_y, d_c, dw = r.backward(dt)
+                o += [d_y, d_c, *dw]
+        torch.cuda.synchronize()
+        for w, o in zip(want, got):
+            assert all(torch.equal(a, b) for a, b in zip(w, o))
+
+
 def test_routed_experts_refuse_what_their_operators_would_misread():
     from paper_2609_33252_amd import moe_block
     bf = dict(dtype=torch.bfloat16, device="cuda")
     w = [torch.zeros(4, 64, 32, **bf), torch.zeros(4, 64, 32, **bf), torch.zeros(4, 32, 64, **bf)]
-    make = lambda a, b, c: moe_block.RoutedExperts(top_k=2, max_tokens=8, w_gate=a, w_up=b, w_down=c)
+    make = lambda a, b, c: moe_block.RoutedExperts(top_k=2, w_gate=a, w_up=b, w_down=c)
     for i in range(3):
         for wrong in (w[i].float(), w[i][:3], w[i].cpu(), w[i].transpose(1, 2)):
             with pytest.raises(ValueError):
@@ -703,7 +819,7 @@ def test_routed_experts_refuse_what_their_operators_would_misread():
     with pytest.raises(ValueError):
         r.backward(y)
     for bad in ((y.float(), ids, c), (y[:, :32], ids, c), (y, ids.long(), c), (y, ids, c.double()),
-                (y, ids[:7], c), (torch.zeros(9, 64, **bf), ids, c)):
+                (y, ids[:7], c), (torch.zeros(9, 64, **bf), ids, c), (y.t(), ids, c)):
         with pytest.raises(ValueError):
             r.forward(*bad)
     r.forward(y, ids, c)
@@ -714,6 +830,19 @@ def test_routed_experts_refuse_what_their_operators_would_misread():
         r.backward(y[:7])
 
 
+def test_routed_experts_of_no_tokens():
+    from paper_2609_33252_amd import moe_block
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    r = moe_block.RoutedExperts(top_k=2, w_gate=torch.ones(4, 64, 32, **bf),
+                                w_up=torch.ones(4, 64, 32, **bf), w_down=torch.ones(4, 32, 64, **bf))
+    for T in (0, 3):  # no tokens; tokens of no expert
+        ids = torch.full((T, 2), -1, dtype=torch.int32, device="cuda")
+        out = r.forward(torch.ones(T, 64, **bf), ids, torch.ones(T, 2, device="cuda"), train=True)
+        d_y, d_w, dw = r.backward(torch.ones(T, 64, **bf))
+        assert (out == 0).all() and (d_y == 0).all() and (d_w == 0).all()
+        assert all((t == 0).all() for t in dw)
+
+
 @pytest.mark.parametrize("seed", [0, 1])
 def test_routed_experts_match_differences(seed):
     """Directional derivatives of the float64 form beside the gradients' product with
@@ -722,7 +851,7 @@ def test_routed_experts_match_differences(seed):
     T, d, I, E, k = 40, 64, 40, 5, 2
     g = _gen(seed + 50)
     w = [_randn(g, E, d, I, std=0.2), _randn(g, E, d, I, std=0.2), _randn(g, E, I, d, std=0.2)]
-    r = moe_block.RoutedExperts(top_k=k, max_tokens=T, w_gate=w[0], w_up=w[1], w_down=w[2])
+    r = moe_block.RoutedExperts(top_k=k, w_gate=w[0], w_up=w[1], w_down=w[2])
     y, dt = _randn(g, T, d), _randn(g, T, d)
     ids = torch.randint(-1, E, (T, k), device="cuda", generator=g).int()
     c = torch.rand(T, k, device="cuda", generator=g)

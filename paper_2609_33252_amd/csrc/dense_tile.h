@@ -44,8 +44,8 @@ __device__ inline int piece_of(int items, int x) { return items / 8 + (x < items
 // second product.  A has k or m contiguous (A_K), B k or n (B_K).
 //
 // STAGED: the sums go through LDS first, and out.load(m, n) and out.store(m, n, v, w,
-// loaded) take eight columns of a row, four rows' loads on the way at once: for an
-// epilogue that reads a matrix of its own.
+// loaded, out.column(n)) take eight columns of a row, four rows' loads on the way at
+// once: for an epilogue that reads a matrix of its own.
 //
 // Each operand's 64-wide step is two halves of HALF rows (columns), loaded
 // straight to LDS; the operands' halves meet in four quadrants, one phase
@@ -329,6 +329,7 @@ __device__ inline void dense_tile(const TileArgs &a, int m0, int n0, int share, 
       meet();
       const int c8 = tid % PER, n = n0 + c8 * 8;
       if (n < a.N) {
+        const auto column = out.column(n);
         for (int r0 = tid / PER; r0 < HALF; r0 += AT_ONCE * ROWS) {
           decltype(out.load(0, 0)) in[AT_ONCE];
 #pragma unroll
@@ -340,7 +341,7 @@ __device__ inline void dense_tile(const TileArgs &a, int m0, int n0, int share, 
           for (int u = 0; u < AT_ONCE; ++u) {
             const int r = r0 + u * ROWS;
             const int64_t m = m0 + mh * HALF + r;
-            if (m < a.M) out.store(m, n, *at(r, 2 * c8), *at(r, 2 * c8 + 1), in[u]);
+            if (m < a.M) out.store(m, n, *at(r, 2 * c8), *at(r, 2 * c8 + 1), in[u], column);
           }
         }
       }

@@ -196,7 +196,17 @@ __device__ inline void finish(const Finish &f, int64_t m, int n, int g, f32x4 z)
   store4(f.y, f.y_dtype, m * f.ld_y + n, v);
 }
 
-// The same for eight columns, in two steps.
+// The same for eight columns, in steps: what a column needs, what a row's columns need.
+struct Column {
+  f32x4 bias[2];
+};
+__device__ inline Column column_of(const Finish &f, int n, int g) {
+  Column c{};
+  if (f.bias)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) c.bias[h] = *(const f32x4 *)(f.bias + (int64_t)g * f.N + n + 4 * h);
+  return c;
+}
 struct Loaded {
   Vec16 mul, res[2];
 };
@@ -214,12 +224,12 @@ __device__ inline f32x4 half_of(const Vec16 &v, int h) {  // four of eight bf16 
   return from_bf16(v[2 * h], v[2 * h + 1]);
 }
 template <int ACT>
-__device__ inline void finish_eight(const Finish &f, int64_t m, int n, int g, const f32x4 &lo,
-                                    const f32x4 &hi, const Loaded &in) {
+__device__ inline void finish_eight(const Finish &f, int64_t m, int n, const f32x4 &lo,
+                                    const f32x4 &hi, const Loaded &in, const Column &c) {
   f32x4 v[2] = {lo, hi};
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    if (f.bias) v[h] += *(const f32x4 *)(f.bias + (int64_t)g * f.N + n + 4 * h);
+    if (f.bias) v[h] += c.bias[h];
     if (f.pre) *(f32x4 *)(f.pre + m * f.N + n + 4 * h) = v[h];
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[h][r] = act_of<ACT>(v[h][r]);
@@ -247,14 +257,15 @@ struct TileOut {
   __device__ inline Loaded load(int64_t m, int n) const {
     return part ? Loaded{} : load_eight(f, row0 + m, n);
   }
-  __device__ inline void store(int64_t m, int n, const f32x4 &lo, const f32x4 &hi,
-                               const Loaded &in) const {
+  __device__ inline Column column(int n) const { return part ? Column{} : column_of(f, n, g); }
+  __device__ inline void store(int64_t m, int n, const f32x4 &lo, const f32x4 &hi, const Loaded &in,
+                               const Column &c) const {
     if (part) {
       float *p = part + (row0 + m) * f.N + n;
       *(f32x4 *)p = lo;
       *(f32x4 *)(p + 4) = hi;
     } else {
-      finish_eight<ACT>(f, row0 + m, n, g, lo, hi, in);
+      finish_eight<ACT>(f, row0 + m, n, lo, hi, in, c);
     }
   }
   __device__ inline void operator()(int64_t m, int n, const f32x4 &v, const f32x4 &) const {
@@ -431,7 +442,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
 // and its store, so that several share a compute unit (32 KB of LDS) instead of one
 // running ahead of itself.  64 rows at a time, [64 rows][128 columns] of each operand,
 // 16-byte chunk pair p of line k at p ^ f(k); lines past the group's rows are zeros.
-// Measured: FEW_US.
+// Measured: 32 groups of 34 rows of 4096 x 2048 154 us, 3.5 TB/s of stores (the tiles
+// above 262); 16 of 128 rows 110 (175).  Stored straight from the accumulators 177 and 124.
 __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
   constexpr int F = 4;  // fragments of a wave in each operand
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][16384];
@@ -514,8 +526,8 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
       const int r = u * 16 + (tid >> 4), n = w.n0 + chunk * 8;
       const int64_t m = w.m0 + (r >> 4) * 64 + i * 16 + (r & 15);
       if (m < a.M && n < a.N)
-        finish_eight<CEP_IDENTITY>(a.f, (int64_t)w.g * a.M + m, n, 0, *at(i, r, 2 * chunk),
-                                   *at(i, r, 2 * chunk + 1), Loaded{});
+        finish_eight<CEP_IDENTITY>(a.f, (int64_t)w.g * a.M + m, n, *at(i, r, 2 * chunk),
+                                   *at(i, r, 2 * chunk + 1), Loaded{}, Column{});
     }
   }
 }
@@ -579,8 +591,13 @@ __global__ __launch_bounds__(256) void k_linear_rows(LinearRowsArgs a) {
 
 // ---- the gradient of the epilogue
 
-constexpr int kDzRows = 32;   // rows of a k_linear_dz block
-constexpr int kDzCols = 256;  // and columns: 32 lanes of eight, eight rows at a time
+constexpr int kDzCols = 256;  // columns of a k_linear_dz block: 32 lanes of eight
+// Its rows, eight at a time: one round of them where blocks are few (us, 8 and 32 rows:
+// 109 x
+// 1408 3.5, 6.2; 378 x 1896 4.7, 8.1; 1116 x 2048 6.6, 12.0), four elsewhere, which leaves fewer sums.
+inline int dz_rows(int rows, int N) {
+  return (int64_t)((rows + 31) / 32) * ((N + kDzCols - 1) / kDzCols) < 512 ? 8 : 32;
+}
 
 struct DzArgs {
   const void *dy;
@@ -599,21 +616,21 @@ struct DzArgs {
 // are db, and those of groups without rows get zeros.  Bound by HBM: 4095 x 2048 from
 // bf16 with GELU and sums 15.7 us, 4.3 TB/s; 8192 x 2048 with SiLU and a factor 42, 4.8.
 // (Eight rows of four columns a lane at once, in fewer waves: 23 and 56.)
-template <int ACT>
+template <int ACT, int ROWS>
 __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
-  __shared__ float sums[kDzRows][kDzCols];
-  __shared__ int group[kDzRows];  // of a row
+  __shared__ float sums[ROWS][kDzCols];
+  __shared__ int group[ROWS];  // of a row
   const int tid = threadIdx.x, lane = tid & 31, rl = tid >> 5;
   const int n = (int)blockIdx.y * kDzCols + lane * 8;
-  const int row0 = blockIdx.x * kDzRows;
-  const int end = min(row0 + kDzRows, a.groups.rows);
+  const int row0 = blockIdx.x * ROWS;
+  const int end = min(row0 + ROWS, a.groups.rows);
   int from = row0, to = end;  // the rows of some group
   if (a.groups.n) {
     from = max(from, a.groups.offsets[0]);
     to = min(to, a.groups.offsets[a.groups.n]);
   }
   if (n < a.N) {
-    for (int r = rl; r < kDzRows; r += 8) {
+    for (int r = rl; r < ROWS; r += 8) {
       const int64_t m = row0 + r;
       float out[8] = {};
       if (m >= from && m < to) {
@@ -642,12 +659,12 @@ __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
     int mine = 0;  // of row row0 + tid: how many groups end up to it
     for (int g0 = 0; g0 < a.groups.n; g0 += 64) {
       const int stop = g0 + tid < a.groups.n ? a.groups.offsets[g0 + tid + 1] : INT32_MAX;
-      for (int r = 0; r < kDzRows; ++r) {
+      for (int r = 0; r < ROWS; ++r) {
         const int n_ended = (int)__popcll(__ballot(stop <= row0 + r));
         if (tid == r) mine += n_ended;
       }
     }
-    if (tid < kDzRows) group[tid] = mine;
+    if (tid < ROWS) group[tid] = mine;
   }
   __syncthreads();
   const int c = (int)blockIdx.y * kDzCols + tid;  // a column a thread
@@ -656,7 +673,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
   if (a.groups.n == 0) {
     float sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < kDzRows; ++r) sum += sums[r][tid];
+    for (int r = 0; r < ROWS; ++r) sum += sums[r][tid];
     *line = sum;
     return;
   }
@@ -677,17 +694,17 @@ __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
 }
 
 // db of a group: its lines of `part`, added in order by 16 lanes of columns' fours.
-__global__ __launch_bounds__(256) void k_linear_dbias(const float *part, int N, Groups groups,
-                                                      float *db) {
+__global__ __launch_bounds__(256) void k_linear_dbias(const float *part, int rows, int N,
+                                                      Groups groups, float *db) {
   __shared__ f32x4 sums[16][16];
   const int lane = threadIdx.x & 15, sl = threadIdx.x >> 4, g = blockIdx.y;
   const int n = ((int)blockIdx.x * 16 + lane) * 4;
   const Span s = groups.n ? span_of(groups, g) : Span{0, groups.rows};
   f32x4 v = {};
   if (s.n && n < N) {
-    const int last = (s.lo + s.n - 1) / kDzRows;
+    const int last = (s.lo + s.n - 1) / rows;
 #pragma unroll 4
-    for (int c = s.lo / kDzRows + sl; c <= last; c += 16)
+    for (int c = s.lo / rows + sl; c <= last; c += 16)
       v += *(const f32x4 *)(part + (int64_t)(c + g) * N + n);
   }
   sums[sl][lane] = v;
@@ -756,6 +773,17 @@ Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
   const double us = (double)((whole + kUnits - 1) / kUnits) * (12 + 1.4 * (K / 64)) +
                     (double)((quarters + kUnits - 1) / kUnits) * (3 + 0.55 * (K / 64));
   if (us < d.us) p.tile = 0, p.splits = 1, p.us = us;
+  // Few 128-wide tiles of one weight share K in shorter pieces than that estimate takes
+  // (us, shared and not: 378 x 1896 x 976 with a factor and z kept 17.3, 21.0; 648 x 632 x
+  // 1024 13.6, 13.9; 64 x 1024 x 1024 9.3, 11.3; of eight groups 700 x 1024 x 1024 16.4,
+  // 14.4)
+  if (!groups && tiles[1] <= 128) {
+    double least = 7 + 0.65 * (K / 64.0);
+    for (int s = 2; s <= 16 && tiles[1] * s <= 256 && K / 64 / s >= 4; ++s) {
+      const double split = 9 + 0.6 * (K / 64.0 / s) + (double)s * rows * N * 4 / 9e6;
+      if (split < least) least = split, p.tile = 1, p.splits = s, p.us = split;
+    }
+  }
   return p;
 }
 
@@ -819,7 +847,10 @@ size_t part_bytes(const Plan &p, int rows, int N) {
   return p.splits > 1 ? (size_t)p.splits * rows * N * 4 : 0;
 }
 
-int dz_chunks(const cep_linear_desc *d) { return (d->rows + kDzRows - 1) / kDzRows; }
+int dz_chunks(const cep_linear_desc *d) {
+  const int rows = dz_rows(d->rows, d->d_out);
+  return (d->rows + rows - 1) / rows;
+}
 
 // Scratch of the backward pass: dz, the parts of db, the K shares of a product.
 struct Space {
@@ -922,6 +953,15 @@ void launch_linear(const Plan &p, const Groups &g, const __bf16 *A, int64_t lda,
   if (p.splits > 1) launch_finish(part, p.splits, g, f, g.rows, s);
 }
 
+template <int ROWS>
+auto dz_kernel(int act) {
+  return act == CEP_RELU        ? k_linear_dz<CEP_RELU, ROWS>
+         : act == CEP_SILU      ? k_linear_dz<CEP_SILU, ROWS>
+         : act == CEP_GELU      ? k_linear_dz<CEP_GELU, ROWS>
+         : act == CEP_GELU_TANH ? k_linear_dz<CEP_GELU_TANH, ROWS>
+                                : k_linear_dz<CEP_IDENTITY, ROWS>;
+}
+
 int check_shared(const char *fn, const cep_linear_desc *d, const int32_t *offsets) {
   if (const char *why = bad_desc(d)) return refuse(CEP_EINVAL, "%s: %s", fn, why);
   if (!offsets != !d->n_groups)
@@ -1004,17 +1044,13 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
     a.part = dbias ? (dz_chunks(d) == 1 ? dbias : sums) : nullptr;
     a.N = N, a.groups = g;
     const dim3 grid(dz_chunks(d), (N + kDzCols - 1) / kDzCols);
-    auto *k = d->act == CEP_RELU        ? k_linear_dz<CEP_RELU>
-              : d->act == CEP_SILU      ? k_linear_dz<CEP_SILU>
-              : d->act == CEP_GELU      ? k_linear_dz<CEP_GELU>
-              : d->act == CEP_GELU_TANH ? k_linear_dz<CEP_GELU_TANH>
-                                        : k_linear_dz<CEP_IDENTITY>;
+    auto *k = dz_rows(T, N) == 8 ? dz_kernel<8>(d->act) : dz_kernel<32>(d->act);
     hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
   }
   if (!same) dz = (const __bf16 *)ws, ld_z = N;
   if (dbias && dz_chunks(d) != 1)
-    hipLaunchKernelGGL(k_linear_dbias, dim3((N + 63) / 64, n_groups), dim3(256), 0, s, sums, N, g,
-                       dbias);
+    hipLaunchKernelGGL(k_linear_dbias, dim3((N + 63) / 64, n_groups), dim3(256), 0, s, sums,
+                       dz_rows(T, N), N, g, dbias);
   Finish f{};
   f.res = dx_add, f.y = dx, f.N = D, f.res_dtype = f.y_dtype = d->dx_dtype;
   f.ld_res = f.ld_y = d->ld_dx ? d->ld_dx : D;

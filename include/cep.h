@@ -587,7 +587,7 @@ typedef struct {
  * x [rows][d_in] bf16; w [d_in][d_out] bf16 (the math orientation of cep_weights,
  * read as it is); bias [d_out] float32, mul [rows][d_out] bf16, residual
  * [rows][d_out] (res_dtype; may be y itself if types and strides agree), each may
- * be NULL.  y (y_dtype) may not overlap x.  preact (NULL: not kept) gets z, float32
+ * be NULL.  y (y_dtype) and preact may not overlap x or each other.  preact (NULL: not kept) gets z, float32
  * [rows][d_out], for cep_linear_backward.
  * With groups, w is [n_groups][d_in][d_out] and bias [n_groups][d_out], and offsets,
  * device int32 [n_groups + 1], ascending within 0..rows, gives the rows
@@ -610,7 +610,7 @@ int cep_linear(const cep_linear_desc *desc, const void *x, const void *w, const 
  * dx (dx_dtype), dw (dw_dtype, layout of w), dbias (float32, layout of bias) and
  * dmul (bf16, layout of mul) are written, not added to, and each may be NULL; so may
  * w without dx and x without dw.  dx_add (dx_dtype, NULL: none, may be dx itself)
- * joins dx.  A group without rows gets zeros in dw and dbias.  dz is rounded to bf16
+ * joins dx, which overlaps neither dy nor x.  A group without rows gets zeros in dw and dbias.  dz is rounded to bf16
  * once, for the products that follow (dbias sums it before that).  The residual's
  * gradient is dy. */
 int cep_linear_backward(const cep_linear_desc *desc, const void *dy, const void *x, const void *w,

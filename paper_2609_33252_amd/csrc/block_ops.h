@@ -1,5 +1,5 @@
 // Device and host helpers shared by the operators around the routed experts
-// (norm, gate, dispatch, dense gated feed-forward).  Internal to libcep.
+// (norm, gate, dispatch, sort, dense feed-forward).  Internal to libcep.
 #pragma once
 
 #include "cep.h"

@@ -4,7 +4,8 @@
 //   y[t] = r[t] + sum over j of w[t][j] ys[place[t][j]]
 //   dys[place[t][j]] = w[t][j] dy[t];  dw[t][j] = <dy[t], ys[place[t][j]]>
 //
-// Every row is read and written once: bound by HBM.  The sum over the slots and the
+// Every row is read and written once: bound by HBM (8192 tokens of 6 rows of 4096, bf16:
+// 106 us, 536 MB, 5.1 TB/s; the gradient 168 us, 870 MB, 5.2 TB/s).  The sum over the slots and the
 // product over the channels have a fixed order, so results do not depend on timing.
 #include "block_ops.h"
 
@@ -166,7 +167,11 @@ void launch_unsort(const UnsortArgs &a, hipStream_t s) {
 }
 template <int KM, bool YS32>
 void launch_grad(const UnsortArgs &a, hipStream_t s) {
-  if (a.d <= 512)
+  // A wave a row, or a workgroup: its waves each start anew for a token, which short rows
+  // do not repay, and more of them are on the way with few tokens (8192 tokens of 6 rows,
+  // us, wave and workgroup: of 256 values 18, 51; 512 22, 50; 1024 47, 60; 2048 102, 93;
+  // 60 tokens: of 512 5.7, 6.4; 2048 13, 6.7)
+  if (a.d <= 1024)
     hipLaunchKernelGGL((k_unsort_grad<64, KM, YS32>), dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_unsort_grad<256, KM, YS32>), dim3(a.rows), dim3(256), 0, s, a);

@@ -375,7 +375,9 @@ __device__ inline float grad_logit(const GateGradArgs &a, int64_t row, int e) {
 
 // LPR lanes a row, V experts a lane (chunk c of a lane is the four experts from (c *
 // LPR + lane) * 4); lane j holds slot j.  The slots' values meet their experts in
-// LDS, from which a row is written whole.
+// LDS, from which a row is written whole.  Bound by HBM and the exponentials of an
+// unnormalised softmax: 65536 rows of 160 experts 24 us, 3.7 TB/s (with a wave a row 43,
+// the sums over lanes being as long for fewer experts each); nine rows of 256 3.2.
 template <int LPR, int V>
 __global__ __launch_bounds__(256) void k_gate_grad(GateGradArgs a) {
   constexpr int ROWS = 256 / LPR;

@@ -7,7 +7,10 @@
 //
 // Few rows a group stream the weights (rows_tile.h), more run the tiled product
 // (dense_tile.h); the tiles of grouped rows are found on the device from the
-// groups' offsets, the grid covers their most.
+// groups' offsets, the grid covers their most.  Bound by HBM with few rows (24 rows on
+// eight weights of 4096 x 2048 25 us, 5.4 TB/s), else by the matrix instructions (8192 x
+// 2048 x 7168 with bias and GELU 179 us, 1.34 PFLOP/s) and, where the epilogue reads a
+// factor or keeps z, by its bytes (eight groups of 8192 x 2048 x 4096 with both 165 us).
 #include "dense_tile.h"
 #include "rows_tile.h"
 
@@ -308,7 +311,9 @@ struct TileWork {
   }
 };
 
-// y (B_K false) or dx (true: N is d_in) in 128-wide tiles of whole groups' rows.
+// y (B_K false) or dx (true: N is d_in) in 128-wide tiles of whole groups' rows, two
+// workgroups a compute unit.  4095 x 2048 x 4096 with GELU and z kept 85 us, 0.8 PFLOP/s:
+// one round, whose tiles all store at its end; 777 x 6144 x 2560 with a residual 42.
 template <bool B_K, bool STAGED, int ACT>
 __global__ __launch_bounds__(256, 2) void k_linear_128(LinearArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[65536];
@@ -344,7 +349,8 @@ __global__ __launch_bounds__(512, 2) void k_linear_256(LinearArgs a) {
 }
 
 // The shares' sums of a row, added in order, eight on the way at once, and what becomes
-// of them.
+// of them.  A launch's start and a trip to memory: one row of 2048 3.0 us, 24 rows of
+// groups 4.7.
 constexpr int kFinishThreads = 128;
 __global__ __launch_bounds__(kFinishThreads) void k_linear_finish(const float *part, int splits,
                                                                   Groups groups, Finish f) {
@@ -430,7 +436,8 @@ __device__ inline void wgrad_run(const WgradArgs &a, const WgradTile &w, uint8_t
   dense_tile<HALF, WM, WN, false, false, false>(t, w.m0, w.n0, w.share, lds, out);
 }
 
-// dW of each group, its rows as K.
+// dW of each group, its rows as K, both operands read across: 4096 x 2048 of 4095 rows in
+// 128-wide tiles 72 us, 0.95 PFLOP/s.
 template <int HALF, int WM, int WN>
 __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
@@ -442,8 +449,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
 // and its store, so that several share a compute unit (32 KB of LDS) instead of one
 // running ahead of itself.  64 rows at a time, [64 rows][128 columns] of each operand,
 // 16-byte chunk pair p of line k at p ^ f(k); lines past the group's rows are zeros.
-// Measured: 32 groups of 34 rows of 4096 x 2048 154 us, 3.5 TB/s of stores (the tiles
-// above 262); 16 of 128 rows 110 (175).  Stored straight from the accumulators 177 and 124.
+// Measured: 32 groups of 34 rows of 4096 x 2048 154 us, 3.5 TB/s of stores
+// (k_linear_wgrad 262); 16 of 128 rows 110 (175).  Stored straight from the accumulators 177 and 124.
 __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
   constexpr int F = 4;  // fragments of a wave in each operand
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][16384];
@@ -569,6 +576,9 @@ struct LinearRowsArgs : RowsArgs {
   Finish f;
 };
 
+// Few rows, MF * 16 of a group at a time, the weights read past them once.  Bound by HBM:
+// one row of 7168 x 2048 7.9 us with its start and end, 24 rows of eight groups of 4096 x
+// 2048 25 us, 5.4 TB/s.
 template <int MF>
 __global__ __launch_bounds__(256) void k_linear_rows(LinearRowsArgs a) {
   __shared__ RowsLds<MF, kRows> lds;
@@ -593,8 +603,8 @@ __global__ __launch_bounds__(256) void k_linear_rows(LinearRowsArgs a) {
 
 constexpr int kDzCols = 256;  // columns of a k_linear_dz block: 32 lanes of eight
 // Its rows, eight at a time: one round of them where blocks are few (us, 8 and 32 rows:
-// 109 x
-// 1408 3.5, 6.2; 378 x 1896 4.7, 8.1; 1116 x 2048 6.6, 12.0), four elsewhere, which leaves fewer sums.
+// 109 x 1408 3.5, 6.2; 378 x 1896 4.7, 8.1; 1116 x 2048 6.6, 12.0), four elsewhere, which
+// leaves fewer sums.
 inline int dz_rows(int rows, int N) {
   return (int64_t)((rows + 31) / 32) * ((N + kDzCols - 1) / kDzCols) < 512 ? 8 : 32;
 }
@@ -745,15 +755,18 @@ struct Plan {
   double us;  // estimated
 };
 
-// Rows of a group, on average, up to which the weights are streamed.
-constexpr int kStreamRows = 32;
+// Rows of one weight, and of a group on average, up to which the weights are streamed:
+// the tiled product reads each weight once for all its rows, with fewer loads on the way
+// at a time (4096 x 2048, us streamed and tiled: 16 rows 6.4, 8.3; 32 7.5, 8.6; 48 11.3,
+// 9.2; of eight groups 3 rows each 24.9, 29.4; 8 30.4, 34.8; 12 40.2, 35.2; 32 42, 34).
+constexpr int kStreamRows = 32, kStreamGroup = 10;
 
 Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
   Plan p{};
   const int g = std::max(groups, 1);
-  if (may_stream && rows <= (int64_t)kStreamRows * g) {
+  if (may_stream && rows <= (int64_t)(groups ? kStreamGroup : kStreamRows) * g) {
     p.stream = true;
-    p.mf = rows <= 16 * g ? 1 : 2;
+    p.mf = rows <= 16 * g ? 1 : 2;  // (16 rows 6.4, 32 in one block 7.5)
     // one workgroup a compute unit (a ring takes most of its LDS), at least a unit
     // for each wave
     const int cols = (N + kCols - 1) / kCols, blocks = cols * std::min(g, std::max(rows, 1));
@@ -992,6 +1005,8 @@ CEP_API int cep_linear(const cep_linear_desc *d, const void *x, const void *w, c
   if (!workspace || workspace_bytes < cep_linear_workspace(d, 0))
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_linear_workspace(d, 0));
+  if (y == x || preact == x || (const void *)preact == y)
+    return refuse(CEP_EINVAL, "%s: y, preact and x overlap", fn);
   const int D = d->d_in, N = d->d_out;
   Finish f{};
   f.bias = bias, f.mul = (const __bf16 *)mul, f.res = residual, f.y = y, f.pre = preact;
@@ -1025,6 +1040,7 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
   if (!workspace || workspace_bytes < cep_linear_workspace(d, 1))
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_linear_workspace(d, 1));
+  if (dx && (dx == dy || dx == x)) return refuse(CEP_EINVAL, "%s: dx overlaps dy or x", fn);
   const int D = d->d_in, N = d->d_out, T = d->rows, n_groups = std::max(d->n_groups, 1);
   const Space space = space_of(d, 1);
   const Groups g{offsets, d->n_groups, T};

@@ -165,6 +165,16 @@ def test_linear_refuses_arguments():
     f(_linear(rows=0), None, None, None, None)  # nothing to do, nothing launched
 
 
+def test_linear_refuses_outputs_over_its_inputs():
+    f, b = cep.cep_linear, cep.cep_linear_backward
+    x, w, y = PTR, PTR + 1024, PTR + 2048
+    _refused(cep.CEP_EINVAL, f, _linear(), x, w, x, BIG)
+    _refused(cep.CEP_EINVAL, f, _linear(), x, w, y, BIG, preact=x)
+    _refused(cep.CEP_EINVAL, f, _linear(), x, w, y, BIG, preact=y)
+    _refused(cep.CEP_EINVAL, b, _linear(), y, x, w, BIG, dx=y)
+    _refused(cep.CEP_EINVAL, b, _linear(), y, x, w, BIG, dx=x, dw=PTR + 4096)
+
+
 # ------------------------------------------------------------ gate gradient
 
 def _gate(**kw):

@@ -70,13 +70,14 @@ SORTS = [
     (0, 2, 4, 64, 0, "any"), (1, 1, 1, 1, 0, "any"), (1, 16, 1024, 14336, 0, "any"),
     (13, 8, 32, 14336, 0, "few"), (16, 16, 64, 17, 1, "any"), (255, 4, 5, 33, 0, "any"),
     (300, 8, 16, 1000, 24, "few"), (512, 8, 64, 272, 0, "any"),   # the last in one launch
-    (513, 8, 64, 272, 0, "any"), (257, 16, 1024, 130, 6, "any"),  # three launches
+    (513, 8, 64, 272, 0, "any"), (257, 16, 1024, 130, 6, "any"),  # more launches
     (1000, 5, 3, 16, 0, "any"), (5000, 1, 7, 2, 3, "any"), (3001, 7, 160, 4112, 0, "few"),
     (600, 8, 64, 131072, 0, "few"), (20000, 16, 1023, 8, 0, "any"),
     (4096, 8, 1, 48, 0, "any"), (4097, 8, 64, 48, 0, "one"), (4097, 2, 64, 48, 0, "none"),
     (1 << 17, 16, 300, 1, 0, "any"),
     # the counts summed by the rows' workgroups, up to both limits, and past them
     (600, 15, 511, 40, 0, "any"), (600, 15, 512, 40, 0, "any"), (1024, 16, 510, 24, 0, "few"),
+    (500, 16, 511, 24, 0, "any"), (4100, 11, 80, 33, 0, "any"), (4700, 11, 80, 33, 0, "any"),
     (1025, 16, 511, 24, 0, "any"), (9000, 11, 80, 33, 0, "any"), (9400, 11, 80, 33, 0, "any"),
 ]
 

@@ -312,16 +312,19 @@ struct TileWork {
 };
 
 // y (B_K false) or dx (true: N is d_in) in 128-wide tiles of whole groups' rows, two
-// workgroups a compute unit.  4095 x 2048 x 4096 with GELU and z kept 85 us, 0.8 PFLOP/s:
-// one round, whose tiles all store at its end; 777 x 6144 x 2560 with a residual 42.
+// workgroups of eight waves a compute unit.  4095 x 2048 x 4096 with GELU and z kept 84
+// us, 0.8 PFLOP/s: one round, whose tiles all store at its end.  (us, eight and four
+// waves: 777 x 6144 x 2560 with a residual 38.7, 39.7; 3000 x 1408 x 2048 in 16 groups
+// 41.4, 43.9; 378 x 1896 x 976 in two shares 11.2, 12.7; one workgroup a unit 50 for the
+// second)
 template <bool B_K, bool STAGED, int ACT>
-__global__ __launch_bounds__(256, 2) void k_linear_128(LinearArgs a) {
+__global__ __launch_bounds__(512, 4) void k_linear_128(LinearArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[65536];
   const int x = blockIdx.x & 7, at = blockIdx.x >> 3;
   const TileWork<128, B_K, STAGED, ACT> work{a, tiles_of<128>(a.groups), (a.N + 127) / 128, lds};
   const int items = work.n_tm * a.splits * work.n_tn;
   if (at >= piece_of(items, x)) return;
-  work.template run<64, 2, 2>(x * (items / 8) + min(x, items % 8) + at, 0, 0);
+  work.template run<64, 2, 4>(x * (items / 8) + min(x, items % 8) + at, 0, 0);
 }
 
 // ... in 256-wide ones, one a compute unit.  Where a few are left after the last full
@@ -437,22 +440,23 @@ __device__ inline void wgrad_run(const WgradArgs &a, const WgradTile &w, uint8_t
 }
 
 // dW of each group, its rows as K, both operands read across: 4096 x 2048 of 4095 rows in
-// 128-wide tiles 72 us, 0.95 PFLOP/s.
+// 128-wide tiles 72 us, 0.95 PFLOP/s; 976 x 1896 of 378 rows 9.1 (with four waves 12.1).
 template <int HALF, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_wgrad(WgradArgs a) {
+__global__ __launch_bounds__(WM * WN * 64, HALF == 64 ? 4 : 2) void k_linear_wgrad(WgradArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
   WgradTile t;
   if (wgrad_item<2 * HALF>(a, blockIdx.x & 7, blockIdx.x >> 3, &t)) wgrad_run<HALF, WM, WN>(a, t, lds);
 }
 
-// dW of groups of few rows, in 128-wide tiles by 2 x 2 waves: a tile is mostly its start
+// dW of groups of few rows, in 128-wide tiles by 2 x 4 waves: a tile is mostly its start
 // and its store, so that several share a compute unit (32 KB of LDS) instead of one
 // running ahead of itself.  64 rows at a time, [64 rows][128 columns] of each operand,
 // 16-byte chunk pair p of line k at p ^ f(k); lines past the group's rows are zeros.
-// Measured: 32 groups of 34 rows of 4096 x 2048 154 us, 3.5 TB/s of stores
-// (k_linear_wgrad 262); 16 of 128 rows 110 (175).  Stored straight from the accumulators 177 and 124.
-__global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
-  constexpr int F = 4;  // fragments of a wave in each operand
+// Measured: 32 groups of 34 rows of 4096 x 2048 147 us, 3.7 TB/s of stores
+// (k_linear_wgrad 262); 16 of 128 rows 108 (175).  By 2 x 2 waves 154 and 110, those
+// stored straight from the accumulators 177 and 124; four workgroups a unit spill.
+__global__ __launch_bounds__(512, 6) void k_linear_wgrad_few(WgradArgs a) {
+  constexpr int MF = 4, NF = 2;  // fragments of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2][16384];
   WgradTile w;
   if (!wgrad_item<128>(a, blockIdx.x & 7, blockIdx.x >> 3, &w)) return;
@@ -469,12 +473,12 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
   const int chunk = tid & 15;
   const __bf16 *srcA = a.A + lo * a.lda + min(w.m0 + chunk * 8, a.M - 8);
   const __bf16 *srcB = a.B0 + lo * a.ldb + min(w.n0 + chunk * 8, a.N - 8);
-  f32x4 acc[F][F] = {};
+  f32x4 acc[MF][NF] = {};
   for (int k0 = 0; k0 < K; k0 += 64) {
-    uint4 v[2][4];
+    uint4 v[2][2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t k = k0 + e * 16 + (tid >> 4);
+    for (int e = 0; e < 2; ++e) {
+      const int64_t k = k0 + e * 32 + (tid >> 4);
       v[0][e] = v[1][e] = make_uint4(0u, 0u, 0u, 0u);
       if (k < K) {
         v[0][e] = *(const uint4 *)(srcA + k * a.lda);
@@ -483,8 +487,8 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
     }
     if (k0) __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int k = e * 16 + (tid >> 4);
+    for (int e = 0; e < 2; ++e) {
+      const int k = e * 32 + (tid >> 4);
       const int to = k * 256 + (((chunk >> 1) ^ f_of(k)) << 5) + (chunk & 1) * 16;
       *(uint4 *)(lds[0] + to) = v[0][e];
       *(uint4 *)(lds[1] + to) = v[1][e];
@@ -503,16 +507,15 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
                                                             (l15 & 3) * 8));
         return o.v;
       };
-      bf16x8 fa[F], fb[F];
+      bf16x8 fa[MF], fb[NF];
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
-        fa[i] = read(lds[0], wm * 64, i);
-        fb[i] = read(lds[1], wn * 64, i);
-      }
+      for (int j = 0; j < NF; ++j) fb[j] = read(lds[1], wn * 32, j);
 #pragma unroll
-      for (int i = 0; i < F; ++i)
+      for (int i = 0; i < MF; ++i) fa[i] = read(lds[0], wm * 64, i);
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
     }
   }
@@ -523,19 +526,16 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
   };
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < F; ++i) {
+  for (int i = 0; i < MF; ++i) {
 #pragma unroll
-    for (int j = 0; j < F; ++j) *at(i, wm * 16 + l15, wn * 16 + j * 4 + g4) = acc[i][j];
+    for (int j = 0; j < NF; ++j) *at(i, wm * 16 + l15, wn * 8 + j * 4 + g4) = acc[i][j];
     wait_lgkm0();
     asm volatile("s_barrier" ::: "memory");
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = u * 16 + (tid >> 4), n = w.n0 + chunk * 8;
-      const int64_t m = w.m0 + (r >> 4) * 64 + i * 16 + (r & 15);
-      if (m < a.M && n < a.N)
-        finish_eight<CEP_IDENTITY>(a.f, (int64_t)w.g * a.M + m, n, *at(i, r, 2 * chunk),
-                                   *at(i, r, 2 * chunk + 1), Loaded{}, Column{});
-    }
+    const int r = tid >> 4, n = w.n0 + chunk * 8;
+    const int64_t m = w.m0 + (r >> 4) * 64 + i * 16 + (r & 15);
+    if (m < a.M && n < a.N)
+      finish_eight<CEP_IDENTITY>(a.f, (int64_t)w.g * a.M + m, n, *at(i, r, 2 * chunk),
+                                 *at(i, r, 2 * chunk + 1), Loaded{}, Column{});
   }
 }
 
@@ -543,7 +543,7 @@ __global__ __launch_bounds__(256, 3) void k_linear_wgrad_few(WgradArgs a) {
 // sum over, dx, the other weights, so that the longest tiles come first and the tiles of
 // one fill the compute units that the others' last round leaves.
 template <int HALF, int WM, int WN, bool STAGED>
-__global__ __launch_bounds__(WM * WN * 64, 2) void k_linear_grads(LinearArgs dx, WgradArgs dw) {
+__global__ __launch_bounds__(WM * WN * 64, HALF == 64 ? 4 : 2) void k_linear_grads(LinearArgs dx, WgradArgs dw) {
   constexpr int SIZE = 2 * HALF;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[HALF * 1024];
   const int x = blockIdx.x & 7, room = wgrad_room<SIZE>(dw);
@@ -805,8 +805,8 @@ Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
 //   256-wide: 12 + 1.4 a step, a round of 256; groups of unlike sizes a tenth more
 //   128-wide, more than a round: 6 + 1.3 a step, a round of 512 (32 groups of 34 rows 262,
 //     16 of 128 rows 175)
-//   few: 5 + 2 a step, a round of 768, three a compute unit (the same two 154 and 110, 16
-//     of 256 rows 147, eight of 512 109, eight of 1024 198); two of them 1.5 a step, one 1
+//   few: 5 + 2 a step, a round of 768, three a compute unit (the same two 147 and 108, 16
+//     of 256 rows 143, eight of 512 109, eight of 1024 198); two of them 1.5 a step, one 1
 constexpr int kFewTile = 2;
 Plan wgrad_plan(const cep_linear_desc *d) {
   const int g = std::max(d->n_groups, 1);
@@ -899,7 +899,7 @@ void launch_kind(const LinearArgs &a, int64_t items, hipStream_t s) {
   const int64_t blocks = TILE == 0 && items > kUnits ? items + 2 * kUnits : items;
   const dim3 grid((unsigned)((blocks + 7) / 8 * 8));
   if constexpr (TILE == 0) hipLaunchKernelGGL((k_linear_256<B_K, STAGED, ACT>), grid, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((k_linear_128<B_K, STAGED, ACT>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_linear_128<B_K, STAGED, ACT>), grid, dim3(512), 0, s, a);
 }
 template <int TILE, bool B_K>
 void launch_tiles(const LinearArgs &a, int64_t items, hipStream_t s) {
@@ -936,9 +936,9 @@ void launch_grads(int tile, const LinearArgs &dx, WgradArgs dw, hipStream_t s) {
   const int64_t items = most_tiles(dx.groups, kTile[tile]) * ((dx.N + kTile[tile] - 1) / kTile[tile]);
   const int64_t room = (dense_tiles(tile, dw.M, dw.N) + 7) / 8 * std::max(dw.groups.n, 1);
   const dim3 grid((unsigned)(((items + 7) / 8 + room) * 8));
-  auto *k = tile == 0 ? k_linear_grads<128, 2, 4, false> : k_linear_grads<64, 2, 2, false>;
-  if (dx.f.res) k = tile == 0 ? k_linear_grads<128, 2, 4, true> : k_linear_grads<64, 2, 2, true>;
-  hipLaunchKernelGGL(k, grid, dim3(tile == 0 ? 512 : 256), 0, s, dx, dw);
+  auto *k = tile == 0 ? k_linear_grads<128, 2, 4, false> : k_linear_grads<64, 2, 4, false>;
+  if (dx.f.res) k = tile == 0 ? k_linear_grads<128, 2, 4, true> : k_linear_grads<64, 2, 4, true>;
+  hipLaunchKernelGGL(k, grid, dim3(512), 0, s, dx, dw);
 }
 
 // A product over the groups' rows: A [rows][K], W as B, the epilogue's output [rows][N].
@@ -1086,14 +1086,14 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
                         f, part, s);
   if (dw && p.tile == kFewTile) {
     const int64_t items = dense_tiles(1, D, N);
-    hipLaunchKernelGGL(k_linear_wgrad_few, dim3((unsigned)((items + 7) / 8 * 8 * n_groups)), dim3(256),
+    hipLaunchKernelGGL(k_linear_wgrad_few, dim3((unsigned)((items + 7) / 8 * 8 * n_groups)), dim3(512),
                        0, s, a);
   } else if (dw) {
     const int64_t items = dense_tiles(p.tile, D, N) * p.splits;
     const dim3 grid((unsigned)((items + 7) / 8 * 8 * n_groups));
     if (p.tile == 0)
       hipLaunchKernelGGL((k_linear_wgrad<128, 2, 4>), grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((k_linear_wgrad<64, 2, 2>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((k_linear_wgrad<64, 2, 4>), grid, dim3(512), 0, s, a);
     if (p.splits > 1) launch_finish(part, p.splits, Groups{nullptr, 0, D}, a.f, D, s);
   }
   return launched(fn);

@@ -235,7 +235,9 @@ LINEARS = [
     (3001, 1544, 3080, 0), (2047, 1032, 4104, 0),                   # 256-wide tiles
     # groups: rows by the list, the first below the offsets' start
     (60, 264, 136, [0, 5, 0, 1, 17, 33, 0]), (24, 1024, 264, [3, 3, 3, 3, 3, 3, 3, 3]),
-    (100, 136, 520, [90, 2, 0, 1]), (8, 264, 136, [0, 3, 0, 0, 4, 0]), (3, 8, 264, [0, 0, 3]), (70, 512, 256, [0, 0, 0]), (64, 8, 8, [64]),
+    (100, 136, 520, [90, 2, 0, 1]), (8, 264, 136, [0, 3, 0, 0, 4, 0]), (3, 8, 264, [0, 0, 3]),
+    (70, 512, 256, [0, 0, 0]), (64, 8, 8, [64]),
+    (80, 1032, 264, [10] * 8), (88, 1032, 264, [11] * 8),           # streamed, and past it
     (300, 264, 392, [1, 127, 0, 128, 12]), (900, 520, 264, [257, 0, 300, 1, 255, 64]),
     (2500, 264, 1032, [1300, 0, 5, 900, 200, 3]), (130, 72, 264, [1] * 130),
     (1500, 40, 264, [5] * 300), (5000, 1024, 1544, [1027, 0, 1500, 2049, 100, 200]),

@@ -634,10 +634,10 @@ __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
   const int n = (int)blockIdx.y * kDzCols + lane * 8;
   const int row0 = blockIdx.x * ROWS;
   const int end = min(row0 + ROWS, a.groups.rows);
-  int from = row0, to = end;  // the rows of some group
+  int from = row0, to = end;  // the rows of some group, inside the block's whatever the offsets hold
   if (a.groups.n) {
-    from = max(from, a.groups.offsets[0]);
-    to = min(to, a.groups.offsets[a.groups.n]);
+    from = min(max(a.groups.offsets[0], row0), end);
+    to = min(max(a.groups.offsets[a.groups.n], from), end);
   }
   if (n < a.N) {
     for (int r = rl; r < ROWS; r += 8) {
@@ -689,7 +689,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
   }
   const bool whole = gridDim.x == 1;
   int next = 0;  // the first line not written yet, of one block
-  for (int r = max(from - row0, 0); r < to - row0;) {
+  for (int r = from - row0; r < to - row0;) {
     const int g = group[r];
     if (g >= a.groups.n) break;
     float sum = 0.f;

@@ -512,6 +512,57 @@ def test_linear_with_broken_offsets_stays_inside_its_arrays(off):
     assert (ws[need:] == 7).all()
 
 
+LOW, HIGH = -(1 << 31), (1 << 31) - 1  # of an offset
+BROKEN = {
+    "last lowest": lambda n, R: [*range(0, n)] + [LOW],
+    "last near the lowest": lambda n, R: [0] + [R] * (n - 1) + [LOW + R // 2],
+    "first lowest": lambda n, R: [LOW] + [R // n * i for i in range(1, n + 1)],
+    "all highest": lambda n, R: [HIGH] * (n + 1),
+    "last highest": lambda n, R: [0] * n + [HIGH],
+    "ends apart": lambda n, R: [HIGH] + [R // 2] * (n - 1) + [LOW],
+    "all rows in every second group": lambda n, R: [i % 2 * R for i in range(n + 1)],
+    "descending": lambda n, R: [R - R // n * i for i in range(n + 1)],
+    "between the ends": lambda n, R: [(LOW, HIGH, R // 2, -1, R)[i * i % 5] for i in range(n + 1)],
+}
+
+
+@pytest.mark.parametrize("rows,d,N,n", [
+    (40, 72, 136, 3), (7, 72, 136, 3),          # streamed; one block of dz
+    (130, 264, 136, 130),                       # streamed, more than 64 groups
+    (900, 520, 264, 6), (2500, 264, 1032, 70),  # 128-wide tiles
+    (8000, 2056, 2056, 6),                      # 256-wide ones, the last in quarters
+    (4096, 520, 4104, 2), (9000, 2056, 1544, 5)])  # dx and dW in one launch
+@pytest.mark.parametrize("kind", BROKEN)
+def test_linear_with_offsets_of_any_number_stays_inside_its_arrays(rows, d, N, n, kind):
+    off = BROKEN[kind](n, rows)
+    assert len(off) == n + 1 and min(off) >= LOW and max(off) <= HIGH
+    off = torch.tensor(off, dtype=torch.int32, device="cuda")
+    g = _gen(1)
+    guarded = {}
+
+    def mk(name, *shape, dtype=torch.bfloat16):  # with 64 KB before and behind it
+        size, pad = int(np.prod(shape)), 65536 // dtype.itemsize
+        buf = guarded[name] = torch.full((size + 2 * pad,), 7, dtype=dtype, device="cuda")
+        return buf[pad:pad + size].view(shape)
+
+    y, pre = mk("y", rows, N), mk("preact", rows, N, dtype=torch.float32)
+    dx, dm = mk("dx", rows, d), mk("dmul", rows, N)
+    dw, db = mk("dw", n, d, N), mk("dbias", n, N, dtype=torch.float32)
+    x, w, mul, dy = _randn(g, rows, d), _randn(g, n, d, N), _randn(g, rows, N), _randn(g, rows, N)
+    desc = cep.make_linear(rows=rows, d_in=d, d_out=N, n_groups=n, act=cep.CEP_SILU, y_dtype=BF16,
+                           dx_dtype=BF16, dw_dtype=BF16)
+    ws = mk("workspace", cep.cep_linear_workspace(desc, True), dtype=torch.uint8)
+    cep.cep_linear(desc, x, w, y, ws, mul=mul, offsets=off, preact=pre)
+    out = dict(dx=dx, dw=dw, dbias=db, dmul=dm)
+    cep.cep_linear_backward(desc, dy, x, w, ws, preact=pre, mul=mul, offsets=off, **out)
+    for name, t in out.items():  # and each alone
+        cep.cep_linear_backward(desc, dy, x, w, ws, preact=pre, mul=mul, offsets=off, **{name: t})
+    torch.cuda.synchronize()
+    for name, buf in guarded.items():
+        pad = 65536 // buf.element_size()
+        assert (buf[:pad] == 7).all() and (buf[-pad:] == 7).all(), name
+
+
 # ------------------------------------------------------------ gate gradient
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 256, 8), (5, 64, 8), (9, 7, 7), (70, 160, 8),

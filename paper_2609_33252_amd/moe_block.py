@@ -137,7 +137,9 @@ class MoEBlock:
         pre = torch.empty(T, 2, self.d_shared, device=y.device) if train else None
         cep.cep_gated_ffn(ffn, y, *self.shared, self.shared_y, self._ffn_space(ffn, train),
                           preact=pre, stream=s)
-        self.saved = (residual.clone(), y.clone(), pre, logits) if train else None
+        self.saved = None
+        if train:
+            self.saved = residual.clone(), y.clone(), pre, logits, self.ids[:T].clone()
         routed = self.routed[0, :T]
         routed.zero_()
         plan = self.plan.cpu()
@@ -167,7 +169,7 @@ class MoEBlock:
         they leave those paths out, as one addend of the gradients."""
         if self.saved is None:
             raise ValueError("backward without a forward(train=True) before it")
-        residual, y, pre, _ = self.saved
+        residual, y, pre, *_ = self.saved
         T, d, s = y.shape[0], self.d, torch.cuda.current_stream()
         BF16 = (torch.bfloat16,)
         _expect("d_out", d_out, y.device, BF16, (T, d))
@@ -197,11 +199,11 @@ class MoEBlock:
         ``backward``'s d_y) and of the gate's weight (float32 [d][n_experts])."""
         if self.saved is None:
             raise ValueError("gate_backward without a forward(train=True) before it")
-        _, y, _, logits = self.saved
+        _, y, _, logits, ids = self.saved
         T = y.shape[0]
         _expect("d_topk_w", d_topk_w, y.device, (torch.float32,), (T, self.top_k))
         d_logits = torch.empty_like(logits)
-        cep.cep_gate_topk_backward(cep.make_gate(rows=T, **self.gate_args), logits, self.ids,
+        cep.cep_gate_topk_backward(cep.make_gate(rows=T, **self.gate_args), logits, ids,
                                    d_topk_w, d_logits, stream=torch.cuda.current_stream())
         return d_logits @ self.gate.T, y.float().T @ d_logits
 

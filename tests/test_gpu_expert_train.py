@@ -963,3 +963,31 @@ def test_routed_experts_match_differences(seed):
         up[i], down[i] = at[i] + h * v, at[i] - h * v
         slope = float(f(*up) - f(*down)) / (2 * h)
         assert abs(slope / float(grad.double().norm()) - 1) < 4 * U16, i
+
+
+def _small_block(seed, T, d=256, I=128, E=8, k=3):
+    """A block with its experts in both forms; inputs as of the block before."""
+    from paper_2609_33252_amd import moe_block
+    g = _gen(seed)
+    n = lambda *s, std=0.08: _randn(g, *s, std=std)
+    experts = [n(E, d, I), n(E, d, I), n(E, I, d)]
+    b = moe_block.MoEBlock(d=d, d_ff=I, d_shared=200, n_experts=E, top_k=k, n_ranks=1, rank=0,
+                           max_tokens=T, norm=1 + n(d).float(), gate=n(d, E).float(),
+                           shared=(n(d, 200), n(d, 200), n(200, d)),
+                           experts=cep.make_weights(*experts), w_dtype=cep.CEP_BF16)
+    routed = moe_block.RoutedExperts(top_k=k, w_gate=experts[0], w_up=experts[1],
+                                     w_down=experts[2])
+    return g, b, routed, n(T, d, std=1.0), n(T, d, std=1.0)
+
+
+def test_gate_gradient_is_of_the_pass_that_was_saved():
+    """The buffers that a pass leaves its choice in may change before the backward pass."""
+    T = 9
+    g, b, _, x, res = _small_block(21, T)
+    b.forward(x, res, train=True)
+    d_w = _randn(g, T, 3, dtype=torch.float32)
+    want = b.gate_backward(d_w)
+    b.ids.copy_((b.ids + 1) % 8)
+    got = b.gate_backward(d_w)
+    assert all(torch.equal(a, c) for a, c in zip(got, want))
+    b.close()

@@ -991,3 +991,70 @@ def test_gate_gradient_is_of_the_pass_that_was_saved():
     got = b.gate_backward(d_w)
     assert all(torch.equal(a, c) for a, c in zip(got, want))
     b.close()
+
+
+@pytest.mark.parametrize("T", [1, 9, 300])
+def test_gate_weight_gradient_from_given_coefficients(T):
+    """MoEBlock.gate_backward alone: from the d_topk_w that it gets.  A logit's gradient is
+    within 2^-18 of the row's sum of |d_topk_w| (as in test_gate_gradient), and the float32
+    products within 2^-12 of the sum of magnitudes."""
+    g, b, _, x, res = _small_block(T + 30, T)
+    b.forward(x, res, train=True)
+    d_w = _randn(g, T, 3, dtype=torch.float32)
+    d_y, d_gate = b.gate_backward(d_w)
+    y, logits = b.y[:T].double(), b.y[:T].float() @ b.gate
+    dl = torch.from_numpy(R.gate_grad(logits.cpu().numpy(), b.ids[:T].cpu().numpy(),
+                                      d_w.cpu().numpy(), normalize=True)).cuda()
+    e = (2.0 ** -18 * d_w.double().abs().sum(1, keepdim=True)).expand_as(dl)
+    across = lambda a, c: a.T.contiguous() @ c
+    want, tol = across(y, dl), across(y.abs(), e + 2.0 ** -12 * dl.abs())
+    assert tol.norm() < 2.0 ** -6 * want.norm()  # a check that can fail
+    _close(d_gate, want, tol, "d_gate")
+    gate = b.gate.double().T.contiguous()
+    want, tol = dl @ gate, (e + 2.0 ** -12 * dl.abs()) @ gate.abs()
+    assert tol.norm() < 2.0 ** -6 * want.norm()
+    _close(d_y, want, tol, "d_y")
+    b.close()
+
+
+@pytest.mark.parametrize("T", [1, 9, 300])
+def test_gate_weight_gradient_through_the_routed_experts(T):
+    """From d_out through the experts' rows to the gate's weight, against float64 from the
+    block's own y on.  A coefficient's gradient is <d_out, row>; on the way to the row u, h
+    and the row itself are rounded to bf16, each by a part of at most 2^-8 / 3^.5 (r.m.s.)
+    with a sign of its own, so that its variance is the sum of the squares of those parts
+    times the derivatives.  Six deviations, of variances carried on through the choice's
+    Jacobian and the product with y, are taken for a gradient."""
+    d, I, E, k = 256, 128, 8, 3
+    g, b, routed, x, res = _small_block(T + 40, T)
+    b.forward(x, res, train=True)
+    y, ids, w = b.y[:T], b.ids[:T], b.w[:T]
+    dout = _randn(g, T, d)
+    routed.forward(y, ids, w, train=True)
+    d_w = routed.backward(dout)[1]
+    d_gate = b.gate_backward(d_w)[1]
+    part = 2.0 ** -8 / 3 ** 0.5
+    yd, dd = y.double(), dout.double()
+    rows, var = (torch.empty(T, k, dtype=torch.float64, device="cuda") for _ in range(2))
+    for t in range(T):
+        for j, e in enumerate(ids[t].tolist()):
+            z, u = (yd[t] @ m[e].double() for m in (routed.w_gate, routed.w_up))
+            h, wd = z * torch.sigmoid(z) * u, routed.w_down[e].double()
+            row = h @ wd
+            rows[t, j] = (dd[t] * row).sum()
+            var[t, j] = part ** 2 * ((dd[t] * row).square().sum()
+                                     + 2 * ((wd @ dd[t]) * h).square().sum())
+    _close(d_w, rows, 6 * var.sqrt() + SUM32 * rows.abs(), "d_w")
+    logits = yd @ b.gate.double()
+    c = torch.softmax(logits.gather(1, ids.long()), 1)
+    jac = torch.diag_embed(c) - c[:, :, None] * c[:, None, :]
+    to_experts = lambda v: torch.zeros(T, E, dtype=torch.float64, device="cuda").scatter(
+        1, ids.long(), v)
+    dl = to_experts((jac * rows[:, None, :]).sum(2))
+    vl = to_experts((jac.square() * var[:, None, :]).sum(2))
+    across = lambda a, c: a.T.contiguous() @ c
+    want = across(yd, dl)
+    tol = 6 * across(yd.square(), vl).sqrt() + 2.0 ** -12 * across(yd.abs(), dl.abs())
+    assert tol.norm() < 2.0 ** -4 * want.norm()  # a check that can fail
+    _close(d_gate, want, tol, "d_gate")
+    b.close()

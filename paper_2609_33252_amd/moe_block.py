@@ -30,6 +30,7 @@ import torch
 from . import cep
 
 EPS = 1e-6
+MAX_ROWS = 1 << 21  # of an operator's descriptor
 
 
 def _expect(name, t, device, dtypes, shape, dense=True):
@@ -230,6 +231,10 @@ class RoutedExperts:
         _expect("w_gate", w_gate, w_gate.device, BF16, (E, d, d_ff))
         _expect("w_up", w_up, w_gate.device, BF16, (E, d, d_ff))
         _expect("w_down", w_down, w_gate.device, BF16, (E, d_ff, d))
+        if not 1 <= E <= 1024 or not 1 <= top_k <= 16:
+            raise ValueError("RoutedExperts holds 1 to 1024 experts, top_k of 1 to 16")
+        if any(n % 8 or not 8 <= n <= 32768 for n in (d, d_ff)):
+            raise ValueError("d and d_ff must be multiples of 8, up to 32768")
         self.E, self.d, self.d_ff, self.top_k = E, d, d_ff, top_k
         self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
         self.saved = None  # of the last forward pass, if that was a training one
@@ -257,6 +262,8 @@ class RoutedExperts:
         _expect("y", y, dev, (torch.bfloat16,), (T, d))
         _expect("ids", ids, dev, (torch.int32,), (T, k))
         _expect("w", w, dev, (torch.float32,), (T, k))
+        if T * k > MAX_ROWS:
+            raise ValueError(f"{T} tokens of {k} slots: the products take up to 2^21 rows")
         with torch.cuda.device(dev):
             return self._forward(y, ids, w, train)
 

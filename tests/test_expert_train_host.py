@@ -175,6 +175,29 @@ def test_linear_refuses_outputs_over_its_inputs():
     _refused(cep.CEP_EINVAL, b, _linear(), y, x, w, BIG, dx=x, dw=PTR + 4096)
 
 
+# --------------------------------------------------------- routed experts
+
+def _routed(E=2, d=8, d_ff=16, top_k=2):
+    from paper_2609_33252_amd import moe_block
+    w = [torch.zeros(E, *n, dtype=torch.bfloat16) for n in ((d, d_ff), (d, d_ff), (d_ff, d))]
+    return moe_block.RoutedExperts(top_k=top_k, w_gate=w[0], w_up=w[1], w_down=w[2])
+
+
+@pytest.mark.parametrize("bad", [dict(E=0), dict(E=1025), dict(d=12), dict(d=0), dict(d=32776),
+                                 dict(d_ff=4), dict(d_ff=20), dict(top_k=0), dict(top_k=17)])
+def test_routed_experts_refuse_sizes_before_a_pass(bad):
+    with pytest.raises(ValueError):
+        _routed(**bad)
+
+
+@pytest.mark.parametrize("T,k", [((1 << 17) + 1, 16), ((1 << 20) + 1, 2), ((1 << 21) + 1, 1)])
+def test_routed_experts_refuse_more_rows_than_the_products_take(T, k, monkeypatch):
+    r = _routed(top_k=k)
+    monkeypatch.setattr(r, "_forward", lambda *a: pytest.fail("launched"))
+    with pytest.raises(ValueError, match="2.21 rows"):
+        r.forward(torch.zeros(T, 8, dtype=torch.bfloat16), torch.zeros(T, k, dtype=torch.int32),
+                  torch.zeros(T, k))
+
 # ------------------------------------------------------------ gate gradient
 
 def _gate(**kw):

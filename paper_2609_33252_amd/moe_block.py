@@ -238,6 +238,7 @@ class RoutedExperts:
         self.E, self.d, self.d_ff, self.top_k = E, d, d_ff, top_k
         self.w_gate, self.w_up, self.w_down = w_gate, w_up, w_down
         self.saved = None  # of the last forward pass, if that was a training one
+        self.bad_ids = None  # of the last forward pass
 
     def _buf(self, *shape, dtype=torch.bfloat16):
         return torch.empty(*shape, dtype=dtype, device=self.w_gate.device)
@@ -257,7 +258,10 @@ class RoutedExperts:
 
     def forward(self, y, ids, w, train=False):
         """y [T][d] bf16; ids int32 and w float32 [T][top_k] as cep_gate_topk leaves
-        them (-1: empty slot).  Returns float32 [T][d], each token's weighted sum."""
+        them (-1: empty slot).  Returns float32 [T][d], each token's weighted sum.
+        Raises for ids outside [-1, n_experts), whose number is also left in
+        ``bad_ids`` (int32 [1] on the device): a pass that is captured into a graph
+        cannot raise, and its replays count such slots as empty."""
         T, k, d, dev = y.shape[0], self.top_k, self.d, self.w_gate.device
         _expect("y", y, dev, (torch.bfloat16,), (T, d))
         _expect("ids", ids, dev, (torch.int32,), (T, k))
@@ -276,6 +280,12 @@ class RoutedExperts:
         cep.cep_expert_sort(sort, ids, plan, pair, place,
                             self._space(cep.cep_expert_sort_workspace(sort)), x=y, out_x=x,
                             stream=s)
+        self.bad_ids, count = plan[self.E + 1:], None
+        if not torch.cuda.is_current_stream_capturing():
+            # the host waits for the sort alone, with the products already enqueued
+            count, sorted_ = torch.empty(1, dtype=torch.int32, pin_memory=True), torch.cuda.Event()
+            count.copy_(self.bad_ids, non_blocking=True)
+            sorted_.record(s)
         up, gate = self._linear(P, d, I), self._linear(P, d, I, cep.CEP_SILU)
         down = self._linear(P, I, d)
         ws = self._space(max(cep.cep_linear_workspace(q) for q in (up, gate, down)))
@@ -287,7 +297,13 @@ class RoutedExperts:
         total = self._buf(T, d, dtype=torch.float32)
         cep.cep_expert_unsort(self._unsort(T, cep.CEP_BF16, cep.CEP_F32), out, place, total, w=w,
                               stream=s)
-        self.saved = (plan, place, w.clone(), x, u, h, pre, out) if train else None
+        self.saved = None
+        if count is not None:
+            sorted_.synchronize()
+            if int(count):
+                raise RuntimeError(f"{int(count)} expert ids outside [-1, {self.E})")
+        if train:
+            self.saved = plan, place, w.clone(), x, u, h, pre, out
         return total
 
     def backward(self, d_total):

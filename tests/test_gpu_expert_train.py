@@ -1058,3 +1058,37 @@ def test_gate_weight_gradient_through_the_routed_experts(T):
     assert tol.norm() < 2.0 ** -4 * want.norm()  # a check that can fail
     _close(d_gate, want, tol, "d_gate")
     b.close()
+
+
+def test_routed_experts_raise_for_ids_of_no_expert():
+    from paper_2609_33252_amd import moe_block
+    T, d, I, E, k = 40, 64, 40, 5, 2
+    g = _gen(60)
+    r = moe_block.RoutedExperts(top_k=k, w_gate=_randn(g, E, d, I), w_up=_randn(g, E, d, I),
+                                w_down=_randn(g, E, I, d))
+    y, c = _randn(g, T, d), torch.rand(T, k, device="cuda", generator=g)
+    good = torch.randint(-1, E, (T, k), device="cuda", generator=g).int()
+    want = r.forward(y, good, c, train=True)
+    assert int(r.bad_ids) == 0 and r.saved is not None
+    for wrong in (E, -2, 2 ** 31 - 1, -2 ** 31):
+        ids = good.clone()
+        ids[3, 1] = ids[7, 0] = wrong
+        with pytest.raises(RuntimeError, match="2 expert ids"):
+            r.forward(y, ids, c, train=True)
+        assert int(r.bad_ids) == 2
+        with pytest.raises(ValueError):
+            r.backward(want)  # that pass kept nothing
+    # captured: the slots are empty, and counted
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = r.forward(y, ids, c)
+    bad = r.bad_ids
+    empty = torch.where(ids == wrong, -1, ids).int()
+    want = r.forward(y, empty, c)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and int(bad) == 2
+    ids.copy_(empty)
+    graph.replay()
+    assert torch.equal(out, want) and int(bad) == 0

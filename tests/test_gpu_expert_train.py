@@ -1092,3 +1092,35 @@ def test_routed_experts_raise_for_ids_of_no_expert():
     ids.copy_(empty)
     graph.replay()
     assert torch.equal(out, want) and int(bad) == 0
+
+
+def test_routed_experts_sum_the_gradient_of_y_in_float32():
+    """Whole numbers that every rounding to bf16 of rows and products keeps: z is 64, where
+    SiLU is its argument and its slope 1.  The gradient of y, a sum of sums beyond eight
+    bits, has to be exact."""
+    from paper_2609_33252_amd import moe_block
+    T, d, I, E, k = 40, 16, 24, 4, 2
+    g = _gen(61)
+    whole = lambda lo, hi, *s: torch.randint(lo, hi + 1, s, device="cuda", generator=g).bfloat16()
+    wg, wu, wd = whole(-7, 7, E, d, I), whole(-7, 7, E, d, I), whole(-1, 1, E, I, d)
+    wg[:, 0], wu[:, 0] = 64, whole(1, 3, E, I)
+    y = torch.zeros(T, d, device="cuda").bfloat16()
+    y[:, 0] = 1
+    ids = torch.rand(T, E, device="cuda", generator=g).topk(k, -1)[1].int()
+    c = torch.tensor([1.0, 0.5], device="cuda").expand(T, k).contiguous()
+    dt = 2 * whole(-2, 2, T, d)
+    r = moe_block.RoutedExperts(top_k=k, w_gate=wg, w_up=wu, w_down=wd)
+    r.forward(y, ids, c, train=True)
+    d_y = r.backward(dt)[0]
+    want = torch.zeros(T, d, dtype=torch.float64, device="cuda")
+    parts = []
+    for t in range(T):
+        for j, e in enumerate(ids[t].tolist()):
+            dh = wd[e].double() @ (c[t, j].double() * dt[t].double())
+            dz, du = dh * wu[e, 0].double(), 64 * dh
+            assert torch.equal(dz, dz.bfloat16().double()) and torch.equal(du, du.bfloat16().double())
+            parts += [wg[e].double() @ dz, wu[e].double() @ du]
+            want[t] += parts[-1] + parts[-2]
+    parts = torch.stack(parts)
+    assert not torch.equal(parts, parts.bfloat16().double()) and float(parts.abs().max()) < 2 ** 24
+    assert torch.equal(d_y.double(), want)

@@ -7,7 +7,7 @@
 // compared as a whole.  More take two: each block's counts and every pair's place
 // among its expert's in the block (k_sort_count), and the places and rows
 // (k_sort_rows), a wave a token, which reads its row once and writes it to each of its
-// places.  It sums the blocks' counts itself, many of them a launch between (k_sort_scan).
+// places.  It sums the blocks' counts itself, those of many blocks a launch between (k_sort_scan).
 // Bound by HBM, mostly the sorted rows' writes: 8191 tokens of 8 KB, eight places each,
 // 116 us for 604 MB, 5.2 TB/s (nontemporal stores: 17 % slower).
 #include "block_ops.h"
@@ -23,10 +23,13 @@ constexpr int kMaxSortExperts = 1024;
 constexpr int kFewPairs = 4096;
 constexpr int kSortPairs = 1024;    // pairs of a k_sort_count block, a quarter a wave
 constexpr int kSortTokens = 4;      // tokens of a k_sort_rows block, one a wave
-// Counts (blocks times buckets) up to which k_sort_rows sums them itself, and buckets.
-// A scan is a launch of 4.6 us; the sums cost the rows 1.6 us with 1040 counts, 2.9 with
-// 2080 and 3864, 6.6 with 4160 and 6.7 with 7567.
-constexpr int kFusedSums = 4096, kFusedCounts = 512;
+// Blocks whose counts k_sort_rows sums itself, a thread 256 buckets apart, and buckets.  A
+// scan is a launch, nearly the same for any blocks; the sums are a walk over them in every
+// workgroup, twice as long past 256 buckets (8 a token, 256-byte rows, us with the sums and
+// with the scan: eight experts 8 blocks 8.6, 9.5; 16 9.9, 10.3; 24 11.4, 11.1; 64 20.2, 15.2;
+// 256 118, 33.  64 experts 16 blocks 11.2, 11.4; 24 13.2, 12.1.  300 experts 8 blocks 12.1,
+// 13.0; 12 14.3, 13.5)
+constexpr int kFusedBlocks = 16, kFusedCounts = 512;
 
 struct SortArgs {
   const int32_t *ids;  // [rows][k]
@@ -384,7 +387,7 @@ CEP_API int cep_expert_sort(const cep_expert_sort_desc *d, const int32_t *topk_i
   } else {
     hipLaunchKernelGGL(k_sort_count, dim3(blocks), dim3(256), 0, s, a);
     const dim3 grid((d->rows + kSortTokens - 1) / kSortTokens), threads(64 * kSortTokens);
-    if (E < kFusedCounts && (int64_t)blocks * (E + 1) <= kFusedSums) {
+    if (E < kFusedCounts && blocks * (E / 256 + 1) <= kFusedBlocks) {
       hipLaunchKernelGGL(k_sort_rows<false>, grid, threads, 0, s, a);
     } else {
       hipLaunchKernelGGL(k_sort_scan, dim3(E / 4 + 1), dim3(256), 0, s, a);

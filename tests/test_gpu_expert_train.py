@@ -127,6 +127,15 @@ def test_sort(T, k, E, row, pad, kind):
         assert (ox[n if copy else 0:] == 5).all()
 
 
+@pytest.mark.parametrize("T,k,E", [
+    # blocks' counts summed by the rows' workgroups, up to 16 blocks (8 past 256 buckets), and
+    # one block more
+    (1024, 16, 8), (1025, 16, 8), (1024, 16, 255), (1025, 16, 255), (512, 16, 256), (513, 16, 256),
+    (512, 16, 511), (513, 16, 511), (512, 16, 512), (16384, 1, 1), (16385, 1, 1), (60000, 8, 3)])
+def test_sort_with_the_counts_of_few_and_many_blocks(T, k, E):
+    test_sort(T, k, E, 40, 0, "any")
+
+
 # ------------------------------------------------------------------- back
 
 UNSORTS = [

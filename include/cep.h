@@ -547,8 +547,8 @@ typedef struct {
  * summed in float32 in slot order and rounded once.  ys [sorted_rows][d]; place
  * [rows][top_k] as cep_expert_sort writes it: a slot with a place outside [0,
  * sorted_rows) is empty, and its weight not used; w [rows][top_k] float32 (NULL:
- * ones); residual (NULL: none; may be y itself if types and strides agree).  A
- * token without a filled slot gets its residual, or 0. */
+ * ones); residual (NULL: none; may be y itself if types and strides agree).  y is
+ * no part of ys.  A token without a filled slot gets its residual, or 0. */
 int cep_expert_unsort(const cep_expert_unsort_desc *desc, const void *ys, const int32_t *place,
                       const float *w, const void *residual, void *y, hipStream_t s);
 
@@ -556,8 +556,8 @@ int cep_expert_unsort(const cep_expert_unsort_desc *desc, const void *ys, const 
  * (ys_dtype): row place[t][j] gets w[t][j] dy[t], rows that are no slot's place are
  * left as they are; dw [rows][top_k] float32: the product of dy[t] and ys[place], 0
  * for an empty slot.  dys or dw may be NULL, ys too without dw.  dys may be ys
- * itself.  The residual's gradient is dy.  A sorted row is the place of at most one
- * pair. */
+ * itself, and is no part of dy.  The residual's gradient is dy.  A sorted row is the
+ * place of at most one pair. */
 int cep_expert_unsort_backward(const cep_expert_unsort_desc *desc, const void *dy, const void *ys,
                                const int32_t *place, const float *w, void *dys, float *dw,
                                hipStream_t s);
@@ -587,8 +587,8 @@ typedef struct {
  * x [rows][d_in] bf16; w [d_in][d_out] bf16 (the math orientation of cep_weights,
  * read as it is); bias [d_out] float32, mul [rows][d_out] bf16, residual
  * [rows][d_out] (res_dtype; may be y itself if types and strides agree), each may
- * be NULL.  y (y_dtype) and preact may not overlap x or each other.  preact (NULL: not kept) gets z, float32
- * [rows][d_out], for cep_linear_backward.
+ * be NULL.  y (y_dtype) overlaps neither x, w nor bias.  preact (NULL: not kept) gets
+ * z, float32 [rows][d_out], for cep_linear_backward, and overlaps no other array.
  * With groups, w is [n_groups][d_in][d_out] and bias [n_groups][d_out], and offsets,
  * device int32 [n_groups + 1], ascending within 0..rows, gives the rows
  * [offsets[g], offsets[g + 1]) of group g, which may be none; rows before the first
@@ -610,9 +610,10 @@ int cep_linear(const cep_linear_desc *desc, const void *x, const void *w, const 
  * dx (dx_dtype), dw (dw_dtype, layout of w), dbias (float32, layout of bias) and
  * dmul (bf16, layout of mul) are written, not added to, and each may be NULL; so may
  * w without dx and x without dw.  dx_add (dx_dtype, NULL: none, may be dx itself)
- * joins dx, which overlaps neither dy nor x.  A group without rows gets zeros in dw and dbias.  dz is rounded to bf16
- * once, for the products that follow (dbias sums it before that).  The residual's
- * gradient is dy. */
+ * joins dx.  dx, dw and dbias overlap neither dy, x nor w, dbias neither mul nor
+ * preact.  A group without rows gets zeros in dw and dbias.  dz is rounded to bf16 once,
+ * for the products that follow (dbias sums it before that).  The residual's gradient is
+ * dy. */
 int cep_linear_backward(const cep_linear_desc *desc, const void *dy, const void *x, const void *w,
                         const void *mul, const int32_t *offsets, const float *preact,
                         const void *dx_add, void *dx, void *dw, float *dbias, void *dmul,

@@ -377,6 +377,7 @@ CEP_API int cep_expert_sort(const cep_expert_sort_desc *d, const int32_t *topk_i
   if (!workspace || !aligned(workspace, 4) || workspace_bytes < cep_expert_sort_workspace(d))
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_expert_sort_workspace(d));
+  if (d->rows && x && x == out_x) return refuse(CEP_EINVAL, "%s: out_x overlaps x", fn);
   const int blocks = sort_blocks(d), E = d->n_experts;
   int32_t *counts = (int32_t *)workspace;
   const SortArgs a{topk_id, (const char *)x, d->ld_x ? d->ld_x : d->row_bytes, d->row_bytes, plan,

@@ -215,6 +215,7 @@ CEP_API int cep_expert_unsort(const cep_expert_unsort_desc *d, const void *ys, c
   if (!aligned(place, 4) || !aligned(w, 4) || !aligned(ys, dtype_bytes(d->ys_dtype)) ||
       !aligned(residual, dtype_bytes(d->res_dtype)) || !aligned(y, dtype_bytes(d->y_dtype)))
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  if (y == ys) return refuse(CEP_EINVAL, "%s: y overlaps ys", fn);
   UnsortArgs a = args_of(d);
   a.ys = ys, a.place = place, a.w = w, a.res = residual, a.y = y;
   auto *launch = a.k <= 8 ? launch_unsort<8, false> : launch_unsort<16, false>;
@@ -235,6 +236,7 @@ CEP_API int cep_expert_unsort_backward(const cep_expert_unsort_desc *d, const vo
       !aligned(ys, dtype_bytes(d->ys_dtype)) || !aligned(dys, dtype_bytes(d->ys_dtype)) ||
       !aligned(dy, dtype_bytes(d->y_dtype)))
     return refuse(CEP_EINVAL, "%s: a pointer is not aligned to its type", fn);
+  if (dys == dy) return refuse(CEP_EINVAL, "%s: dys overlaps dy", fn);
   UnsortArgs a = args_of(d);
   a.dy = dy, a.ys = ys, a.place = place, a.w = w, a.dys = dys, a.dw = dw;
   auto *launch = a.k <= 8 ? launch_grad<8, false> : launch_grad<16, false>;

@@ -1014,8 +1014,11 @@ CEP_API int cep_linear(const cep_linear_desc *d, const void *x, const void *w, c
   if (!workspace || workspace_bytes < cep_linear_workspace(d, 0))
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_linear_workspace(d, 0));
-  if (y == x || preact == x || (const void *)preact == y)
-    return refuse(CEP_EINVAL, "%s: y, preact and x overlap", fn);
+  for (const void *p : {x, w, (const void *)bias})
+    if (p && (y == p || preact == p))
+      return refuse(CEP_EINVAL, "%s: y or preact overlaps x, w or bias", fn);
+  if (preact && (preact == y || preact == mul || preact == residual))
+    return refuse(CEP_EINVAL, "%s: preact overlaps y, mul or residual", fn);
   const int D = d->d_in, N = d->d_out;
   Finish f{};
   f.bias = bias, f.mul = (const __bf16 *)mul, f.res = residual, f.y = y, f.pre = preact;
@@ -1049,7 +1052,11 @@ CEP_API int cep_linear_backward(const cep_linear_desc *d, const void *dy, const 
   if (!workspace || workspace_bytes < cep_linear_workspace(d, 1))
     return refuse(workspace ? CEP_ENOMEM : CEP_EINVAL, "%s: needs a workspace of %zu bytes", fn,
                   cep_linear_workspace(d, 1));
-  if (dx && (dx == dy || dx == x)) return refuse(CEP_EINVAL, "%s: dx overlaps dy or x", fn);
+  for (const void *p : {dy, x, w})
+    if (p && (dx == p || dw == p || dbias == p))
+      return refuse(CEP_EINVAL, "%s: dx, dw or dbias overlaps dy, x or w", fn);
+  for (const void *p : {mul, (const void *)preact})
+    if (p && dbias == p) return refuse(CEP_EINVAL, "%s: dbias overlaps mul or preact", fn);
   const int D = d->d_in, N = d->d_out, T = d->rows, n_groups = std::max(d->n_groups, 1);
   const Space space = space_of(d, 1);
   const Groups g{offsets, d->n_groups, T};

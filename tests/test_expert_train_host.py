@@ -175,6 +175,25 @@ def test_linear_refuses_outputs_over_its_inputs():
     _refused(cep.CEP_EINVAL, b, _linear(), y, x, w, BIG, dx=x, dw=PTR + 4096)
 
 
+def test_outputs_over_arrays_that_are_still_read_are_refused():
+    f, b = cep.cep_linear, cep.cep_linear_backward
+    x, w, y, v = (PTR + 4096 * i for i in range(4))
+    for over in (dict(y=w), dict(y=x), dict(bias=y)):
+        _refused(cep.CEP_EINVAL, f, _linear(), x, w, over.get("y", y), BIG, bias=over.get("bias"))
+    for name in ("bias", "mul", "residual"):
+        _refused(cep.CEP_EINVAL, f, _linear(), x, w, y, BIG, preact=v, **{name: v})
+    _refused(cep.CEP_EINVAL, f, _linear(), x, w, y, BIG, preact=w)
+    for out in ("dx", "dw", "dbias"):
+        for p in (y, x, w):
+            _refused(cep.CEP_EINVAL, b, _linear(), y, x, w, BIG, **{out: p})
+    for name in ("mul", "preact"):
+        _refused(cep.CEP_EINVAL, b, _linear(act=cep.CEP_SILU), y, x, w, BIG, dbias=v,
+                 **{"preact": PTR + 5 * 4096, name: v})
+    _refused(cep.CEP_EINVAL, cep.cep_expert_sort, _sort(), PTR, PTR, PTR, PTR, BIG, x=x, out_x=x)
+    _refused(cep.CEP_EINVAL, cep.cep_expert_unsort, _unsort(), x, PTR, x)
+    _refused(cep.CEP_EINVAL, cep.cep_expert_unsort_backward, _unsort(), x, y, PTR, None, x, None)
+
+
 # --------------------------------------------------------- routed experts
 
 def _routed(E=2, d=8, d_ff=16, top_k=2):

@@ -9,8 +9,9 @@
 // (dense_tile.h); the tiles of grouped rows are found on the device from the
 // groups' offsets, the grid covers their most.  Bound by HBM with few rows (24 rows on
 // eight weights of 4096 x 2048 25 us, 5.4 TB/s), else by the matrix instructions (8192 x
-// 2048 x 7168 with bias and GELU 179 us, 1.34 PFLOP/s) and, where the epilogue reads a
-// factor or keeps z, by its bytes (eight groups of 8192 x 2048 x 4096 with both 165 us).
+// 2048 x 7168 with bias and GELU 179 us among others, 1.34 PFLOP/s, 186 in a trace) and,
+// where the epilogue reads a factor or keeps z, by its bytes (eight groups of 8192 x 2048
+// x 4096 with both 166 us).
 #include "dense_tile.h"
 #include "rows_tile.h"
 
@@ -97,10 +98,9 @@ __device__ inline int group_of(const Groups &gr, int row) {
 // after the other rounded to float32 and the rest fitted anew).  2^(x^2 c) takes the
 // rounding errors of x^2, of c = -log2(e) / 2 and of their product back as a factor 1 + r
 // ln(2): without, they are 7.5e-6 of the value at x = 13 (8192 x 2048 x 7168 with GELU 168
-// us, 170 with).  As evaluated, Phi and the
-// density are within 2^-20 of their values for x up to 12.9, where Phi(-x) becomes
-// subnormal.  With the library's erfc the gradient of 4095 x 2048 GELUs took 24 us, bound
-// by its instructions.
+// us, 170 with).  As evaluated, Phi and the density are within 2^-20 of their values for x
+// up to 12.9, where Phi(-x) becomes subnormal.  With the library's erfc the gradient of
+// 4095 x 2048 GELUs took 24 us, bound by its instructions.
 __device__ inline float normal_cdf(float z, float *density = nullptr) {
   constexpr float kC = -0.721347511f, kCRest = -9.62981506e-9f;
   const float x = fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.31f, x, 1.0f));
@@ -321,8 +321,9 @@ struct TileWork {
 };
 
 // y (B_K false) or dx (true: N is d_in) in 128-wide tiles of whole groups' rows, two
-// workgroups of eight waves a compute unit.  4095 x 2048 x 4096 with GELU and z kept 84
-// us, 0.8 PFLOP/s: one round, whose tiles all store at its end.  (us, eight and four
+// workgroups of eight waves a compute unit.  4095 x 2048 x 4096 with GELU and z kept 87 to
+// 94 us from machine to machine, 0.73 to 0.79 PFLOP/s: one round, whose tiles all store at
+// its end.  (us, eight and four
 // waves: 777 x 6144 x 2560 with a residual 38.7, 39.7; 3000 x 1408 x 2048 in 16 groups
 // 41.4, 43.9; 378 x 1896 x 976 in two shares 11.2, 12.7; one workgroup a unit 50 for the
 // second)
@@ -548,9 +549,11 @@ __global__ __launch_bounds__(512, 6) void k_linear_wgrad_few(WgradArgs a) {
   }
 }
 
-// dW and dx in one launch: the weights of groups with more rows than dx has columns to
-// sum over, dx, the other weights, so that the longest tiles come first and the tiles of
-// one fill the compute units that the others' last round leaves.
+// dW and dx in one launch, so that the tiles of one fill the compute units that the others'
+// last round leaves: weights' gradients, as many groups' as have more rows than dx has
+// columns to sum over, then dx, then the other weights'.  Of 256-wide tiles the groups go
+// by size, so that the longest come first; of 128-wide ones in their own order, whichever
+// are the large ones (wgrad_item).
 template <int HALF, int WM, int WN, bool STAGED>
 __global__ __launch_bounds__(WM * WN * 64, HALF == 64 ? 4 : 2) void k_linear_grads(LinearArgs dx, WgradArgs dw) {
   constexpr int SIZE = 2 * HALF;
@@ -632,9 +635,13 @@ struct DzArgs {
 // dz and dm of a block's rows, and their sums over each group's rows there: those of
 // group g go to line blockIdx.x + g of `part` (from one pair of block and group to the
 // next, one of the two grows, so no line is written twice).  With one block the lines
-// are db, and those of groups without rows get zeros.  Bound by HBM: 4095 x 2048 from
-// bf16 with GELU and sums 15.7 us, 4.3 TB/s; 8192 x 2048 with SiLU and a factor 42, 4.8.
-// (Eight rows of four columns a lane at once, in fewer waves: 23 and 56.)
+// are db, and those of groups without rows get zeros.  dz is rounded to bf16, which the
+// matrix instructions of dx and dW take beside bf16 weights and rows: their error against
+// 64 bits is 2.34e-3 of their size, where their own rounding alone is 1.66e-3.  A second
+// term of dz would take those instructions twice (dx and dW of 4095 x 4096 x 2048: 110 us
+// of a step of 214).  Bound by HBM: 4095 x 2048 from bf16 with GELU and sums 16.6 us, 4.0
+// TB/s; 8192 x 2048 with SiLU and a factor 40, 5.0.  (Eight rows of four columns a lane at
+// once, in fewer waves: 23 and 56.)
 template <int ACT, int ROWS>
 __global__ __launch_bounds__(256) void k_linear_dz(DzArgs a) {
   __shared__ float sums[ROWS][kDzCols];
@@ -768,6 +775,9 @@ struct Plan {
 // the tiled product reads each weight once for all its rows, with fewer loads on the way
 // at a time (4096 x 2048, us streamed and tiled: 16 rows 6.4, 8.3; 32 7.5, 8.6; 48 11.3,
 // 9.2; of eight groups 3 rows each 24.9, 29.4; 8 30.4, 34.8; 12 40.2, 35.2; 32 42, 34).
+// The host knows the groups' mean alone, and these are of even groups.  With all rows in
+// one of many groups the streamed form reads that weight for every 16 of them: 10 rows a
+// group on average in one of 32 groups 35 us, tiled 33; in one of 256 208 and 60.
 constexpr int kStreamRows = 32, kStreamGroup = 10;
 
 Plan plan_of(int rows, int N, int K, int groups, bool may_stream) {
@@ -899,9 +909,11 @@ void launch_finish(const float *part, int splits, const Groups &g, const Finish 
                      dim3(kFinishThreads), 0, s, part, splits, g, f);
 }
 
-// The epilogue is staged except where it is a plain store (us, staged and not: 777 x
-// 6144 x 2560 with bias and residual 42, 47; 8192 x 2048 x 4096 in eight groups with
-// a factor 212, 229; plain 4095 x 4096 x 2048 68, 64).
+// The epilogue is staged, but for a dx that nothing is added to (us, staged and not: 777 x
+// 6144 x 2560 with bias and residual 42, 47; 8192 x 2048 x 4096 in eight groups with a
+// factor 212, 229; dx of 4095 x 4096 x 2048 68, 64).  Plain stores of y gain on neither
+// side (4095 x 4096 x 2048 55.8, 53.8; 8192 x 2048 x 4096 in eight groups 128, 127; 8192 x
+// 2048 x 7168 161, 159; 777 x 6144 x 2560 35.5, 36.7; 3000 x 1408 x 2048 in 16 30.3, 31.1).
 template <int TILE, bool B_K, bool STAGED, int ACT>
 void launch_kind(const LinearArgs &a, int64_t items, hipStream_t s) {
   // with groups fewer tiles may be live, and then quarters

@@ -118,6 +118,7 @@ class MoEBlock:
             raise ValueError(f"{T} tokens, the block holds {self.max_tokens}")
         _expect("x", x, self.y.device, (torch.float32, torch.bfloat16), (T, d))
         _expect("residual", residual, self.y.device, (torch.bfloat16,), (T, d))
+        self.saved = None  # a pass that fails keeps nothing
         mx = self.row_dtype == cep.CEP_MXFP8
         desc = cep.make_norm(rows=T, d=d, res_dtype=cep.CEP_BF16, w_dtype=cep.CEP_F32,
                              x_dtype=cep.CEP_F32 if x.dtype == torch.float32 else cep.CEP_BF16,
@@ -138,9 +139,7 @@ class MoEBlock:
         pre = torch.empty(T, 2, self.d_shared, device=y.device) if train else None
         cep.cep_gated_ffn(ffn, y, *self.shared, self.shared_y, self._ffn_space(ffn, train),
                           preact=pre, stream=s)
-        self.saved = None
-        if train:
-            self.saved = residual.clone(), y.clone(), pre, logits, self.ids[:T].clone()
+        saved = (residual.clone(), y.clone(), pre, logits, self.ids[:T].clone()) if train else None
         routed = self.routed[0, :T]
         routed.zero_()
         plan = self.plan.cpu()
@@ -158,6 +157,7 @@ class MoEBlock:
         else:
             cep.cep_submit_chunk(self.ctx, self.generation, 0, 0, 0, None, None, None, None, None)
         cep.cep_combine(self.ctx, s)
+        self.saved = saved
         return routed.add_(self.shared_y[:T])
 
     def backward(self, d_out, d_residual=None, d_y=None):
@@ -272,6 +272,7 @@ class RoutedExperts:
         _expect("w", w, dev, (torch.float32,), (T, k))
         if T * k > MAX_ROWS:
             raise ValueError(f"{T} tokens of {k} slots: the products take up to 2^21 rows")
+        self.saved = None  # a pass that fails keeps nothing
         with torch.cuda.device(dev):
             return self._forward(y, ids, w, train)
 
@@ -301,7 +302,6 @@ class RoutedExperts:
         total = self._buf(T, d, dtype=torch.float32)
         cep.cep_expert_unsort(self._unsort(T, cep.CEP_BF16, cep.CEP_F32), out, place, total, w=w,
                               stream=s)
-        self.saved = None
         if count is not None:
             sorted_.synchronize()
             if int(count):

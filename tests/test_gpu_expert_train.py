@@ -1133,3 +1133,30 @@ def test_routed_experts_sum_the_gradient_of_y_in_float32():
     parts = torch.stack(parts)
     assert not torch.equal(parts, parts.bfloat16().double()) and float(parts.abs().max()) < 2 ** 24
     assert torch.equal(d_y.double(), want)
+
+
+def test_a_pass_that_fails_leaves_nothing_to_go_back_through(monkeypatch):
+    T = 9
+    g, b, routed, x, res = _small_block(70, T)
+    b.forward(x, res, train=True)
+    routed.forward(b.y[:T], b.ids[:T], b.w[:T], train=True)
+
+    def fails(*a, **kw):
+        raise cep.CepError(cep.CEP_ENOMEM, "cep")
+
+    with monkeypatch.context() as m:
+        m.setattr(cep, "cep_linear", fails)
+        m.setattr(cep, "cep_dispatch", fails)
+        with pytest.raises(cep.CepError):
+            routed.forward(b.y[:T], b.ids[:T], b.w[:T], train=True)
+        with pytest.raises(cep.CepError):
+            b.forward(x, res, train=True)
+    with pytest.raises(ValueError):
+        routed.backward(x)
+    with pytest.raises(ValueError):
+        b.backward(x)
+    with pytest.raises(ValueError):
+        b.gate_backward(torch.zeros(T, 3, device="cuda"))
+    b.forward(x, res, train=True)
+    assert len(b.backward(x)) == 3
+    b.close()
